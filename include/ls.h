@@ -299,6 +299,66 @@ int ls_attn_core_bwd(const ls_block_cfg* cfg, const ls_bf16* qkv, const ls_bf16*
 int ls_attn_core_bwd_noalloc(const ls_block_cfg* cfg, const ls_bf16* qkv, const ls_bf16* o,
                              const float* lse, const ls_bf16* dout, ls_bf16* dqkv, void* stream);
 
+/* ---- packed sequences ----------------------------------------------------------
+ *
+ * Sequences of different lengths laid end to end in one row of `total` tokens,
+ * as training on documents has them, without padding between.  cu_seqlens
+ * (device, n_seqs + 1 int32) holds the first row of every sequence and, last,
+ * the row after the last sequence: sequence s is rows cu_seqlens[s] ..
+ * cu_seqlens[s+1] - 1.  Entries must not fall, start at 0 or more and end at
+ * `total` or less; a sequence may be empty.  Rows before the first and behind
+ * the last sequence belong to none: their inputs (whatever they hold, NaN
+ * too) reach no other row, and every output of theirs is left as it was.
+ * The library never reads cu_seqlens on the host.  Entries that break the rule
+ * give unspecified values in the outputs, with nothing read or written outside
+ * a buffer.
+ *
+ * Buffers are those of the attention core: qkv [total, (n_q_heads +
+ * 2*n_kv_heads)*head_dim], o [total, n_q_heads*head_dim], lse [n_q_heads, total].
+ * As there, NaN or infinities in a sequence's k and v may reach all rows of that
+ * sequence (a masked probability is 0, and 0 x NaN is NaN); they reach no other.
+ * They may exceed 2 GiB.  head_dim is 64 or 128; total < 2^28, total x n_q_heads
+ * < 2^31 and a row of qkv holds less than 2^20 features. */
+typedef struct {
+  int64_t total;
+  int32_t n_seqs;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+} ls_packed_cfg;
+
+/* The plan of one batch (opaque, device): where every row lies in its sequence
+ * and the tiles of all sequences in order of falling work.  Made once per batch
+ * and read by the calls below, forward and backward, of every layer; it depends
+ * on total, n_seqs and the contents of cu_seqlens only, and a call must be given
+ * the plan of its own total and n_seqs.  ls_packed_plan_bytes: 0 for a *cfg that
+ * the calls refuse. */
+size_t ls_packed_plan_bytes(const ls_packed_cfg* cfg);
+int ls_packed_plan(const ls_packed_cfg* cfg, const int32_t* cu_seqlens, void* plan, size_t plan_bytes,
+                   void* stream);
+
+/* RoPE with positions that restart at 0 in every sequence: pairs (i, i +
+ * head_dim/2) of each q and k head turn by p * theta^(-2i/head_dim) radians,
+ * with `inverse` by the negative angle (the gradient's way back: the gradient of
+ * q and k before the rotation from that behind it).  theta > 1.  dst == src
+ * works in place and leaves v alone; otherwise the buffers must not overlap and
+ * v is copied. */
+int ls_packed_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, float theta, int inverse,
+                   const ls_bf16* src, ls_bf16* dst, void* stream);
+
+/* Causal attention inside every sequence on q and k already rotated:
+ * ls_attn_core_fwd / _bwd with the mask start of i's sequence <= j <= i.  What a
+ * sequence gives does not depend on its neighbours, bit for bit, nor on where
+ * in the row it lies (of dk and dv: for a given total and n_seqs, which decide over
+ * how many workgroups a kv head's query heads are spread).  The backward takes o and lse of the forward call;
+ * workspace: at least ls_packed_attn_bwd_workspace(cfg) bytes. */
+int ls_packed_attn_fwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, const ls_bf16* qkv,
+                       ls_bf16* o, float* lse, void* stream);
+size_t ls_packed_attn_bwd_workspace(const ls_packed_cfg* cfg);
+int ls_packed_attn_bwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, const ls_bf16* qkv,
+                       const ls_bf16* o, const float* lse, const ls_bf16* dout, ls_bf16* dqkv, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
 /* RMSNorm over rows of length `hidden`: h = x * r * gamma, r = (mean x^2 + eps)^-1/2.
  * x, h: [rows, hidden] bf16; r: [rows] fp32. */
 int ls_rmsnorm_fwd(int64_t rows, int32_t hidden, float eps, const ls_bf16* x,
@@ -367,7 +427,8 @@ int ls_gemm_tile_override(int32_t bm, int32_t bn);
  * equals `label` (labels: "rmsnorm fwd", "qkv projection", "attention fwd",
  * "output projection", "gate/up projection", "down projection", "dact",
  * "dWd", "dh2", "dWg/dWu", "rmsnorm bwd", "dO", "dWo", "attention bwd",
- * "dh1", "dWqkv", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
+ * "dh1", "dWqkv", "packed plan", "packed rope", "packed attention fwd",
+ * "packed attention bwd", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
  * "logits", "cross-entropy", "dh head", "dE head", "loss", "embedding bwd",
  * and "adamw" for ls_adamw_step),
  * creating up to max_launches event pairs up front;

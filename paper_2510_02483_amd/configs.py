@@ -71,6 +71,17 @@ PRESETS = {c.name: c for c in (TINY, B3, B3_8K, B30, PAPER_3B, PAPER_30B)}
 
 
 @dataclass(frozen=True)
+class PackedConfig:
+    """Sequences of different lengths laid end to end in one row of tokens, and
+    the heads of the attention over them."""
+    total: int           # rows, those of no sequence included
+    n_seqs: int
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+
+
+@dataclass(frozen=True)
 class StackConfig:
     """A stack of identical blocks between a tied token embedding and a final
     RMSNorm + LM head, trained on next-token cross-entropy (Section 2.4)."""

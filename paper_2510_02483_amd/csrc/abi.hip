@@ -1073,6 +1073,110 @@ int ls_attn_core_bwd_noalloc(const ls_block_cfg* cfg, const ls_bf16* qkv, const 
   return LS_OK;
 }
 
+// ---- packed sequences --------------------------------------------------------------
+
+static int check_packed_cfg(const ls_packed_cfg* c, ls::PackedShape& p) {
+  if (!c) return fail(LS_ERR_NULL, "cfg is NULL");
+  if (c->total <= 0 || c->n_seqs <= 0 || c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
+    return fail(LS_ERR_SHAPE, "all sizes must be positive");
+  if (c->n_q_heads % c->n_kv_heads != 0)
+    return fail(LS_ERR_SHAPE, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", c->n_q_heads, c->n_kv_heads);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(LS_ERR_UNSUPPORTED, "packed sequences take head_dim 64 or 128 (got %d)", c->head_dim);
+  // rows and positions are 32-bit, a row's byte offset inside a 64-row tile too, and
+  // there is a workgroup per tile and head
+  if (c->total >= (int64_t)1 << 28) return fail(LS_ERR_SHAPE, "total (%lld) reaches 2^28", (long long)c->total);
+  if (((int64_t)c->n_q_heads + 2 * (int64_t)c->n_kv_heads) * c->head_dim >= (int64_t)1 << 20)
+    return fail(LS_ERR_SHAPE, "a row of q, k and v reaches 2^20 features");
+  if (c->total * c->n_q_heads >= (int64_t)1 << 31)
+    return fail(LS_ERR_SHAPE, "total x n_q_heads (%lld) reaches 2^31", (long long)(c->total * c->n_q_heads));
+  p = ls::PackedShape{c->total, c->n_seqs, c->n_q_heads, c->n_kv_heads, c->head_dim};
+  return LS_OK;
+}
+
+static size_t packed_qkv_bytes(const ls::PackedShape& p) { return (size_t)p.total * (p.nq + 2 * p.nkv) * p.d * 2; }
+static size_t packed_o_bytes(const ls::PackedShape& p) { return (size_t)p.total * p.nq * p.d * 2; }
+
+static int check_plan_bytes(const ls::PackedShape& p, size_t plan_bytes) {
+  const size_t need = ls::packed_plan_bytes(p);
+  if (plan_bytes < need) return fail(LS_ERR_WORKSPACE, "plan %zu < %zu bytes", plan_bytes, need);
+  return LS_OK;
+}
+
+size_t ls_packed_plan_bytes(const ls_packed_cfg* cfg) {
+  ls::PackedShape p;
+  return check_packed_cfg(cfg, p) ? 0 : ls::packed_plan_bytes(p);
+}
+
+int ls_packed_plan(const ls_packed_cfg* cfg, const int32_t* cu_seqlens, void* plan, size_t plan_bytes, void* stream) {
+  ls::PackedShape p;
+  if (int e = check_packed_cfg(cfg, p)) return e;
+  const Range in[] = {{cu_seqlens, ((size_t)p.n_seqs + 1) * 4, "cu_seqlens"}};
+  const Range out[] = {{plan, plan_bytes, "plan"}};
+  if (int e = check_ranges(in, 1, out, 1)) return e;
+  if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("packed plan", st, ls::packed_plan(p, cu_seqlens, plan, st));
+  return LS_OK;
+}
+
+int ls_packed_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, float theta, int inverse,
+                   const ls_bf16* src, ls_bf16* dst, void* stream) {
+  ls::PackedShape p;
+  if (int e = check_packed_cfg(cfg, p)) return e;
+  if (!(theta > 1.0f) || !(theta <= 3.4e38f)) return fail(LS_ERR_SHAPE, "theta must exceed 1 and be finite");
+  const size_t bytes = packed_qkv_bytes(p);
+  const bool in_place = src == dst;
+  const Range in[] = {{plan, plan_bytes, "plan"}, {src, bytes, "src"}};
+  const Range out[] = {{dst, bytes, "dst"}};
+  if (int e = check_ranges(in, in_place ? 1 : 2, out, 1)) return e;
+  if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("packed rope", st,
+          ls::packed_rope(p, plan, (double)theta, inverse != 0, (const bf16_t*)src, (bf16_t*)dst, st));
+  return LS_OK;
+}
+
+int ls_packed_attn_fwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, const ls_bf16* qkv, ls_bf16* o,
+                       float* lse, void* stream) {
+  ls::PackedShape p;
+  if (int e = check_packed_cfg(cfg, p)) return e;
+  const Range in[] = {{plan, plan_bytes, "plan"}, {qkv, packed_qkv_bytes(p), "qkv"}};
+  const Range out[] = {{o, packed_o_bytes(p), "o"}, {lse, (size_t)p.nq * p.total * 4, "lse"}};
+  if (int e = check_ranges(in, 2, out, 2)) return e;
+  if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("packed attention fwd", st, ls::packed_attn_fwd(p, plan, (const bf16_t*)qkv, (bf16_t*)o, lse, st));
+  return LS_OK;
+}
+
+size_t ls_packed_attn_bwd_workspace(const ls_packed_cfg* cfg) {
+  ls::PackedShape p;
+  return check_packed_cfg(cfg, p) ? 0 : ls::packed_attn_bwd_workspace(p);
+}
+
+int ls_packed_attn_bwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, const ls_bf16* qkv,
+                       const ls_bf16* o, const float* lse, const ls_bf16* dout, ls_bf16* dqkv, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  ls::PackedShape p;
+  if (int e = check_packed_cfg(cfg, p)) return e;
+  const Range in[] = {{plan, plan_bytes, "plan"},
+                      {qkv, packed_qkv_bytes(p), "qkv"},
+                      {o, packed_o_bytes(p), "o"},
+                      {lse, (size_t)p.nq * p.total * 4, "lse"},
+                      {dout, packed_o_bytes(p), "dout"}};
+  const Range out[] = {{dqkv, packed_qkv_bytes(p), "dqkv"}, {workspace, workspace_bytes, "workspace"}};
+  if (int e = check_ranges(in, 5, out, 2)) return e;
+  if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  const size_t need = ls::packed_attn_bwd_workspace(p);
+  if (workspace_bytes < need) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, need);
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("packed attention bwd", st,
+          ls::packed_attn_bwd(p, plan, (const bf16_t*)qkv, (const bf16_t*)o, lse, (const bf16_t*)dout, (bf16_t*)dqkv,
+                              workspace, st));
+  return LS_OK;
+}
+
 static int check_norm_shape(int64_t rows, int32_t hidden) {
   if (rows <= 0 || hidden <= 0) return fail(LS_ERR_SHAPE, "rows and hidden must be positive");
   if (hidden % 8) return fail(LS_ERR_SHAPE, "hidden %d is not a multiple of 8", hidden);

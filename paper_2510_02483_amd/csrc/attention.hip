@@ -38,8 +38,7 @@
 // first, which balances the triangular work over the compute units.
 #include <math.h>
 
-#include "common.h"
-#include "kernels.h"
+#include "packed.h"
 
 namespace ls {
 
@@ -52,6 +51,7 @@ constexpr int BQ = 128;       // queries per workgroup (forward, dQ)
 constexpr int BKV = 64;       // keys per tile (forward, dQ)
 constexpr int BWD_BKV = 128;  // keys per workgroup (dK/dV)
 constexpr int BWD_BQ = 64;    // queries per tile (dK/dV)
+static_assert(BQ == PACKED_ROWS && BWD_BKV == PACKED_ROWS, "one plan of packed sequences for all kernels");
 
 LS_DEV u32x4 load16(const bf16_t* p) { return *(const u32x4*)p; }
 LS_DEV u32x4 pack_frag(const f32x16& v, int r0) {
@@ -186,13 +186,29 @@ struct FragAddr {
 
 // Query-tile workgroups (forward, dQ): the 1-D grid runs the longest tiles
 // (highest query index, most keys) first.
+//
+// A tile belongs to one sequence: S rows from row row0 of the token-major
+// matrices, whose values of head h (log-sum-exp, D) start at vec0 of a vector
+// with one entry per token of a head.  Equal sequences (batch x seq) follow
+// from the workgroup's number, packed ones from the plan's list of tiles, which
+// is in order of falling work too; there S = 0 means that there is no tile (the
+// grid is as large as the list can be).
 struct QTile {
-  int qt, h, b;
+  int qt, h, S;
+  int64_t row0, vec0;
 };
-LS_DEV QTile q_tile(const AttnShape& sh) {
-  const int nqt = (sh.seq + BQ - 1) / BQ, per = sh.nq * sh.batch;
+template <bool PACKED>
+LS_DEV QTile q_tile(const AttnShape& sh, const PackedTile* tiles) {
   const int x = (int)blockIdx.x;
-  return QTile{nqt - 1 - x / per, (x % per) % sh.nq, (x % per) / sh.nq};
+  if constexpr (PACKED) {
+    const PackedTile t = packed_tile(tiles, x / sh.nq, sh.seq);
+    const int h = x % sh.nq;
+    return QTile{t.rank, h, t.len, t.start, (int64_t)h * sh.seq + t.start};
+  } else {
+    const int nqt = (sh.seq + BQ - 1) / BQ, per = sh.nq * sh.batch;
+    const int h = (x % per) % sh.nq, b = (x % per) / sh.nq;
+    return QTile{nqt - 1 - x / per, h, sh.seq, (int64_t)b * sh.seq, ((int64_t)b * sh.nq + h) * sh.seq};
+  }
 }
 
 // The two halves of a wave (lanes 0-31 and 32-63) hold the same 32 queries
@@ -216,21 +232,22 @@ LS_DEV float halves_sum(float x) {
 // log-sum-exp m + log2 l, does not depend on the reference point.
 constexpr float LAG = 8.0f;
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, const bf16_t* __restrict__ qkv,
-                                                           bf16_t* __restrict__ o, float* __restrict__ lse,
-                                                           float sl2) {
+template <int D, bool PACKED>
+__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, const PackedTile* __restrict__ tiles,
+                                                           const bf16_t* __restrict__ qkv, bf16_t* __restrict__ o,
+                                                           float* __restrict__ lse, float sl2) {
   __shared__ __attribute__((aligned(1024))) bf16_t Ks[2][BKV * D];
   __shared__ __attribute__((aligned(1024))) bf16_t Vs[2][BKV * D];
   // the scale in a register before the loop: a scalar load still in flight
   // at the loop entry makes the first LDS wait of every tile a full wait
   asm volatile("" : "+s"(sl2));
 
-  const int S = sh.seq, nq = sh.nq, nkv = sh.nkv;
-  const QTile qtile = q_tile(sh);
-  const int h = qtile.h, b = qtile.b, kvh = h / (nq / nkv);
+  const int nq = sh.nq, nkv = sh.nkv;
+  const QTile qtile = q_tile<PACKED>(sh, tiles);
+  if (PACKED && qtile.S == 0) return;
+  const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv);
   const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
-  const bf16_t* base = qkv + (int64_t)b * S * ld;
+  const bf16_t* base = qkv + qtile.row0 * ld;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 31, lh = lane >> 5;
   const int q0 = qtile.qt * BQ;
   const int qrow = q0 + 32 * wave + lr;
@@ -331,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, const bf
 
   if (qrow < S) {
     const float inv = 1.0f / l;
-    bf16_t* orow = o + ((int64_t)b * S + qrow) * nq * D + h * D;
+    bf16_t* orow = o + (qtile.row0 + qrow) * nq * D + h * D;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -340,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, const bf
         *(u32x2*)(orow + d) = u32x2{pack_bf2(oacc[i][4 * rq] * inv, oacc[i][4 * rq + 1] * inv),
                                     pack_bf2(oacc[i][4 * rq + 2] * inv, oacc[i][4 * rq + 3] * inv)};
       }
-    if (lh == 0) lse[((int64_t)b * nq + h) * S + qrow] = (m + log2f(l)) * LN2;
+    if (lh == 0) lse[qtile.vec0 + qrow] = (m + log2f(l)) * LN2;
   }
 }
 
@@ -448,8 +465,9 @@ LS_DEV void unrotate_store(const f32x16 (&acc)[D / 32], float scale, const float
 // slots before the end of tile t each wave waits for its loads of tile t+1
 // and for the other waves (whose reads of tile t-1 are then done), and the
 // loads of tile t+2 go into tile t-1's stage.
-template <int D, bool SPLIT>
-__global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, const bf16_t* __restrict__ qkv,
+template <int D, bool SPLIT, bool PACKED>
+__global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, const PackedTile* __restrict__ tiles,
+                                                                const bf16_t* __restrict__ qkv,
                                                                 const bf16_t* __restrict__ dout,
                                                                 const float* __restrict__ lse2,
                                                                 const float* __restrict__ Dv, bf16_t* __restrict__ dqkv,
@@ -475,14 +493,22 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, con
   __shared__ __attribute__((aligned(1024))) Stage stg[NST];
 
   const int hsplit = SPLIT ? hsplit_arg : 1;  // the unsplit instance folds every split term away
-  const int S = sh.seq, nq = sh.nq, nkv = sh.nkv, G = nq / nkv, Gs = SPLIT ? G / hsplit : G;
+  const int nq = sh.nq, nkv = sh.nkv, G = nq / nkv, Gs = SPLIT ? G / hsplit : G;
   const int per = nkv * sh.batch * hsplit, x = (int)blockIdx.x;
-  const int kvt = x / per, hs = (x % per) % hsplit, kvh = ((x % per) / hsplit) % nkv,
-            b = ((x % per) / hsplit) / nkv;
+  const int hs = (x % per) % hsplit, kvh = ((x % per) / hsplit) % nkv, b = ((x % per) / hsplit) / nkv;
+  int kvt = x / per, S = sh.seq;
+  int64_t row0 = (int64_t)b * S, vec0 = (int64_t)b * nq * S;  // this sequence's first row; its entry of head 0's vectors
+  if constexpr (PACKED) {
+    const PackedTile t = packed_tile(tiles, x / per, sh.seq);
+    if (t.len == 0) return;
+    kvt = (t.len + BWD_BKV - 1) / BWD_BKV - 1 - t.rank;  // the most work: the first keys
+    S = t.len;
+    row0 = vec0 = t.start;
+  }
   const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
   const int64_t ldo = (int64_t)nq * D;
-  const bf16_t* base = qkv + (int64_t)b * S * ld;
-  const bf16_t* dbase = dout + (int64_t)b * S * ldo;
+  const bf16_t* base = qkv + row0 * ld;
+  const bf16_t* dbase = dout + row0 * ldo;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
   const int kv0 = kvt * BWD_BKV;
@@ -497,8 +523,9 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, con
     const int h = kvh * G + hs * Gs + t / nqt, q0 = q_begin + (t % nqt) * BWD_BQ;
     tlq(base, ld, q0, S, h * D, stg[st].q, wave);
     tlo(dbase, ldo, q0, S, h * D, stg[st].o, wave);
-    if (wave == 0) load_vec64(rsrc(lse2 + ((int64_t)b * nq + h) * S, (uint32_t)S * 4), q0, S, stg[st].l, lane);
-    if (wave == 1) load_vec64(rsrc(Dv + ((int64_t)b * nq + h) * S, (uint32_t)S * 4), q0, S, stg[st].d, lane);
+    const int64_t v0 = vec0 + (int64_t)h * sh.seq;
+    if (wave == 0) load_vec64(rsrc(lse2 + v0, (uint32_t)S * 4), q0, S, stg[st].l, lane);
+    if (wave == 1) load_vec64(rsrc(Dv + v0, (uint32_t)S * 4), q0, S, stg[st].d, lane);
   };
   issue(0, 0);
   if (ntiles > 1) issue(1, 1);
@@ -620,7 +647,7 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, con
   // dK = scale * dS^T Q (un-rotated), dV = P^T dO.  Lane holds key kvrow.
   if (kvrow >= S) return;
   if constexpr (SPLIT) {  // partial sums of this workgroup's heads; lane holds columns 32i + 8(r/4) + 4lh + r%4
-    float* row = part + (((int64_t)hs * sh.batch * S + (int64_t)b * S + kvrow) * nkv + kvh) * (2 * D);
+    float* row = part + (((int64_t)hs * sh.batch * sh.seq + row0 + kvrow) * nkv + kvh) * (2 * D);
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -630,8 +657,8 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, con
         *(f32x4*)(row + D + c) = f32x4{dv[i][4 * rq], dv[i][4 * rq + 1], dv[i][4 * rq + 2], dv[i][4 * rq + 3]};
       }
   } else {
-    unrotate_store<D>(dk, scale, rope_cs, S, kvrow, lh, dqkv + ((int64_t)b * S + kvrow) * ld + (nq + kvh) * D);
-    unrotate_store<D>(dv, 1.0f, nullptr, S, kvrow, lh, dqkv + ((int64_t)b * S + kvrow) * ld + (nq + nkv + kvh) * D);
+    unrotate_store<D>(dk, scale, rope_cs, S, kvrow, lh, dqkv + (row0 + kvrow) * ld + (nq + kvh) * D);
+    unrotate_store<D>(dv, 1.0f, nullptr, S, kvrow, lh, dqkv + (row0 + kvrow) * ld + (nq + nkv + kvh) * D);
   }
 }
 
@@ -639,8 +666,11 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, con
 // order, then scale and inverse RoPE for dK, bf16 stores into dqkv.  One wave
 // per (token, kv head): lane l holds columns 4l .. 4l+3 of [dK | dV] (D = 128)
 // or 2l .. 2l+1 (D = 64); the RoPE partner of dK column c < D/2 is c + D/2.
+// rows_pos: null, or of packed sequences each row's position, negative where the
+// row belongs to none (and has no partial sums).
 template <int D>
-__global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, int hsplit, const float* __restrict__ part,
+__global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, const int32_t* __restrict__ rows_pos,
+                                                            int hsplit, const float* __restrict__ part,
                                                             bf16_t* __restrict__ dqkv, const float* __restrict__ rope_cs,
                                                             float scale) {
   constexpr int E = 2 * D / 64;  // columns per lane
@@ -650,6 +680,7 @@ __global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, int hs
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (token, kv head)
   if (w >= T * sh.nkv) return;
   const int64_t t = w / sh.nkv;
+  if (rows_pos && rows_pos[t] < 0) return;
   const int kvh = (int)(w % sh.nkv), pos = (int)(t % sh.seq);
   const int c0 = E * lane;  // first of this lane's columns in [dK | dV]
   float v[E];
@@ -706,8 +737,9 @@ __global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, int hs
 // block 0's dQ^T.  MFMA operands from LDS are read RA slots ahead into a ring
 // of registers within the tile; two workgroups per compute unit keep the
 // matrix cores busy across tile boundaries and while one wave waits.
-template <int D>
-__global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, const bf16_t* __restrict__ qkv,
+template <int D, bool PACKED>
+__global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, const PackedTile* __restrict__ tiles,
+                                                              const bf16_t* __restrict__ qkv,
                                                               const bf16_t* __restrict__ dout,
                                                               const float* __restrict__ lse2,
                                                               const float* __restrict__ Dv, bf16_t* __restrict__ dqkv,
@@ -722,12 +754,13 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, const
   __shared__ __attribute__((aligned(1024))) bf16_t Ks[2][BKV * D];
   __shared__ __attribute__((aligned(1024))) bf16_t Vs[2][BKV * D];
 
-  const int S = sh.seq, nq = sh.nq, nkv = sh.nkv;
-  const QTile qtile = q_tile(sh);
-  const int h = qtile.h, b = qtile.b, kvh = h / (nq / nkv);
+  const int nq = sh.nq, nkv = sh.nkv;
+  const QTile qtile = q_tile<PACKED>(sh, tiles);
+  if (PACKED && qtile.S == 0) return;
+  const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv);
   const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
   const int64_t ldo = (int64_t)nq * D;
-  const bf16_t* base = qkv + (int64_t)b * S * ld;
+  const bf16_t* base = qkv + qtile.row0 * ld;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
   const int q0 = qtile.qt * BQ;
@@ -745,10 +778,10 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, const
 #pragma unroll
   for (int s = 0; s < NSD; ++s) {
     qf[s] = qok ? load16(base + (int64_t)qrow * ld + h * D + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
-    df[s] = qok ? load16(dout + ((int64_t)b * S + qrow) * ldo + h * D + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
+    df[s] = qok ? load16(dout + (qtile.row0 + qrow) * ldo + h * D + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
   }
-  const float L2 = qok ? lse2[((int64_t)b * nq + h) * S + qrow] : 0.f;
-  const float Dq = qok ? Dv[((int64_t)b * nq + h) * S + qrow] : 0.f;
+  const float L2 = qok ? lse2[qtile.vec0 + qrow] : 0.f;
+  const float Dq = qok ? Dv[qtile.vec0 + qrow] : 0.f;
 
   f32x16 dq[NI];
 #pragma unroll
@@ -834,23 +867,36 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, const
     if (kt + 1 < nkt) step(std::integral_constant<int, 1>{}, kt + 1);
   }
   if (!qok) return;
-  unrotate_store<D>(dq, scale, rope_cs, S, qrow, lh, dqkv + ((int64_t)b * S + qrow) * ld + h * D);
+  unrotate_store<D>(dq, scale, rope_cs, S, qrow, lh, dqkv + (qtile.row0 + qrow) * ld + h * D);
 }
 
-template <int D>
-hipError_t attn_fwd_t(const AttnShape& sh, const bf16_t* qkv, bf16_t* o, float* lse, hipStream_t s) {
-  const unsigned grid = (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
+// What a launch of packed sequences takes from the plan (all null or 0 for equal ones).
+struct PackedView {
+  const PackedTile* tiles = nullptr;
+  const int32_t* pos = nullptr;
+  int64_t ntiles = 0;
+};
+
+template <int D, bool PACKED>
+hipError_t attn_fwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, bf16_t* o, float* lse,
+                      hipStream_t s) {
+  const unsigned grid = PACKED ? (unsigned)(pk.ntiles * sh.nq) : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
   const float sl2 = LOG2E / sqrtf((float)(sh.d_scale > 0 ? sh.d_scale : D));
-  hipLaunchKernelGGL((attn_fwd_kernel<D>), dim3(grid), dim3(256), 0, s, sh, qkv, o, lse, sl2);
+  hipLaunchKernelGGL((attn_fwd_kernel<D, PACKED>), dim3(grid), dim3(256), 0, s, sh, pk.tiles, qkv, o, lse, sl2);
   return hipGetLastError();
+}
+
+// Key tiles of all sequences (packed ones: as many as there can be).
+int64_t key_tiles(const AttnShape& sh, int64_t ntiles) {
+  return ntiles > 0 ? ntiles : (int64_t)((sh.seq + BWD_BKV - 1) / BWD_BKV) * sh.batch;
 }
 
 // Split of each kv head's query-head group over workgroups of the dK/dV
 // kernel: the smallest divisor of the group size that gives at least two
 // workgroups per compute unit (256 CUs), or the whole group.
-int dkdv_split(const AttnShape& sh) {
+int dkdv_split(const AttnShape& sh, int64_t ntiles) {
   const int G = sh.nq / sh.nkv;
-  const int64_t g1 = (int64_t)((sh.seq + BWD_BKV - 1) / BWD_BKV) * sh.nkv * sh.batch;
+  const int64_t g1 = key_tiles(sh, ntiles) * sh.nkv;
   for (int h = 1; h < G; ++h)
     if (G % h == 0 && g1 * h >= 512) return h;
   return G;
@@ -861,9 +907,17 @@ int64_t bwd_ws_head(const AttnShape& sh) {
   return 2 * (int64_t)sh.batch * sh.seq * sh.nq * (int64_t)sizeof(float);
 }
 
-template <int D>
-hipError_t attn_bwd_t(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, const float* lse, const bf16_t* dout,
-                      bf16_t* dqkv, const float* rope_cs, void* ws, hipStream_t s) {
+size_t bwd_workspace(const AttnShape& sh, int64_t ntiles) {
+  // D and the base-2 log-sum-exp of every query, then (when the dK/dV group
+  // is split) the fp32 partial dK | dV rows of every split
+  const int hsplit = dkdv_split(sh, ntiles);
+  const int64_t part = hsplit > 1 ? (int64_t)hsplit * sh.batch * sh.seq * sh.nkv * 2 * sh.d * (int64_t)sizeof(float) : 0;
+  return (size_t)(bwd_ws_head(sh) + part);
+}
+
+template <int D, bool PACKED>
+hipError_t attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, const bf16_t* o, const float* lse,
+                      const bf16_t* dout, bf16_t* dqkv, const float* rope_cs, void* ws, hipStream_t s) {
   const int64_t T = (int64_t)sh.batch * sh.seq;
   float* Dv = (float*)ws;
   float* lse2 = Dv + T * sh.nq;
@@ -872,50 +926,68 @@ hipError_t attn_bwd_t(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, c
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const float scale = 1.0f / sqrtf((float)(sh.d_scale > 0 ? sh.d_scale : D));
-  const int hsplit = dkdv_split(sh);
+  const int hsplit = dkdv_split(sh, pk.ntiles);
   float* part = hsplit > 1 ? (float*)((char*)ws + bwd_ws_head(sh)) : nullptr;
-  const unsigned gkv = (unsigned)((sh.seq + BWD_BKV - 1) / BWD_BKV) * sh.nkv * sh.batch * hsplit;
+  const unsigned gkv = (unsigned)(key_tiles(sh, pk.ntiles) * sh.nkv * hsplit);
   if (part)
-    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, true>), dim3(gkv), dim3(256), 0, s, sh, qkv, dout, (const float*)lse2,
-                       (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E, hsplit, part);
+    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, true, PACKED>), dim3(gkv), dim3(256), 0, s, sh, pk.tiles, qkv, dout,
+                       (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E, hsplit, part);
   else
-    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false>), dim3(gkv), dim3(256), 0, s, sh, qkv, dout,
+    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, PACKED>), dim3(gkv), dim3(256), 0, s, sh, pk.tiles, qkv, dout,
                        (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E, 1, nullptr);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (part) {
     const int64_t rows = T * sh.nkv;  // one wave each, four per workgroup
-    hipLaunchKernelGGL((attn_bwd_dkdv_reduce<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, sh, hsplit,
+    hipLaunchKernelGGL((attn_bwd_dkdv_reduce<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, sh, pk.pos, hsplit,
                        (const float*)part, dqkv, rope_cs, scale);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const unsigned gq = (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
-  hipLaunchKernelGGL((attn_bwd_dq_kernel<D>), dim3(gq), dim3(256), 0, s, sh, qkv, dout, (const float*)lse2,
-                     (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E);
+  const unsigned gq =
+      PACKED ? (unsigned)(pk.ntiles * sh.nq) : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
+  hipLaunchKernelGGL((attn_bwd_dq_kernel<D, PACKED>), dim3(gq), dim3(256), 0, s, sh, pk.tiles, qkv, dout,
+                     (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E);
   return hipGetLastError();
+}
+
+AttnShape packed_shape(const PackedShape& p) { return AttnShape{1, (int)p.total, p.nq, p.nkv, p.d}; }
+PackedView packed_view(const PackedShape& p, const void* plan) {
+  return PackedView{packed_tiles(plan), packed_pos(p, plan), packed_max_tiles(p)};
 }
 
 }  // namespace
 
 hipError_t attn_fwd(const AttnShape& sh, const bf16_t* qkv, bf16_t* o, float* lse, hipStream_t s) {
-  if (sh.d == 128) return attn_fwd_t<128>(sh, qkv, o, lse, s);
-  if (sh.d == 64) return attn_fwd_t<64>(sh, qkv, o, lse, s);
+  if (sh.d == 128) return attn_fwd_t<128, false>(sh, {}, qkv, o, lse, s);
+  if (sh.d == 64) return attn_fwd_t<64, false>(sh, {}, qkv, o, lse, s);
   return hipErrorInvalidValue;
 }
 
-size_t attn_bwd_workspace(const AttnShape& sh) {
-  // D and the base-2 log-sum-exp of every query, then (when the dK/dV group
-  // is split) the fp32 partial dK | dV rows of every split
-  const int hsplit = dkdv_split(sh);
-  const int64_t part = hsplit > 1 ? (int64_t)hsplit * sh.batch * sh.seq * sh.nkv * 2 * sh.d * (int64_t)sizeof(float) : 0;
-  return (size_t)(bwd_ws_head(sh) + part);
-}
+size_t attn_bwd_workspace(const AttnShape& sh) { return bwd_workspace(sh, 0); }
 
 hipError_t attn_bwd(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, const float* lse, const bf16_t* dout,
                     bf16_t* dqkv, const float* rope_cs, void* ws, hipStream_t s) {
-  if (sh.d == 128) return attn_bwd_t<128>(sh, qkv, o, lse, dout, dqkv, rope_cs, ws, s);
-  if (sh.d == 64) return attn_bwd_t<64>(sh, qkv, o, lse, dout, dqkv, rope_cs, ws, s);
+  if (sh.d == 128) return attn_bwd_t<128, false>(sh, {}, qkv, o, lse, dout, dqkv, rope_cs, ws, s);
+  if (sh.d == 64) return attn_bwd_t<64, false>(sh, {}, qkv, o, lse, dout, dqkv, rope_cs, ws, s);
+  return hipErrorInvalidValue;
+}
+
+hipError_t packed_attn_fwd(const PackedShape& p, const void* plan, const bf16_t* qkv, bf16_t* o, float* lse,
+                           hipStream_t s) {
+  const AttnShape sh = packed_shape(p);
+  if (p.d == 128) return attn_fwd_t<128, true>(sh, packed_view(p, plan), qkv, o, lse, s);
+  if (p.d == 64) return attn_fwd_t<64, true>(sh, packed_view(p, plan), qkv, o, lse, s);
+  return hipErrorInvalidValue;
+}
+
+size_t packed_attn_bwd_workspace(const PackedShape& p) { return bwd_workspace(packed_shape(p), packed_max_tiles(p)); }
+
+hipError_t packed_attn_bwd(const PackedShape& p, const void* plan, const bf16_t* qkv, const bf16_t* o, const float* lse,
+                           const bf16_t* dout, bf16_t* dqkv, void* ws, hipStream_t s) {
+  const AttnShape sh = packed_shape(p);
+  if (p.d == 128) return attn_bwd_t<128, true>(sh, packed_view(p, plan), qkv, o, lse, dout, dqkv, nullptr, ws, s);
+  if (p.d == 64) return attn_bwd_t<64, true>(sh, packed_view(p, plan), qkv, o, lse, dout, dqkv, nullptr, ws, s);
   return hipErrorInvalidValue;
 }
 

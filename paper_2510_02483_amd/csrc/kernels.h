@@ -112,6 +112,26 @@ size_t attn_bwd_workspace(const AttnShape& sh);
 hipError_t attn_bwd(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, const float* lse,
                     const bf16_t* dout, bf16_t* dqkv, const float* rope_cs, void* ws, hipStream_t s);
 
+// ---- packed sequences -------------------------------------------------------------
+// `total` rows hold n_seqs sequences end to end; see packed.h for the plan.
+constexpr int PACKED_ROWS = 128;  // rows of a tile of the plan (query and key tiles of the attention kernels)
+struct PackedShape {
+  int64_t total;
+  int n_seqs, nq, nkv, d;
+};
+int64_t packed_max_tiles(const PackedShape& p);
+size_t packed_tile_bytes(const PackedShape& p);  // bytes of the plan before the rows' positions
+size_t packed_plan_bytes(const PackedShape& p);
+hipError_t packed_plan(const PackedShape& p, const int32_t* cu, void* plan, hipStream_t s);
+// dst = q and k of src turned (v copied unless dst == src); rows of no sequence are left alone.
+hipError_t packed_rope(const PackedShape& p, const void* plan, double theta, int inverse, const bf16_t* src,
+                       bf16_t* dst, hipStream_t s);
+hipError_t packed_attn_fwd(const PackedShape& p, const void* plan, const bf16_t* qkv, bf16_t* o, float* lse,
+                           hipStream_t s);
+size_t packed_attn_bwd_workspace(const PackedShape& p);
+hipError_t packed_attn_bwd(const PackedShape& p, const void* plan, const bf16_t* qkv, const bf16_t* o, const float* lse,
+                           const bf16_t* dout, bf16_t* dqkv, void* ws, hipStream_t s);
+
 // ---- padded head layout (64 < d < 128 held in 128-wide slots) -------------------
 // Feature s of a head sits at slot s (s < d/2) or dp/2 + s - d/2; other slots are zero.
 hipError_t pad_head_rows(const bf16_t* src, bf16_t* dst, int heads, int d, int dp, int cols, hipStream_t s);

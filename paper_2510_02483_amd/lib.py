@@ -11,7 +11,7 @@ import os
 
 import torch
 
-from .configs import BlockConfig, StackConfig
+from .configs import BlockConfig, PackedConfig, StackConfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libls.so")
@@ -62,6 +62,11 @@ class LsStackGrads(ctypes.Structure):
                 ("layers", ctypes.POINTER(LsBlockGrads))]
 
 
+class LsPackedCfg(ctypes.Structure):
+    _fields_ = [("total", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
 class LsAdamwCfg(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
                 ("weight_decay", ctypes.c_float), ("max_norm", ctypes.c_float), ("step", ctypes.c_int32)]
@@ -83,6 +88,12 @@ _PROTOS = {
     "ls_attn_core_bwd_workspace": (ctypes.c_size_t, [_P]),
     "ls_attn_core_bwd": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "ls_attn_core_bwd_noalloc": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P]),
+    "ls_packed_plan_bytes": (ctypes.c_size_t, [_P]),
+    "ls_packed_plan": (ctypes.c_int, [_P, _P, _P, ctypes.c_size_t, _P]),
+    "ls_packed_rope": (ctypes.c_int, [_P, _P, ctypes.c_size_t, ctypes.c_float, ctypes.c_int, _P, _P, _P]),
+    "ls_packed_attn_fwd": (ctypes.c_int, [_P, _P, ctypes.c_size_t, _P, _P, _P, _P]),
+    "ls_packed_attn_bwd_workspace": (ctypes.c_size_t, [_P]),
+    "ls_packed_attn_bwd": (ctypes.c_int, [_P, _P, ctypes.c_size_t, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "ls_rmsnorm_fwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_float, _P, _P, _P, _P, _P]),
     "ls_rmsnorm_bwd_workspace": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int32]),
     "ls_rmsnorm_bwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P, ctypes.c_int, _P,
@@ -219,6 +230,50 @@ def ls_attn_core_bwd_noalloc(c, qkv, o, lse, dout, dqkv, stream=None):
     cfg = make_cfg(c)
     _check(lib().ls_attn_core_bwd_noalloc(ctypes.byref(cfg), _p(qkv), _p(o), _p(lse), _p(dout), _p(dqkv),
                                           _stream(stream)), "ls_attn_core_bwd_noalloc")
+
+
+def make_packed_cfg(c: PackedConfig) -> LsPackedCfg:
+    return LsPackedCfg(c.total, c.n_seqs, c.n_q_heads, c.n_kv_heads, c.head_dim)
+
+
+def _bytes(t) -> int:
+    return t.numel() * t.element_size()
+
+
+def ls_packed_plan_bytes(c) -> int:
+    cfg = make_packed_cfg(c)
+    return lib().ls_packed_plan_bytes(ctypes.byref(cfg))
+
+
+def ls_packed_plan(c, cu_seqlens, plan, stream=None):
+    """cu_seqlens: n_seqs + 1 int32 on the device; plan: a uint8 buffer of ls_packed_plan_bytes(c)."""
+    cfg = make_packed_cfg(c)
+    _check(lib().ls_packed_plan(ctypes.byref(cfg), _p(cu_seqlens), _p(plan), _bytes(plan), _stream(stream)),
+           "ls_packed_plan")
+
+
+def ls_packed_rope(c, plan, theta, src, dst, inverse=False, stream=None):
+    """q and k of every row turned by its position; dst may be src."""
+    cfg = make_packed_cfg(c)
+    _check(lib().ls_packed_rope(ctypes.byref(cfg), _p(plan), _bytes(plan), theta, int(inverse), _p(src), _p(dst),
+                                _stream(stream)), "ls_packed_rope")
+
+
+def ls_packed_attn_fwd(c, plan, qkv, o, lse, stream=None):
+    cfg = make_packed_cfg(c)
+    _check(lib().ls_packed_attn_fwd(ctypes.byref(cfg), _p(plan), _bytes(plan), _p(qkv), _p(o), _p(lse),
+                                    _stream(stream)), "ls_packed_attn_fwd")
+
+
+def ls_packed_attn_bwd_workspace(c) -> int:
+    cfg = make_packed_cfg(c)
+    return lib().ls_packed_attn_bwd_workspace(ctypes.byref(cfg))
+
+
+def ls_packed_attn_bwd(c, plan, qkv, o, lse, dout, dqkv, workspace, stream=None):
+    cfg = make_packed_cfg(c)
+    _check(lib().ls_packed_attn_bwd(ctypes.byref(cfg), _p(plan), _bytes(plan), _p(qkv), _p(o), _p(lse), _p(dout),
+                                    _p(dqkv), _p(workspace), _bytes(workspace), _stream(stream)), "ls_packed_attn_bwd")
 
 
 def ls_rmsnorm_fwd(rows, hidden, eps, x, gamma, h, r, stream=None):
