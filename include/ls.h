@@ -400,6 +400,47 @@ int ls_cross_entropy(int64_t tokens, int32_t seq, int32_t vocab, ls_bf16* logits
                      const int32_t* ids, const int32_t* targets, float* loss, float* row_loss,
                      void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- head loss: the cross-entropy of logits that are never kept -------------------
+ *
+ * For hidden states h [tokens, hidden] (behind the final norm) and head weights
+ * embed [vocab, hidden], with logits z = h embed^T formed tile by tile and not
+ * stored:
+ *
+ *   lse[t] = ln sum_v exp z[t,v];  row_loss[t] = lse[t] - z[t, targets[t]], 0
+ *   when targets[t] = -1;  loss = sum(row_loss) / max(N, 1),
+ *
+ * N = rows with a target in [0, vocab).  A target outside [-1, vocab) makes its
+ * row_loss, the loss, its row of dh and every row of the head's gradient NaN.  The logits stay in
+ * fp32 (ls_cross_entropy works on logits rounded to bf16).  The forward call by
+ * itself is an evaluation: it writes 8 bytes where 128 logits (64 for few tokens)
+ * would be.
+ *
+ * The backward call forms the logits again, `piece` columns of the vocabulary
+ * at a time (0: as many as keep one piece's gradient within 512 MiB; rounded up
+ * to a multiple of 64, and held to what one matrix operand may be), and gives, for
+ * the loss's own gradient dloss (one fp32 on the device; NULL: 1),
+ *
+ *   dz = (softmax(z) - onehot) dloss / max(N, 1)  (rows without a target: 0;
+ *        rounded to bf16, the operand of the next products)
+ *   dh = dz embed                     (bf16, summed in fp32; NULL: not wanted)
+ *   d_embed (+)= dz^T h               (fp32, added with `accumulate`; or
+ *   d_embed_bf16 = dz^T h              rounded once to bf16, without `accumulate`).
+ *
+ * At most one of d_embed and d_embed_bf16; both NULL for a frozen head.  lse is the
+ * forward call's, for the same h, embed and targets.
+ * hidden: a multiple of 8; tokens and vocab: any; tokens x hidden x 2 bytes below
+ * 2047 MiB, embed and its gradient may be larger.  workspace: at least
+ * ls_head_loss_workspace(tokens, hidden, vocab, piece) bytes, which serves the
+ * forward call too (with any piece).  Every output is deterministic. */
+size_t ls_head_loss_workspace(int64_t tokens, int32_t hidden, int32_t vocab, int32_t piece);
+int ls_head_loss_fwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf16* h, const ls_bf16* embed,
+                     const int32_t* targets, float* loss, float* row_loss, float* lse, void* workspace,
+                     size_t workspace_bytes, void* stream);
+int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf16* h, const ls_bf16* embed,
+                     const int32_t* targets, const float* lse, const float* dloss, ls_bf16* dh, float* d_embed,
+                     int accumulate, ls_bf16* d_embed_bf16, int32_t piece, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
 /* Token embedding rows: x[t] = embed[ids[t]] ([tokens, hidden] bf16; an id
  * outside [0, vocab) gives a NaN row), and its backward, which ADDS dx[t] into
  * d_embed[ids[t]] (fp32; the rows of repeated ids summed in token order, so
@@ -428,7 +469,8 @@ int ls_gemm_tile_override(int32_t bm, int32_t bn);
  * "output projection", "gate/up projection", "down projection", "dact",
  * "dWd", "dh2", "dWg/dWu", "rmsnorm bwd", "dO", "dWo", "attention bwd",
  * "dh1", "dWqkv", "packed plan", "packed rope", "packed attention fwd",
- * "packed attention bwd", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
+ * "packed attention bwd", "head loss logits", "head loss rows", "head loss coef",
+ * "head loss dz", "head loss dh", "head loss dE", "head loss dh rounding", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
  * "logits", "cross-entropy", "dh head", "dE head", "loss", "embedding bwd",
  * and "adamw" for ls_adamw_step),
  * creating up to max_launches event pairs up front;

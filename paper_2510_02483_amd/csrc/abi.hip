@@ -1505,6 +1505,208 @@ int ls_cross_entropy(int64_t tokens, int32_t seq, int32_t vocab, ls_bf16* logits
   return LS_OK;
 }
 
+// ---- head loss -------------------------------------------------------------------------
+
+// Columns of the pieces in which the vocabulary is taken, and the workspace.  Forward: statistics and target
+// logits.  Backward: the factor of the gradients, one piece's dz, dh in fp32 when there are several pieces, and
+// partial sums of products whose K is split.  One workspace serves either.
+struct HeadWs {
+  int64_t fwd_piece, bwd_piece, ldz;
+  size_t stats, zt, fwd_total;
+  size_t coef, dz, dh, kpart, bwd_total, total;
+  int64_t kpart_floats;
+  int64_t pieces(int64_t V) const { return (V + bwd_piece - 1) / bwd_piece; }
+};
+
+static constexpr int64_t kHeadDzBytes = (int64_t)512 << 20;  // dz of one piece, unless the caller says
+
+static ls::GemmArgs head_logits(int64_t T, int64_t H, int64_t V, int64_t col0, int64_t cols, int epi) {
+  ls::GemmArgs a;
+  a.M = (int)T;
+  a.N = (int)cols;
+  a.K = (int)H;
+  a.lda = a.ldb = H;
+  a.epi = epi;
+  a.col0 = (int)col0;
+  a.vocab = (int)V;
+  return a;
+}
+// dh (+)= dz E_piece: bf16 from a single piece, else summed in fp32
+static ls::GemmArgs head_dh(int64_t T, int64_t H, int64_t cols, int64_t ldz, bool single) {
+  ls::GemmArgs a;
+  a.M = (int)T;
+  a.N = (int)H;
+  a.K = (int)cols;
+  a.lda = ldz;
+  a.ldb = a.ldc = a.ldf = H;
+  a.b_kcontig = false;
+  a.epi = single ? ls::EPI_BF16 : ls::EPI_F32;
+  return a;
+}
+// dE_piece (+)= dz^T h
+static ls::GemmArgs head_de(int64_t T, int64_t H, int64_t cols, int64_t ldz, bool bf16) {
+  ls::GemmArgs a;
+  a.M = (int)cols;
+  a.N = (int)H;
+  a.K = (int)T;
+  a.lda = ldz;
+  a.ldb = a.ldc = a.ldf = H;
+  a.a_kcontig = a.b_kcontig = false;
+  a.epi = bf16 ? ls::EPI_BF16 : ls::EPI_F32;
+  return a;
+}
+
+static HeadWs head_ws(int64_t T, int64_t H, int64_t V, int64_t piece) {
+  HeadWs w;
+  // a piece's rows of E are one operand of a product, its dz another
+  auto fit = [&](int64_t p) { return std::max<int64_t>(p & ~(int64_t)255, 256); };
+  const int64_t most = fit((kMaxBytes - 1) / (2 * H));
+  w.fwd_piece = std::min(V, most);
+  const int64_t by_dz = piece > 0 ? (piece + 63) / 64 * 64 : fit(kHeadDzBytes / (2 * T));
+  w.bwd_piece = std::min({V, most, by_dz, std::max<int64_t>((kMaxBytes - 1) / (2 * T) / 64 * 64, 64)});
+  w.ldz = (w.bwd_piece + 63) / 64 * 64;
+  Carver f;
+  int64_t blocks = 0;
+  for (int64_t c0 = 0; c0 < V; c0 += w.fwd_piece) {
+    const int64_t cols = std::min(w.fwd_piece, V - c0);
+    const ls::GemmPlan p = ls::gemm_plan_free(head_logits(T, H, V, c0, cols, ls::EPI_LSE));
+    blocks += 2 * ((cols + p.bn - 1) / p.bn);
+  }
+  w.stats = f.take((size_t)(blocks * T * 8));
+  w.zt = f.take((size_t)T * 4);
+  w.fwd_total = f.off;
+  Carver b;
+  w.coef = b.take(16);
+  w.dz = b.take((size_t)(T * w.ldz * 2));
+  const bool single = w.bwd_piece == V;
+  w.dh = b.take(single ? 0 : (size_t)(T * H * 4));
+  w.kpart_floats = 0;
+  for (int64_t cols : {w.bwd_piece, V % w.bwd_piece ? V % w.bwd_piece : w.bwd_piece})
+    w.kpart_floats = std::max({w.kpart_floats, ls::gemm_kpart_floats(head_dh(T, H, cols, w.ldz, single)),
+                               ls::gemm_kpart_floats(head_de(T, H, cols, w.ldz, false)),
+                               ls::gemm_kpart_floats(head_de(T, H, cols, w.ldz, true))});
+  w.kpart = b.take((size_t)w.kpart_floats * 4);
+  w.bwd_total = b.off;
+  w.total = std::max(w.fwd_total, w.bwd_total);
+  return w;
+}
+
+static int check_head(int64_t tokens, int32_t hidden, int32_t vocab, int32_t piece) {
+  if (tokens <= 0 || hidden <= 0 || vocab <= 0 || hidden % 8 != 0)
+    return fail(LS_ERR_SHAPE, "tokens, vocab must be positive and hidden a positive multiple of 8");
+  if (piece < 0) return fail(LS_ERR_SHAPE, "piece must be >= 0");
+  if (vocab >= 1 << 30) return fail(LS_ERR_SHAPE, "vocab (%d) reaches 2^30", vocab);
+  // h is one operand of the products, and so are 256 rows of E and 64 columns of dz
+  if (tokens * hidden * 2 >= kMaxBytes || (int64_t)hidden * 256 * 2 >= kMaxBytes || tokens * 64 * 2 >= kMaxBytes)
+    return fail(LS_ERR_SHAPE, "problem too large (h, or the smallest piece, reaches 2047 MiB)");
+  return LS_OK;
+}
+
+size_t ls_head_loss_workspace(int64_t tokens, int32_t hidden, int32_t vocab, int32_t piece) {
+  return check_head(tokens, hidden, vocab, piece) ? 0 : head_ws(tokens, hidden, vocab, piece).total;
+}
+
+int ls_head_loss_fwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf16* h, const ls_bf16* embed,
+                     const int32_t* targets, float* loss, float* row_loss, float* lse, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  if (int e = check_head(tokens, hidden, vocab, 0)) return e;
+  const int64_t T = tokens, H = hidden, V = vocab;
+  const Range in[] = {{h, (size_t)(T * H * 2), "h"}, {embed, (size_t)(V * H * 2), "embed"}, {targets, (size_t)T * 4, "targets"}};
+  const Range out[] = {{loss, 4, "loss"},
+                       {row_loss, (size_t)T * 4, "row_loss"},
+                       {lse, (size_t)T * 4, "lse"},
+                       {workspace, workspace_bytes, "workspace"}};
+  if (int e = check_ranges(in, 3, out, 4)) return e;
+  const HeadWs w = head_ws(T, H, V, 0);
+  if (workspace_bytes < w.fwd_total) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, w.fwd_total);
+  const hipStream_t st = (hipStream_t)stream;
+  float* stats = at<float>(workspace, w.stats);
+  float* zt = at<float>(workspace, w.zt);
+  int64_t blocks = 0;
+  for (int64_t c0 = 0; c0 < V; c0 += w.fwd_piece) {
+    const int64_t cols = std::min(w.fwd_piece, V - c0);
+    ls::GemmArgs a = head_logits(T, H, V, c0, cols, ls::EPI_LSE);
+    a.A = (const bf16_t*)h;
+    a.B[0] = (const bf16_t*)embed + c0 * H;
+    a.target = targets;
+    a.stats = stats + blocks * T * 2;
+    a.zt = zt;
+    ls::GemmPlan used;
+    LS_STEP("head loss logits", st, ls::gemm(a, st, &used));
+    blocks += 2 * ((cols + used.bn - 1) / used.bn);
+  }
+  LS_STEP("head loss rows", st, ls::head_rows(T, (int)V, blocks, stats, zt, targets, lse, row_loss, loss, st));
+  return LS_OK;
+}
+
+int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf16* h, const ls_bf16* embed,
+                     const int32_t* targets, const float* lse, const float* dloss, ls_bf16* dh, float* d_embed,
+                     int accumulate, ls_bf16* d_embed_bf16, int32_t piece, void* workspace, size_t workspace_bytes,
+                     void* stream) {
+  if (int e = check_head(tokens, hidden, vocab, piece)) return e;
+  if (!dh && !d_embed && !d_embed_bf16) return fail(LS_ERR_NULL, "dh, d_embed and d_embed_bf16 are all NULL");
+  if (d_embed && d_embed_bf16) return fail(LS_ERR_UNSUPPORTED, "d_embed and d_embed_bf16 are both given");
+  const int64_t T = tokens, H = hidden, V = vocab;
+  Range in[5] = {{h, (size_t)(T * H * 2), "h"},
+                 {embed, (size_t)(V * H * 2), "embed"},
+                 {targets, (size_t)T * 4, "targets"},
+                 {lse, (size_t)T * 4, "lse"}};
+  size_t nin = 4, nout = 1;
+  if (dloss) in[nin++] = {dloss, 4, "dloss"};
+  Range out[4] = {{workspace, workspace_bytes, "workspace"}};
+  if (dh) out[nout++] = {dh, (size_t)(T * H * 2), "dh"};
+  if (d_embed) out[nout++] = {d_embed, (size_t)(V * H * 4), "d_embed"};
+  if (d_embed_bf16) out[nout++] = {d_embed_bf16, (size_t)(V * H * 2), "d_embed_bf16"};
+  if (int e = check_ranges(in, nin, out, nout)) return e;
+  const HeadWs w = head_ws(T, H, V, piece);
+  if (workspace_bytes < w.bwd_total) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, w.bwd_total);
+  const hipStream_t st = (hipStream_t)stream;
+  float* coef = at<float>(workspace, w.coef);
+  bf16_t* dz = at<bf16_t>(workspace, w.dz);
+  float* dh32 = at<float>(workspace, w.dh);
+  float* kpart = at<float>(workspace, w.kpart);
+  const bool single = w.bwd_piece == V;
+  LS_STEP("head loss coef", st, ls::head_coef(T, (int)V, targets, dloss, coef, st));
+  for (int64_t c0 = 0; c0 < V; c0 += w.bwd_piece) {
+    const int64_t cols = std::min(w.bwd_piece, V - c0);
+    {
+      ls::GemmArgs a = head_logits(T, H, V, c0, cols, ls::EPI_DZ);
+      a.A = (const bf16_t*)h;
+      a.B[0] = (const bf16_t*)embed + c0 * H;
+      a.target = targets;
+      a.lse = lse;
+      a.coef = coef;
+      a.C = dz;
+      a.ldc = w.ldz;
+      LS_STEP("head loss dz", st, ls::gemm(a, st));
+    }
+    if (dh) {
+      ls::GemmArgs a = head_dh(T, H, cols, w.ldz, single);
+      a.A = dz;
+      a.B[0] = (const bf16_t*)embed + c0 * H;
+      a.C = (bf16_t*)dh;
+      a.F[0] = dh32;
+      a.accumulate = c0 > 0;
+      a.kpart = kpart;
+      a.kpart_floats = w.kpart_floats;
+      LS_STEP("head loss dh", st, ls::gemm(a, st));
+    }
+    if (d_embed || d_embed_bf16) {
+      ls::GemmArgs a = head_de(T, H, cols, w.ldz, d_embed_bf16 != nullptr);
+      a.A = dz;
+      a.B[0] = (const bf16_t*)h;
+      if (d_embed) a.F[0] = d_embed + c0 * H;
+      else a.C = (bf16_t*)d_embed_bf16 + c0 * H;
+      a.accumulate = accumulate != 0;
+      a.kpart = kpart;
+      a.kpart_floats = w.kpart_floats;
+      LS_STEP("head loss dE", st, ls::gemm(a, st));
+    }
+  }
+  if (dh && !single) LS_STEP("head loss dh rounding", st, ls::round_bf16(T * H, dh32, (bf16_t*)dh, st));
+  return LS_OK;
+}
+
 int ls_embed_fwd(int64_t tokens, int32_t hidden, int32_t vocab, const int32_t* ids, const ls_bf16* embed, ls_bf16* x,
                  void* stream) {
   if (tokens <= 0 || hidden <= 0 || hidden % 8 != 0 || vocab <= 0)

@@ -211,19 +211,6 @@ LS_DEV QTile q_tile(const AttnShape& sh, const PackedTile* tiles) {
   }
 }
 
-// The two halves of a wave (lanes 0-31 and 32-63) hold the same 32 queries
-// at different keys: combine a per-lane value with the other half's, through a
-// lane swap on the vector unit rather than an LDS permute (which would also
-// wait for every LDS read in flight).
-LS_DEV float halves_max(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-LS_DEV float halves_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 // Online softmax with a lagging reference maximum: the running reference m
 // moves only when some query's scores exceed it by more than 2^LAG (base 2), so
 // that most tiles skip the rescale of O and l.  P = 2^(s - m) then lies in

@@ -198,3 +198,16 @@ LS_DEV float wave_sum(float v) {
   for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
+
+// Combine a per-lane value with the one that lane l ^ 32 holds (the MFMA result
+// layouts spread a row or column over the two halves of a wave), through a
+// lane swap on the vector unit rather than an LDS permute (which would also
+// wait for every LDS read in flight).
+LS_DEV float halves_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+LS_DEV float halves_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}

@@ -191,7 +191,7 @@ GemmPlan make_plan(const GemmArgs& a, int64_t kpart_floats, int forced) {
   const bool nt = a.a_kcontig && a.b_kcontig, f32 = a.epi == EPI_F32;
   // 192-wide tiles of a k-contiguous B put a wave's blocks in two 64-row segments: one buffer only
   const bool n192 = nt ? (a.epi == EPI_BF16 || a.epi == EPI_RESID) && a.b_start[1] >= a.N : a.epi != EPI_GLU_BWD;
-  const bool m192 = f32;
+  const bool m192 = f32 && !a.a_kcontig;
   const int ncu = compute_units();
   const int64_t ktiles = ((int64_t)a.K + KT - 1) / KT;
   GemmPlan best;
@@ -275,11 +275,13 @@ int64_t gemm_kpart_floats(const GemmArgs& a) {
   return need;
 }
 
+GemmPlan gemm_plan_free(const GemmArgs& a) { return make_plan(a, 0, 0); }
+
 GemmPlan gemm_plan(const GemmArgs& a, int64_t kpart_floats) {
   return make_plan(a, kpart_floats, g_tile_override.load(std::memory_order_relaxed));
 }
 
-hipError_t gemm(const GemmArgs& args, hipStream_t s) {
+hipError_t gemm(const GemmArgs& args, hipStream_t s, GemmPlan* used) {
   GemmArgs a = args;
   // A k-contiguous B split over buffers (or gate/up interleaved) is loaded a
   // wave's 64 rows at a time from one buffer: segments start at multiples of 64.
@@ -287,6 +289,7 @@ hipError_t gemm(const GemmArgs& args, hipStream_t s) {
     return hipErrorInvalidValue;
   if (!a.a_kcontig && a.b_kcontig) return hipErrorInvalidValue;
   const GemmPlan p = gemm_plan(a, a.kpart ? a.kpart_floats : 0);
+  if (used) *used = p;
   a.ksplit = p.ks;
   a.group_m = group_rows(a.M, a.N, a.K, p.bm, p.bn);
   const GemmTile t = p.bm == 128 ? (p.deep ? TILE_128_DEEP : TILE_128)
@@ -295,7 +298,10 @@ hipError_t gemm(const GemmArgs& args, hipStream_t s) {
                                                : (p.bn == 256 ? TILE_192x256 : TILE_192);
   const int epi = a.epi;
   if (p.ks > 1 && t == TILE_256 && epi != EPI_F32) a.epi = EPI_PART;
-  hipError_t e = a.a_kcontig ? (a.b_kcontig ? gemm_nt(a, t, s) : gemm_nn(a, t, s)) : gemm_tn(a, t, s);
+  const bool head = a.epi == EPI_LSE || a.epi == EPI_DZ || (a.a_kcontig && a.epi == EPI_F32) ||
+                    (!a.a_kcontig && a.epi != EPI_F32);
+  hipError_t e = head ? gemm_head(a, t, s)
+                      : a.a_kcontig ? (a.b_kcontig ? gemm_nt(a, t, s) : gemm_nn(a, t, s)) : gemm_tn(a, t, s);
   a.epi = epi;
   if (e != hipSuccess || p.ks == 1) return e;
   const int64_t items = a.epi == EPI_F32 ? (int64_t)a.M * a.N / 4 : (int64_t)a.M * a.N / 8;

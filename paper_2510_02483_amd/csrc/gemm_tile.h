@@ -350,6 +350,82 @@ LS_DEV void store_glu_bwd8(const GemmArgs& p, int m, int n, const float da[8]) {
   *(u32x4*)(dst + p.glu_I) = pack8f(du);
 }
 
+constexpr float EPI_LOG2E = 1.4426950408889634f;
+
+// EPI_LSE: per row the maximum and the sum of exponentials of a wave's columns
+// (32 TN from global column nw on, column block `block`), and the row's target
+// logit if it is among them; nothing else of the logits is kept.  Lanes l and
+// l + 32 hold a row's columns between them.  Columns past N count as -inf, and
+// a block without any finite logit gets the maximum -inf and the sum 0.  In
+// fp32 throughout; v_exp_f32 flushes terms below 2^-126 of the row's largest,
+// which are nothing next to it.
+template <int TM, int TN>
+LS_DEV void lse_epilogue(const GemmArgs& p, f32x16 (&acc)[TM][TN], int mw, int nw, int block, int lr, int lh) {
+  int t[TM];  // target as a column of the wave's
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = mw + 32 * i + lr;
+    t[i] = m < p.M ? p.target[m] : -1;
+    t[i] = t[i] < 0 ? -1 : t[i] - p.col0 - nw;
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = mw + 32 * i + lr;
+    if (nw + 32 * TN > p.N) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (nw + 32 * j + 8 * (r >> 2) + 4 * lh + (r & 3) >= p.N) acc[i][j][r] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
+    mx = halves_max(mx);
+    const float mb = mx == -INFINITY ? 0.f : mx * EPI_LOG2E;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r & 3] += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], EPI_LOG2E, -mb));
+    const float sum = halves_sum((s[0] + s[1]) + (s[2] + s[3]));
+    if (lh == 0 && m < p.M) *(float2*)(p.stats + 2 * ((int64_t)block * p.M + m)) = make_float2(mx, sum);
+    if (__builtin_amdgcn_ballot_w64(t[i] >= 0 && t[i] < 32 * TN)) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * j + 8 * (r >> 2) + 4 * lh + (r & 3) == t[i]) p.zt[m] = acc[i][j][r];
+    }
+  }
+}
+
+// EPI_DZ: what a row's logits become: (exp(z - lse) - [target]) coef, 0 in a row
+// without a target, NaN in one whose target is out of range.  One rounding, to
+// bf16, as the operand of the gradients' products.  (exp2 flushes probabilities
+// below 2^-126.)
+struct DzRow {
+  float l2, coef;
+  int t;
+  bool none;
+  LS_DEV DzRow() {}
+  LS_DEV DzRow(const GemmArgs& p, int m) {
+    const bool in = m < p.M;
+    t = in ? p.target[m] : -1;
+    l2 = in ? p.lse[m] * EPI_LOG2E : 0.f;
+    none = t == -1;
+    coef = t < -1 || t >= p.vocab ? NAN : p.coef[0];
+    t -= p.col0;
+  }
+  // logit z of the product's column n
+  LS_DEV float operator()(float z, int n) const {
+    const float d = __builtin_amdgcn_exp2f(fmaf(z, EPI_LOG2E, -l2)) - (n == t ? 1.f : 0.f);
+    return none ? 0.f : d * coef;
+  }
+};
+
 // Epilogue of a 128-column tile (all but the fp32 weight gradients): 8 columns
 // per lane and step, straight from the registers.  c0, c1: tile-local first
 // columns of the wave's two 32-column blocks.  When K is split, every slice
@@ -380,6 +456,15 @@ LS_DEV void small_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int m
         }
       } else if constexpr (EPI == EPI_ROPE || EPI == EPI_ROPE64) {
         if (na < p.N) store_rope8<EPI == EPI_ROPE ? 128 : 64>(p, m, na, a, b);
+      } else if constexpr (EPI == EPI_DZ) {
+        const DzRow row(p, m);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {  // columns past N, up to the next multiple of 8, become 0
+          a[e] = na + e < p.N ? row(a[e], na + e) : 0.f;
+          b[e] = nb + e < p.N ? row(b[e], nb + e) : 0.f;
+        }
+        if (na < p.N) *(u32x4*)(p.C + (int64_t)m * p.ldc + na) = pack8f(a);
+        if (nb < p.N) *(u32x4*)(p.C + (int64_t)m * p.ldc + nb) = pack8f(b);
       } else if constexpr (EPI == EPI_GLU_FWD) {
         const int f = n0 / 2 + c0 + o;
         if (f < p.glu_I) store_glu_fwd8(p, m, f, a, b);
@@ -714,6 +799,10 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
       ++kt;
     }
   });
+  if constexpr (EPI == EPI_LSE) {
+    lse_epilogue<TM, TN>(p, acc, m0 + wm * WM, n0 + wn * WN, 2 * tn + wn, lr, lh);
+    return;
+  }
   if constexpr (SMALL && EPI != EPI_F32) {
     small_epilogue<EPI, TM, TN>(p, acc, m0 + wm * WM, n0, bcol(0), bcol(1), slice, ks, lr, lh);
     return;
@@ -764,7 +853,7 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
     }
   };
 
-  if constexpr ((SMALL && EPI != EPI_F32) || EPI == EPI_PART) {
+  if constexpr ((SMALL && EPI != EPI_F32) || EPI == EPI_PART || EPI == EPI_LSE) {
   } else if constexpr (EPI == EPI_F32) {
     // fp32 weight gradients straight from the registers: a lane's 4 columns are
     // 16 contiguous bytes (read-modify-write with accumulate).  Slices 1.. of a
@@ -952,7 +1041,12 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
       }
     }
   } else {
-    // EPI_BF16, EPI_ROPE, EPI_ROPE64
+    // EPI_BF16, EPI_DZ, EPI_ROPE, EPI_ROPE64
+    DzRow dzr[TM];
+    if constexpr (EPI == EPI_DZ) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) dzr[i] = DzRow(p, mw + 32 * i + lr);
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int m = mw + 32 * i + lr;
@@ -1008,6 +1102,11 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+            if constexpr (EPI == EPI_DZ) {
+              const int n = nw + 32 * j + 8 * q + 4 * lh;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = n + e < p.N ? dzr[i](v[e], n + e) : 0.f;
+            }
             put4(32 * i + lr, 32 * j + 8 * q + 4 * lh, v);
           }
       }

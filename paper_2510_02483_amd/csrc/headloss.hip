@@ -1,0 +1,164 @@
+// The cross-entropy of logits h E^T that are never kept: what follows and precedes
+// the products (gemm_tile.h holds their epilogues).
+//
+// Forward: z = h E^T tile by tile; each wave leaves the maximum and the sum of
+// exponentials of its 128 (or 64) columns per row, 8 bytes for 128 logits, and the
+// target's logit.  head_rows_kernel joins a row's blocks:
+//   lse = M + ln sum_b s_b exp(m_b - M),  M = max m_b.
+// Backward, for each piece of the vocabulary: z again, dz = (exp(z - lse) -
+// onehot) dloss / N in bf16, then dh += dz E_piece in fp32 and dE_piece = dz^T h.
+//
+// The products are bound by the matrix cores (2 T V H operations each), the
+// kernels here by memory and latency: they move 16 bytes per row and column block.
+#include <math.h>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace ls {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int HL_THREADS = 1024;
+constexpr int HL_WAVES = HL_THREADS / 64;
+constexpr int HL_ROWS = 64;  // rows per workgroup, one per lane
+
+LS_DEV bool has_target(int t, int V) { return t >= 0 && t < V; }
+
+// Sums v and n over the workgroup in a fixed order (valid in thread 0).
+LS_DEV void block_sums(double& v, int& n, double* vp, int* np) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    v += __shfl_xor(v, o);
+    n += __shfl_xor(n, o);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    vp[threadIdx.x >> 6] = v;
+    np[threadIdx.x >> 6] = n;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    v = 0.0;
+    n = 0;
+    for (int w = 0; w < HL_WAVES; ++w) {
+      v += vp[w];
+      n += np[w];
+    }
+  }
+}
+
+// 64 rows per workgroup: wave w joins column blocks w, w + 16, .. of its lanes'
+// rows, then wave 0 joins the waves.  A lone workgroup also forms the loss.
+__global__ __launch_bounds__(HL_THREADS) void head_rows_kernel(int64_t T, int V, int64_t blocks,
+                                                               const float2* __restrict__ stats,
+                                                               const float* __restrict__ zt,
+                                                               const int32_t* __restrict__ targets,
+                                                               float* __restrict__ lse, float* __restrict__ row_loss,
+                                                               float* __restrict__ loss) {
+  __shared__ float pm[HL_WAVES][HL_ROWS], ps[HL_WAVES][HL_ROWS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * HL_ROWS + lane;
+  float m = -INFINITY, s = 0.f;
+  // a block without finite logits (max -inf, sum 0) changes nothing
+  auto join = [&](float bm, float bs) {
+    const float hi = fmaxf(m, bm);
+    const float ref = hi == -INFINITY ? 0.f : hi;
+    s = s * __builtin_amdgcn_exp2f((m - ref) * kLog2e) + bs * __builtin_amdgcn_exp2f((bm - ref) * kLog2e);
+    m = hi;
+  };
+  if (row < T) {
+#pragma unroll 4
+    for (int64_t b = wave; b < blocks; b += HL_WAVES) {
+      const float2 x = stats[b * T + row];
+      join(x.x, x.y);
+    }
+  }
+  pm[wave][lane] = m;
+  ps[wave][lane] = s;
+  __syncthreads();
+  if (wave != 0) return;
+  for (int w = 1; w < HL_WAVES; ++w) join(pm[w][lane], ps[w][lane]);
+  double sum = 0.0;
+  int n = 0;
+  if (row < T) {
+    const float l = m + __log2f(s) * kLn2;
+    const int t = targets[row];
+    const float r = t == -1 ? 0.f : has_target(t, V) ? l - zt[row] : NAN;
+    lse[row] = l;
+    row_loss[row] = r;
+    sum = r;
+    n = has_target(t, V);
+  }
+  if (gridDim.x == 1) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      sum += __shfl_xor(sum, o);
+      n += __shfl_xor(n, o);
+    }
+    if (lane == 0) loss[0] = (float)(sum / (double)max(n, 1));
+  }
+}
+
+// One workgroup: loss = sum of row losses over the rows that have a target, in fp64 in a fixed order.
+__global__ __launch_bounds__(HL_THREADS) void head_mean_kernel(int64_t T, int V, const int32_t* __restrict__ targets,
+                                                               const float* __restrict__ row_loss,
+                                                               float* __restrict__ loss) {
+  __shared__ double vp[HL_WAVES];
+  __shared__ int np[HL_WAVES];
+  double v = 0.0;
+  int n = 0;
+  for (int64_t t = threadIdx.x; t < T; t += HL_THREADS) {
+    v += (double)row_loss[t];
+    n += has_target(targets[t], V);
+  }
+  block_sums(v, n, vp, np);
+  if (threadIdx.x == 0) loss[0] = (float)(v / (double)max(n, 1));
+}
+
+__global__ __launch_bounds__(HL_THREADS) void head_coef_kernel(int64_t T, int V, const int32_t* __restrict__ targets,
+                                                               const float* __restrict__ dloss,
+                                                               float* __restrict__ coef) {
+  __shared__ double vp[HL_WAVES];
+  __shared__ int np[HL_WAVES];
+  double v = 0.0;
+  int n = 0;
+  for (int64_t t = threadIdx.x; t < T; t += HL_THREADS) n += has_target(targets[t], V);
+  block_sums(v, n, vp, np);
+  if (threadIdx.x == 0) coef[0] = (dloss ? dloss[0] : 1.0f) / (float)max(n, 1);
+}
+
+__global__ __launch_bounds__(256) void round_bf16_kernel(int64_t n8, const float* __restrict__ src,
+                                                         bf16_t* __restrict__ dst) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (int64_t)gridDim.x * 256) {
+    const f32x4 a = ((const f32x4*)src)[2 * i], b = ((const f32x4*)src)[2 * i + 1];
+    ((u32x4*)dst)[i] = u32x4{pack_bf2(a[0], a[1]), pack_bf2(a[2], a[3]), pack_bf2(b[0], b[1]), pack_bf2(b[2], b[3])};
+  }
+}
+
+}  // namespace
+
+hipError_t head_rows(int64_t T, int V, int64_t blocks, const float* stats, const float* zt, const int32_t* targets,
+                     float* lse, float* row_loss, float* loss, hipStream_t s) {
+  const unsigned grid = (unsigned)((T + HL_ROWS - 1) / HL_ROWS);
+  hipLaunchKernelGGL(head_rows_kernel, dim3(grid), dim3(HL_THREADS), 0, s, T, V, blocks, (const float2*)stats, zt,
+                     targets, lse, row_loss, loss);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || grid == 1) return e;
+  hipLaunchKernelGGL(head_mean_kernel, dim3(1), dim3(HL_THREADS), 0, s, T, V, targets, row_loss, loss);
+  return hipGetLastError();
+}
+
+hipError_t head_coef(int64_t T, int V, const int32_t* targets, const float* dloss, float* coef, hipStream_t s) {
+  hipLaunchKernelGGL(head_coef_kernel, dim3(1), dim3(HL_THREADS), 0, s, T, V, targets, dloss, coef);
+  return hipGetLastError();
+}
+
+hipError_t round_bf16(int64_t n, const float* src, bf16_t* dst, hipStream_t s) {
+  const int64_t n8 = n / 8, need = (n8 + 255) / 256;
+  hipLaunchKernelGGL(round_bf16_kernel, dim3((unsigned)(need < 4096 ? need : 4096)), dim3(256), 0, s, n8, src, dst);
+  return hipGetLastError();
+}
+
+}  // namespace ls

@@ -26,6 +26,8 @@ enum Epilogue {
   EPI_GLU_BWD = 4,  // C = dgu: dgu[m][i] = acc u silu'(g), dgu[m][I+i] = acc silu(g)
   EPI_F32 = 5,      // F (fp32, rows split over up to three buffers) (+)= acc
   EPI_PART = 6,     // kpart[slice] = acc: a slice of a split K (256 x 256 tiles; set by gemm())
+  EPI_LSE = 7,      // acc are logits: maximum and sum of exponentials per row and column block, target logits
+  EPI_DZ = 8,       // C (bf16) = the cross-entropy's gradient of the logits acc
 };
 
 struct GemmArgs {
@@ -52,6 +54,13 @@ struct GemmArgs {
   int f_start[3] = {0, 1 << 30, 1 << 30};
   int64_t ldf = 0;
   int accumulate = 0;
+  // EPI_LSE and EPI_DZ: columns are entries col0 .. col0 + N - 1 of a vocabulary, row m has target[m] (-1: none)
+  int col0 = 0, vocab = 0;
+  const int32_t* target = nullptr;
+  float* stats = nullptr;       // EPI_LSE: [column block][M] (max, sum of exp(z - max)); two blocks per tile column
+  float* zt = nullptr;          // EPI_LSE: [M], the logit of a row's target where this product has it
+  const float* lse = nullptr;   // EPI_DZ: [M]
+  const float* coef = nullptr;  // EPI_DZ: one factor of all gradients
   // fp32 workspace for splitting K over workgroups when the output tiles alone
   // would leave compute units idle (slices * M * N floats, one slice fewer for
   // EPI_F32, see gemm_kpart_floats); null or smaller means fewer slices or none.
@@ -69,7 +78,10 @@ struct GemmPlan {
 };
 // What gemm() chooses with kpart_floats of scratch (and the forced shape, if any).
 GemmPlan gemm_plan(const GemmArgs& a, int64_t kpart_floats);
-hipError_t gemm(const GemmArgs& a, hipStream_t s);
+// The same without scratch and whatever shape is forced; a forced one has no narrower columns.
+GemmPlan gemm_plan_free(const GemmArgs& a);
+// `used`, if given, gets the choice.
+hipError_t gemm(const GemmArgs& a, hipStream_t s, GemmPlan* used = nullptr);
 // Floats of GemmArgs::kpart with which a product of this shape and epilogue
 // runs with its full split of K (0: it is not split).
 int64_t gemm_kpart_floats(const GemmArgs& a);
@@ -81,6 +93,7 @@ enum GemmTile { TILE_256, TILE_256x192, TILE_192x256, TILE_192, TILE_256x128, TI
 hipError_t gemm_nt(const GemmArgs& a, GemmTile t, hipStream_t s);
 hipError_t gemm_nn(const GemmArgs& a, GemmTile t, hipStream_t s);
 hipError_t gemm_tn(const GemmArgs& a, GemmTile t, hipStream_t s);
+hipError_t gemm_head(const GemmArgs& a, GemmTile t, hipStream_t s);  // the instances that only the head loss uses
 // Force the tile shape of later gemm launches (bm, bn in {256, 192}; 0, 0 =
 // automatic).  Variants that only exist as 256 x 256 ignore it.  -1 on bad sizes.
 int gemm_tile_override(int bm, int bn);
@@ -156,6 +169,16 @@ hipError_t ce_rows(int64_t rows, int V, bf16_t* z, const int32_t* tg, const int*
                    hipStream_t s);
 // loss = sum(row_loss[0 .. T)) / max(counts[0], 1).
 hipError_t ce_loss(int64_t T, const float* row_loss, const int* counts, float* loss, hipStream_t s);
+
+// ---- head loss (cross-entropy of h E^T whose logits are not kept) ------------------
+// Per row from EPI_LSE's statistics (`blocks` column blocks): lse, row_loss (0 without a target, NaN for one
+// outside [-1, V)), and loss = sum(row_loss) / max(rows with a target in [0, V), 1).
+hipError_t head_rows(int64_t T, int V, int64_t blocks, const float* stats, const float* zt, const int32_t* targets,
+                     float* lse, float* row_loss, float* loss, hipStream_t s);
+// coef[0] = dloss[0] (null: 1) / max(rows with a target in [0, V), 1).
+hipError_t head_coef(int64_t T, int V, const int32_t* targets, const float* dloss, float* coef, hipStream_t s);
+// dst = src rounded to bf16, n a multiple of 8.
+hipError_t round_bf16(int64_t n, const float* src, bf16_t* dst, hipStream_t s);
 
 // ---- optimizer ------------------------------------------------------------------
 struct AdamwHyper {

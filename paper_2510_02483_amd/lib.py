@@ -107,6 +107,11 @@ _PROTOS = {
     "ls_cross_entropy_workspace": (ctypes.c_size_t, [ctypes.c_int64]),
     "ls_cross_entropy": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P, _P, _P,
                                         ctypes.c_size_t, _P]),
+    "ls_head_loss_workspace": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
+    "ls_head_loss_fwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P,
+                                        ctypes.c_size_t, _P]),
+    "ls_head_loss_bwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P,
+                                        ctypes.c_int, _P, ctypes.c_int32, _P, ctypes.c_size_t, _P]),
     "ls_embed_fwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P]),
     "ls_embed_bwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P]),
     "ls_adamw_workspace": (ctypes.c_size_t, []),
@@ -348,6 +353,28 @@ def ls_cross_entropy(logits, seq, ids, targets, loss, row_loss, workspace, strea
     _check(lib().ls_cross_entropy(T, int(seq), V, _p(logits), _p(ids), _p(targets), _p(loss), _p(row_loss),
                                   _p(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
            "ls_cross_entropy")
+
+
+def ls_head_loss_workspace(tokens: int, hidden: int, vocab: int, piece: int = 0) -> int:
+    return lib().ls_head_loss_workspace(int(tokens), int(hidden), int(vocab), int(piece))
+
+
+def ls_head_loss_fwd(h, embed, targets, loss, row_loss, lse, workspace, stream=None):
+    T, H = h.shape
+    _check(lib().ls_head_loss_fwd(T, H, embed.shape[0], _p(h), _p(embed), _p(targets), _p(loss), _p(row_loss), _p(lse),
+                                  _p(workspace), _bytes(workspace), _stream(stream)), "ls_head_loss_fwd")
+
+
+def ls_head_loss_bwd(h, embed, targets, lse, dloss, dh, d_embed, accumulate, workspace, piece=0, stream=None):
+    """dloss: one fp32 or None (1); dh or d_embed may be None; d_embed: fp32, added to with
+    ``accumulate``, or bf16, always overwritten."""
+    T, H = h.shape
+    low = d_embed is not None and d_embed.dtype == torch.bfloat16
+    if low and accumulate:
+        raise ValueError("a bf16 d_embed is overwritten, never added to")
+    _check(lib().ls_head_loss_bwd(T, H, embed.shape[0], _p(h), _p(embed), _p(targets), _p(lse), _p(dloss), _p(dh),
+                                  None if low else _p(d_embed), int(accumulate), _p(d_embed) if low else None,
+                                  int(piece), _p(workspace), _bytes(workspace), _stream(stream)), "ls_head_loss_bwd")
 
 
 def ls_embed_fwd(ids, embed, x, stream=None):
