@@ -420,11 +420,14 @@ int ls_cross_entropy(int64_t tokens, int32_t seq, int32_t vocab, ls_bf16* logits
  * to a multiple of 64, and held to what one matrix operand may be), and gives, for
  * the loss's own gradient dloss (one fp32 on the device; NULL: 1),
  *
- *   dz = (softmax(z) - onehot) dloss / max(N, 1)  (rows without a target: 0;
- *        rounded to bf16, the operand of the next products)
- *   dh = dz embed                     (bf16, summed in fp32; NULL: not wanted)
- *   d_embed (+)= dz^T h               (fp32, added with `accumulate`; or
- *   d_embed_bf16 = dz^T h              rounded once to bf16, without `accumulate`).
+ *   dz = softmax(z) - onehot            (rounded to bf16, the operand of the next
+ *        products; rows with targets[t] = -1 are left out, so that they cost
+ *        nothing here and their h may hold anything)
+ *   c  = dloss / max(N, 1)
+ *   dh = c dz embed                     (bf16, summed in fp32; 0 in the rows left
+ *                                        out; NULL: not wanted)
+ *   d_embed (+)= c dz^T h               (fp32, added with `accumulate`; or
+ *   d_embed_bf16 = c dz^T h              rounded once to bf16, without `accumulate`).
  *
  * At most one of d_embed and d_embed_bf16; both NULL for a frozen head.  lse is the
  * forward call's, for the same h, embed and targets.
@@ -469,8 +472,8 @@ int ls_gemm_tile_override(int32_t bm, int32_t bn);
  * "output projection", "gate/up projection", "down projection", "dact",
  * "dWd", "dh2", "dWg/dWu", "rmsnorm bwd", "dO", "dWo", "attention bwd",
  * "dh1", "dWqkv", "packed plan", "packed rope", "packed attention fwd",
- * "packed attention bwd", "head loss logits", "head loss rows", "head loss coef",
- * "head loss dz", "head loss dh", "head loss dE", "head loss dh rounding", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
+ * "packed attention bwd", "head loss logits", "head loss rows", "head loss slots",
+ * "head loss gather", "head loss dz", "head loss dh", "head loss dE", "head loss scatter", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
  * "logits", "cross-entropy", "dh head", "dE head", "loss", "embedding bwd",
  * and "adamw" for ls_adamw_step),
  * creating up to max_launches event pairs up front;

@@ -1508,14 +1508,14 @@ int ls_cross_entropy(int64_t tokens, int32_t seq, int32_t vocab, ls_bf16* logits
 // ---- head loss -------------------------------------------------------------------------
 
 // Columns of the pieces in which the vocabulary is taken, and the workspace.  Forward: statistics and target
-// logits.  Backward: the factor of the gradients, one piece's dz, dh in fp32 when there are several pieces, and
-// partial sums of products whose K is split.  One workspace serves either.
+// logits.  Backward: the rows that have a target (their number, places, targets, lse and h), the factor of the
+// gradients, one piece's dz, dh of those rows in fp32, and partial sums of products whose K is split.  One
+// workspace serves either.
 struct HeadWs {
   int64_t fwd_piece, bwd_piece, ldz;
   size_t stats, zt, fwd_total;
-  size_t coef, dz, dh, kpart, bwd_total, total;
+  size_t coef, rows, slot, tc, lc, hc, dz, dh, kpart, bwd_total, total;
   int64_t kpart_floats;
-  int64_t pieces(int64_t V) const { return (V + bwd_piece - 1) / bwd_piece; }
 };
 
 static constexpr int64_t kHeadDzBytes = (int64_t)512 << 20;  // dz of one piece, unless the caller says
@@ -1531,19 +1531,19 @@ static ls::GemmArgs head_logits(int64_t T, int64_t H, int64_t V, int64_t col0, i
   a.vocab = (int)V;
   return a;
 }
-// dh (+)= dz E_piece: bf16 from a single piece, else summed in fp32
-static ls::GemmArgs head_dh(int64_t T, int64_t H, int64_t cols, int64_t ldz, bool single) {
+// dh (+)= dz E_piece
+static ls::GemmArgs head_dh(int64_t T, int64_t H, int64_t cols, int64_t ldz) {
   ls::GemmArgs a;
   a.M = (int)T;
   a.N = (int)H;
   a.K = (int)cols;
   a.lda = ldz;
-  a.ldb = a.ldc = a.ldf = H;
+  a.ldb = a.ldf = H;
   a.b_kcontig = false;
-  a.epi = single ? ls::EPI_BF16 : ls::EPI_F32;
+  a.epi = ls::EPI_DH;
   return a;
 }
-// dE_piece (+)= dz^T h
+// dE_piece (+)= coef dz^T h
 static ls::GemmArgs head_de(int64_t T, int64_t H, int64_t cols, int64_t ldz, bool bf16) {
   ls::GemmArgs a;
   a.M = (int)cols;
@@ -1552,7 +1552,7 @@ static ls::GemmArgs head_de(int64_t T, int64_t H, int64_t cols, int64_t ldz, boo
   a.lda = ldz;
   a.ldb = a.ldc = a.ldf = H;
   a.a_kcontig = a.b_kcontig = false;
-  a.epi = bf16 ? ls::EPI_BF16 : ls::EPI_F32;
+  a.epi = bf16 ? ls::EPI_DE16 : ls::EPI_DE;
   return a;
 }
 
@@ -1577,12 +1577,16 @@ static HeadWs head_ws(int64_t T, int64_t H, int64_t V, int64_t piece) {
   w.fwd_total = f.off;
   Carver b;
   w.coef = b.take(16);
+  w.rows = b.take(16);
+  w.slot = b.take((size_t)T * 4);
+  w.tc = b.take((size_t)T * 4);
+  w.lc = b.take((size_t)T * 4);
+  w.hc = b.take((size_t)(T * H * 2));
   w.dz = b.take((size_t)(T * w.ldz * 2));
-  const bool single = w.bwd_piece == V;
-  w.dh = b.take(single ? 0 : (size_t)(T * H * 4));
+  w.dh = b.take((size_t)(T * H * 4));
   w.kpart_floats = 0;
   for (int64_t cols : {w.bwd_piece, V % w.bwd_piece ? V % w.bwd_piece : w.bwd_piece})
-    w.kpart_floats = std::max({w.kpart_floats, ls::gemm_kpart_floats(head_dh(T, H, cols, w.ldz, single)),
+    w.kpart_floats = std::max({w.kpart_floats, ls::gemm_kpart_floats(head_dh(T, H, cols, w.ldz)),
                                ls::gemm_kpart_floats(head_de(T, H, cols, w.ldz, false)),
                                ls::gemm_kpart_floats(head_de(T, H, cols, w.ldz, true))});
   w.kpart = b.take((size_t)w.kpart_floats * 4);
@@ -1662,29 +1666,34 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
   if (workspace_bytes < w.bwd_total) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, w.bwd_total);
   const hipStream_t st = (hipStream_t)stream;
   float* coef = at<float>(workspace, w.coef);
+  int* rows = at<int>(workspace, w.rows);
+  int32_t* slot = at<int32_t>(workspace, w.slot);
+  int32_t* tc = at<int32_t>(workspace, w.tc);
+  float* lc = at<float>(workspace, w.lc);
+  bf16_t* hc = at<bf16_t>(workspace, w.hc);
   bf16_t* dz = at<bf16_t>(workspace, w.dz);
   float* dh32 = at<float>(workspace, w.dh);
   float* kpart = at<float>(workspace, w.kpart);
-  const bool single = w.bwd_piece == V;
-  LS_STEP("head loss coef", st, ls::head_coef(T, (int)V, targets, dloss, coef, st));
+  LS_STEP("head loss slots", st, ls::head_slots(T, (int)V, targets, dloss, slot, rows, coef, st));
+  LS_STEP("head loss gather", st, ls::head_gather(T, (int)H, slot, (const bf16_t*)h, targets, lse, hc, tc, lc, st));
   for (int64_t c0 = 0; c0 < V; c0 += w.bwd_piece) {
     const int64_t cols = std::min(w.bwd_piece, V - c0);
     {
       ls::GemmArgs a = head_logits(T, H, V, c0, cols, ls::EPI_DZ);
-      a.A = (const bf16_t*)h;
+      a.A = hc;
       a.B[0] = (const bf16_t*)embed + c0 * H;
-      a.target = targets;
-      a.lse = lse;
-      a.coef = coef;
+      a.target = tc;
+      a.lse = lc;
+      a.rows = rows;
       a.C = dz;
       a.ldc = w.ldz;
       LS_STEP("head loss dz", st, ls::gemm(a, st));
     }
     if (dh) {
-      ls::GemmArgs a = head_dh(T, H, cols, w.ldz, single);
+      ls::GemmArgs a = head_dh(T, H, cols, w.ldz);
       a.A = dz;
       a.B[0] = (const bf16_t*)embed + c0 * H;
-      a.C = (bf16_t*)dh;
+      a.rows = rows;
       a.F[0] = dh32;
       a.accumulate = c0 > 0;
       a.kpart = kpart;
@@ -1694,7 +1703,9 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
     if (d_embed || d_embed_bf16) {
       ls::GemmArgs a = head_de(T, H, cols, w.ldz, d_embed_bf16 != nullptr);
       a.A = dz;
-      a.B[0] = (const bf16_t*)h;
+      a.B[0] = hc;
+      a.rows = rows;
+      a.coef = coef;
       if (d_embed) a.F[0] = d_embed + c0 * H;
       else a.C = (bf16_t*)d_embed_bf16 + c0 * H;
       a.accumulate = accumulate != 0;
@@ -1703,7 +1714,7 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
       LS_STEP("head loss dE", st, ls::gemm(a, st));
     }
   }
-  if (dh && !single) LS_STEP("head loss dh rounding", st, ls::round_bf16(T * H, dh32, (bf16_t*)dh, st));
+  if (dh) LS_STEP("head loss scatter", st, ls::head_scatter(T, (int)H, slot, coef, dh32, (bf16_t*)dh, st));
   return LS_OK;
 }
 

@@ -69,6 +69,10 @@ __global__ __launch_bounds__(256) void ksplit_finish_kernel(GemmArgs p) {
       store_rope8<HD>(p, m, n, a, b);
     } else {
       sum_slices8(p, m, c, a);
+      if constexpr (EPI == EPI_DE16) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] *= p.coef[0];
+      }
       if constexpr (EPI == EPI_GLU_BWD) store_glu_bwd8(p, m, c, a);
       else if constexpr (EPI == EPI_RESID) store_resid8(p, m, c, a);
       else *(u32x4*)(p.C + (int64_t)m * p.ldc + c) = pack8f(a);
@@ -182,16 +186,17 @@ int ksplit_of(int M, int N, int K) {
 }
 
 // Floats of kpart that `ks` slices need (slice 0 of a weight gradient goes to its buffer).
+bool f32_out(int epi) { return epi == EPI_F32 || epi == EPI_DH || epi == EPI_DE; }
 int64_t kpart_need(const GemmArgs& a, int ks) {
-  return ks <= 1 ? 0 : (int64_t)(a.epi == EPI_F32 ? ks - 1 : ks) * a.M * a.N;
+  return ks <= 1 ? 0 : (int64_t)(f32_out(a.epi) ? ks - 1 : ks) * a.M * a.N;
 }
 
 // forced: 0, or the tile shape of ls_gemm_tile_override (1000 BM + BN).
 GemmPlan make_plan(const GemmArgs& a, int64_t kpart_floats, int forced) {
-  const bool nt = a.a_kcontig && a.b_kcontig, f32 = a.epi == EPI_F32;
+  const bool nt = a.a_kcontig && a.b_kcontig, f32 = f32_out(a.epi);
   // 192-wide tiles of a k-contiguous B put a wave's blocks in two 64-row segments: one buffer only
   const bool n192 = nt ? (a.epi == EPI_BF16 || a.epi == EPI_RESID) && a.b_start[1] >= a.N : a.epi != EPI_GLU_BWD;
-  const bool m192 = f32 && !a.a_kcontig;
+  const bool m192 = a.epi == EPI_F32;
   const int ncu = compute_units();
   const int64_t ktiles = ((int64_t)a.K + KT - 1) / KT;
   GemmPlan best;
@@ -271,7 +276,7 @@ int gemm_tile_override(int bm, int bn) {
 int64_t gemm_kpart_floats(const GemmArgs& a) {
   int64_t need = kpart_need(a, make_plan(a, INT64_MAX, 0).ks);
   // the split a forced tile shape would use
-  if (a.epi == EPI_F32) need = std::max(need, kpart_need(a, ksplit_of(a.M, a.N, a.K)));
+  if (f32_out(a.epi)) need = std::max(need, kpart_need(a, ksplit_of(a.M, a.N, a.K)));
   return need;
 }
 
@@ -297,18 +302,19 @@ hipError_t gemm(const GemmArgs& args, hipStream_t s, GemmPlan* used) {
                                  : p.bm == 256 ? (p.bn == 256 ? TILE_256 : TILE_256x192)
                                                : (p.bn == 256 ? TILE_192x256 : TILE_192);
   const int epi = a.epi;
-  if (p.ks > 1 && t == TILE_256 && epi != EPI_F32) a.epi = EPI_PART;
-  const bool head = a.epi == EPI_LSE || a.epi == EPI_DZ || (a.a_kcontig && a.epi == EPI_F32) ||
-                    (!a.a_kcontig && a.epi != EPI_F32);
-  hipError_t e = head ? gemm_head(a, t, s)
-                      : a.a_kcontig ? (a.b_kcontig ? gemm_nt(a, t, s) : gemm_nn(a, t, s)) : gemm_tn(a, t, s);
+  if (p.ks > 1 && t == TILE_256 && !f32_out(epi)) a.epi = EPI_PART;
+  hipError_t e = epi >= EPI_LSE ? gemm_head(a, t, s)
+                 : a.a_kcontig ? (a.b_kcontig ? gemm_nt(a, t, s) : gemm_nn(a, t, s)) : gemm_tn(a, t, s);
   a.epi = epi;
   if (e != hipSuccess || p.ks == 1) return e;
-  const int64_t items = a.epi == EPI_F32 ? (int64_t)a.M * a.N / 4 : (int64_t)a.M * a.N / 8;
+  const int64_t items = f32_out(a.epi) ? (int64_t)a.M * a.N / 4 : (int64_t)a.M * a.N / 8;
   const dim3 grid((unsigned)std::min<int64_t>((items + 255) / 256, 256 * 8)), block(256);
   switch (a.epi) {
-    case EPI_F32: hipLaunchKernelGGL(kpart_reduce_kernel, grid, block, 0, s, a); break;
+    case EPI_F32:
+    case EPI_DH:
+    case EPI_DE: hipLaunchKernelGGL(kpart_reduce_kernel, grid, block, 0, s, a); break;
     case EPI_BF16: hipLaunchKernelGGL((ksplit_finish_kernel<EPI_BF16>), grid, block, 0, s, a); break;
+    case EPI_DE16: hipLaunchKernelGGL((ksplit_finish_kernel<EPI_DE16>), grid, block, 0, s, a); break;
     case EPI_RESID: hipLaunchKernelGGL((ksplit_finish_kernel<EPI_RESID>), grid, block, 0, s, a); break;
     case EPI_ROPE:
       if (a.head_dim == 64) hipLaunchKernelGGL((ksplit_finish_kernel<EPI_ROPE64>), grid, block, 0, s, a);

@@ -402,27 +402,26 @@ LS_DEV void lse_epilogue(const GemmArgs& p, f32x16 (&acc)[TM][TN], int mw, int n
   }
 }
 
-// EPI_DZ: what a row's logits become: (exp(z - lse) - [target]) coef, 0 in a row
-// without a target, NaN in one whose target is out of range.  One rounding, to
-// bf16, as the operand of the gradients' products.  (exp2 flushes probabilities
-// below 2^-126.)
+// EPI_DZ: what a row's logits become: softmax(z) - onehot, NaN in a row whose
+// target is out of range.  One rounding, to bf16, as the operand of the
+// gradients' products; the loss's factor comes after them, in fp32: with it, the
+// target's entry, the largest, would be one number close to -dloss / N in every
+// row and carry the same rounding error in all, which no sum evens out (errors
+// of dh and dE 0.0039 of their norm against 0.0024 so).  exp2 flushes
+// probabilities below 2^-126.
 struct DzRow {
-  float l2, coef;
+  float l2;
   int t;
-  bool none;
   LS_DEV DzRow() {}
-  LS_DEV DzRow(const GemmArgs& p, int m) {
-    const bool in = m < p.M;
-    t = in ? p.target[m] : -1;
-    l2 = in ? p.lse[m] * EPI_LOG2E : 0.f;
-    none = t == -1;
-    coef = t < -1 || t >= p.vocab ? NAN : p.coef[0];
+  LS_DEV DzRow(const GemmArgs& p, int M, int m) {
+    const bool in = m < M;
+    t = in ? p.target[m] : 0;
+    l2 = in ? (t >= 0 && t < p.vocab ? p.lse[m] * EPI_LOG2E : NAN) : 0.f;
     t -= p.col0;
   }
   // logit z of the product's column n
   LS_DEV float operator()(float z, int n) const {
-    const float d = __builtin_amdgcn_exp2f(fmaf(z, EPI_LOG2E, -l2)) - (n == t ? 1.f : 0.f);
-    return none ? 0.f : d * coef;
+    return __builtin_amdgcn_exp2f(fmaf(z, EPI_LOG2E, -l2)) - (n == t ? 1.f : 0.f);
   }
 };
 
@@ -431,8 +430,8 @@ struct DzRow {
 // columns of the wave's two 32-column blocks.  When K is split, every slice
 // stores its fp32 partial sums ([slice][M][N]) for ksplit_finish_kernel.
 template <int EPI, int TM, int TN>
-LS_DEV void small_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw, int n0, int c0, int c1, int slice,
-                           int ks, int lr, int lh) {
+LS_DEV void small_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int M, int mw, int n0, int c0, int c1,
+                           int slice, int ks, int lr, int lh) {
   static_assert(TN == 2, "two 32-column blocks per wave");
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
@@ -443,7 +442,7 @@ LS_DEV void small_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int m
       cols8(acc[i][0], pp, a);
       cols8(acc[i][1], pp, b);
       const int o = 16 * pp + 8 * lh, na = n0 + c0 + o, nb = n0 + c1 + o;
-      if (m >= p.M) continue;
+      if (m >= M) continue;
       if (ks > 1) {
         float* row = p.kpart + ((int64_t)slice * p.M + m) * p.N;
         if (na < p.N) {
@@ -457,7 +456,7 @@ LS_DEV void small_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int m
       } else if constexpr (EPI == EPI_ROPE || EPI == EPI_ROPE64) {
         if (na < p.N) store_rope8<EPI == EPI_ROPE ? 128 : 64>(p, m, na, a, b);
       } else if constexpr (EPI == EPI_DZ) {
-        const DzRow row(p, m);
+        const DzRow row(p, M, m);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {  // columns past N, up to the next multiple of 8, become 0
           a[e] = na + e < p.N ? row(a[e], na + e) : 0.f;
@@ -475,6 +474,14 @@ LS_DEV void small_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int m
         if (na < p.N) store_resid8(p, m, na, a);
         if (nb < p.N) store_resid8(p, m, nb, b);
       } else {
+        if constexpr (EPI == EPI_DE16) {
+          const float c = p.coef[0];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            a[e] *= c;
+            b[e] *= c;
+          }
+        }
         if (na < p.N) *(u32x4*)(p.C + (int64_t)m * p.ldc + na) = pack8f(a);
         if (nb < p.N) *(u32x4*)(p.C + (int64_t)m * p.ldc + nb) = pack8f(b);
       }
@@ -525,6 +532,12 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
   constexpr int BS = KSTEPS - RA;  // the k-step of a tile that holds the barrier
   constexpr bool KSEG = !BKC;  // a k-strided B may come from up to three buffers along k
   constexpr bool GLU = EPI == EPI_GLU_FWD;
+  constexpr bool F32OUT = EPI == EPI_F32 || EPI == EPI_DH || EPI == EPI_DE;
+  // the head loss's products count only the rows that have a target, as many as
+  // the device says (a split product with k-strided operands and a bf16 result
+  // is one of them too)
+  constexpr bool DEV_M = EPI == EPI_DZ || EPI == EPI_DH;
+  constexpr bool DEV_K = EPI == EPI_DE || EPI == EPI_DE16 || (EPI == EPI_PART && !AK);
   constexpr uint32_t A_BYTES = AK ? (BM / 8) * KC_PITCH : BM * KT * 2;
   constexpr uint32_t B_BYTES = BKC ? (BN / 8) * KC_PITCH : BN * KT * 2;
   constexpr uint32_t RING_BYTES = ST * A_BYTES + SB * B_BYTES;  // [A stages | B stages]
@@ -538,14 +551,20 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / 2, wn = wave % 2;
-  const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN;
+  int M = p.M;
+  if constexpr (DEV_M) M = max(0, min(M, p.rows[0]));
+  const int tiles_m = (M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN;
   // K may be split: workgroup x runs slice x / tiles of tile x % tiles
   const int ks = p.ksplit;
+  if constexpr (DEV_M) {
+    if ((int)blockIdx.x >= tiles_m * tiles_n * ks) return;
+  }
   const int slice = ks > 1 ? (int)blockIdx.x / (tiles_m * tiles_n) : 0;
   int tm, tn;
   map_tile((int)blockIdx.x - slice * tiles_m * tiles_n, tiles_m, tiles_n, p.group_m, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
-  const int K = p.K;
+  int K = p.K;
+  if constexpr (DEV_K) K = max(0, min(K, p.rows[0]));
 
   // k segments of B: [0, S1), [S1, S2), [S2, K) (one segment unless a
   // k-strided B is split over buffers).  The tiles of a segment start at its
@@ -570,9 +589,9 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
   OpLoads<NA> la;
   OpLoads<NB> lb;
   if constexpr (AK) {
-    kc_setup(la, p.A, m0 + 64 * (wave * NA >> 3), p.M, p.lda, lane, wave * NA);
+    kc_setup(la, p.A, m0 + 64 * (wave * NA >> 3), M, p.lda, lane, wave * NA);
   } else {
-    ks_setup<NA, BM, NW>(la, m0, p.M, p.lda, wave, lane);
+    ks_setup<NA, BM, NW>(la, m0, M, p.lda, wave, lane);
     la.r = rsrc(p.A, clamp_bytes((int64_t)K * p.lda * 2));
   }
   if constexpr (BKC) {
@@ -803,8 +822,8 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
     lse_epilogue<TM, TN>(p, acc, m0 + wm * WM, n0 + wn * WN, 2 * tn + wn, lr, lh);
     return;
   }
-  if constexpr (SMALL && EPI != EPI_F32) {
-    small_epilogue<EPI, TM, TN>(p, acc, m0 + wm * WM, n0, bcol(0), bcol(1), slice, ks, lr, lh);
+  if constexpr (SMALL && !F32OUT) {
+    small_epilogue<EPI, TM, TN>(p, acc, M, m0 + wm * WM, n0, bcol(0), bcol(1), slice, ks, lr, lh);
     return;
   }
   if constexpr (EPI == EPI_PART) {  // a slice's fp32 partial sums ([slice][M][N]) for ksplit_finish_kernel
@@ -848,17 +867,19 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
     for (int t = 0; t < WM / 4; ++t) {
       const int c = lane + 64 * t, r = c >> 4, cc = c & 15;
       const u32x4 v = *(const u32x4*)&stg[sb(r, cc * 8)];
-      if (cc < WN / 8 && mw + r < p.M && cc * 8 < ncols_valid)
+      if (cc < WN / 8 && mw + r < M && cc * 8 < ncols_valid)
         *(u32x4*)(dst + (int64_t)(mw + r) * ldd + col0 + cc * 8) = v;
     }
   };
 
-  if constexpr ((SMALL && EPI != EPI_F32) || EPI == EPI_PART || EPI == EPI_LSE) {
-  } else if constexpr (EPI == EPI_F32) {
+  if constexpr ((SMALL && !F32OUT) || EPI == EPI_PART || EPI == EPI_LSE) {
+  } else if constexpr (F32OUT) {
     // fp32 weight gradients straight from the registers: a lane's 4 columns are
     // 16 contiguous bytes (read-modify-write with accumulate).  Slices 1.. of a
     // split K store plain partial sums ([M][N] each) for kpart_reduce_kernel.
     float* kp = slice > 0 ? p.kpart + (int64_t)(slice - 1) * p.M * p.N : nullptr;
+    float coef = 1.f;
+    if constexpr (EPI == EPI_DE) coef = p.coef[0];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int m = mw + 32 * i + lr;
@@ -875,7 +896,7 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
         for (int q = 0; q < 4; ++q) {
           const int n = nw + 32 * j + 8 * q + 4 * lh;
           old[j][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-          if (p.accumulate && !kp && m < p.M && n < p.N) old[j][q] = *(const f32x4*)(row + n);
+          if (p.accumulate && !kp && m < M && n < p.N) old[j][q] = *(const f32x4*)(row + n);
         }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -883,8 +904,9 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int n = nw + 32 * j + 8 * q + 4 * lh;
-          const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-          if (m < p.M && n < p.N) *(f32x4*)(row + n) = v + old[j][q];
+          f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+          if constexpr (EPI == EPI_DE) v *= coef;
+          if (m < M && n < p.N) *(f32x4*)(row + n) = v + old[j][q];
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -1041,11 +1063,13 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
       }
     }
   } else {
-    // EPI_BF16, EPI_DZ, EPI_ROPE, EPI_ROPE64
+    // EPI_BF16, EPI_DZ, EPI_DE16, EPI_ROPE, EPI_ROPE64
+    float coef = 1.f;
+    if constexpr (EPI == EPI_DE16) coef = p.coef[0];
     DzRow dzr[TM];
     if constexpr (EPI == EPI_DZ) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) dzr[i] = DzRow(p, mw + 32 * i + lr);
+      for (int i = 0; i < TM; ++i) dzr[i] = DzRow(p, M, mw + 32 * i + lr);
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -1106,6 +1130,10 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
               const int n = nw + 32 * j + 8 * q + 4 * lh;
 #pragma unroll
               for (int e = 0; e < 4; ++e) v[e] = n + e < p.N ? dzr[i](v[e], n + e) : 0.f;
+            }
+            if constexpr (EPI == EPI_DE16) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] *= coef;
             }
             put4(32 * i + lr, 32 * j + 8 * q + 4 * lh, v);
           }

@@ -5,11 +5,16 @@
 // exponentials of its 128 (or 64) columns per row, 8 bytes for 128 logits, and the
 // target's logit.  head_rows_kernel joins a row's blocks:
 //   lse = M + ln sum_b s_b exp(m_b - M),  M = max m_b.
-// Backward, for each piece of the vocabulary: z again, dz = (exp(z - lse) -
-// onehot) dloss / N in bf16, then dh += dz E_piece in fp32 and dE_piece = dz^T h.
+// Backward: the n rows that have a target are gathered first, so that prompts and
+// padding cost nothing and whatever their h holds (uninitialised memory, NaN) reaches
+// no gradient; n stays on the device, where the products read it.  Then for each piece
+// of the vocabulary: z again, dz = softmax(z) - onehot in bf16, dh += dz E_piece in
+// fp32 and dE_piece = (dloss / N) dz^T h.  At the end dh goes back to its rows, times
+// dloss / N, in bf16.
 //
-// The products are bound by the matrix cores (2 T V H operations each), the
-// kernels here by memory and latency: they move 16 bytes per row and column block.
+// The products are bound by the matrix cores (2 T V H operations forward, 6 n V H
+// backward), the kernels here by memory and latency: 8 bytes per row and column
+// block forward, a copy of h and of dh backward.
 #include <math.h>
 
 #include "common.h"
@@ -117,23 +122,77 @@ __global__ __launch_bounds__(HL_THREADS) void head_mean_kernel(int64_t T, int V,
   if (threadIdx.x == 0) loss[0] = (float)(v / (double)max(n, 1));
 }
 
-__global__ __launch_bounds__(HL_THREADS) void head_coef_kernel(int64_t T, int V, const int32_t* __restrict__ targets,
-                                                               const float* __restrict__ dloss,
-                                                               float* __restrict__ coef) {
+// One workgroup: every row's place among the rows that have a target (kept in their
+// order), their number, and the factor of all gradients.
+__global__ __launch_bounds__(HL_THREADS) void head_slots_kernel(int64_t T, int V, const int32_t* __restrict__ targets,
+                                                                const float* __restrict__ dloss,
+                                                                int32_t* __restrict__ slot, int* __restrict__ rows,
+                                                                float* __restrict__ coef) {
+  __shared__ int part[2][HL_WAVES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0, valid = 0, buf = 0;
+  for (int64_t t0 = 0; t0 < T; t0 += HL_THREADS, buf ^= 1) {
+    const int64_t t = t0 + threadIdx.x;
+    const int g = t < T ? targets[t] : -1;
+    valid += has_target(g, V);
+    const unsigned long long in = __ballot(g != -1);
+    if (lane == 0) part[buf][wave] = __popcll(in);
+    __syncthreads();  // (two buffers: the next round's writes meet no reads of this one)
+    int at = before;
+    for (int w = 0; w < HL_WAVES; ++w) {
+      if (w < wave) at += part[buf][w];
+      before += part[buf][w];
+    }
+    if (t < T) slot[t] = g == -1 ? -1 : at + __popcll(in & ((1ull << lane) - 1));
+  }
   __shared__ double vp[HL_WAVES];
   __shared__ int np[HL_WAVES];
   double v = 0.0;
-  int n = 0;
-  for (int64_t t = threadIdx.x; t < T; t += HL_THREADS) n += has_target(targets[t], V);
-  block_sums(v, n, vp, np);
-  if (threadIdx.x == 0) coef[0] = (dloss ? dloss[0] : 1.0f) / (float)max(n, 1);
+  block_sums(v, valid, vp, np);
+  if (threadIdx.x == 0) {
+    rows[0] = before;
+    coef[0] = (dloss ? dloss[0] : 1.0f) / (float)max(valid, 1);
+  }
 }
 
-__global__ __launch_bounds__(256) void round_bf16_kernel(int64_t n8, const float* __restrict__ src,
-                                                         bf16_t* __restrict__ dst) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (int64_t)gridDim.x * 256) {
-    const f32x4 a = ((const f32x4*)src)[2 * i], b = ((const f32x4*)src)[2 * i + 1];
-    ((u32x4*)dst)[i] = u32x4{pack_bf2(a[0], a[1]), pack_bf2(a[2], a[3]), pack_bf2(b[0], b[1]), pack_bf2(b[2], b[3])};
+// One wave per row.  Bound by HBM bandwidth: h is read once and written once.
+__global__ __launch_bounds__(256) void head_gather_kernel(int64_t T, int H, const int32_t* __restrict__ slot,
+                                                          const bf16_t* __restrict__ h,
+                                                          const int32_t* __restrict__ targets,
+                                                          const float* __restrict__ lse, bf16_t* __restrict__ hc,
+                                                          int32_t* __restrict__ tc, float* __restrict__ lc) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= T) return;
+  const int at = slot[t];
+  if (at < 0) return;
+  const u32x4* src = (const u32x4*)(h + t * H);
+  u32x4* dst = (u32x4*)(hc + (int64_t)at * H);
+  for (int c = lane; c < H / 8; c += 64) dst[c] = src[c];
+  if (lane == 0) {
+    tc[at] = targets[t];
+    lc[at] = lse[t];
+  }
+}
+
+// One wave per row; the only rounding of dh.
+__global__ __launch_bounds__(256) void head_scatter_kernel(int64_t T, int H, const int32_t* __restrict__ slot,
+                                                           const float* __restrict__ coef,
+                                                           const float* __restrict__ dhc, bf16_t* __restrict__ dh) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= T) return;
+  const int at = slot[t];
+  u32x4* dst = (u32x4*)(dh + t * H);
+  if (at < 0) {
+    for (int c = lane; c < H / 8; c += 64) dst[c] = u32x4{0u, 0u, 0u, 0u};
+    return;
+  }
+  const float k = coef[0];
+  const f32x4* src = (const f32x4*)(dhc + (int64_t)at * H);
+  for (int c = lane; c < H / 8; c += 64) {
+    const f32x4 a = src[2 * c] * k, b = src[2 * c + 1] * k;
+    dst[c] = u32x4{pack_bf2(a[0], a[1]), pack_bf2(a[2], a[3]), pack_bf2(b[0], b[1]), pack_bf2(b[2], b[3])};
   }
 }
 
@@ -150,14 +209,22 @@ hipError_t head_rows(int64_t T, int V, int64_t blocks, const float* stats, const
   return hipGetLastError();
 }
 
-hipError_t head_coef(int64_t T, int V, const int32_t* targets, const float* dloss, float* coef, hipStream_t s) {
-  hipLaunchKernelGGL(head_coef_kernel, dim3(1), dim3(HL_THREADS), 0, s, T, V, targets, dloss, coef);
+hipError_t head_slots(int64_t T, int V, const int32_t* targets, const float* dloss, int32_t* slot, int* rows,
+                      float* coef, hipStream_t s) {
+  hipLaunchKernelGGL(head_slots_kernel, dim3(1), dim3(HL_THREADS), 0, s, T, V, targets, dloss, slot, rows, coef);
   return hipGetLastError();
 }
 
-hipError_t round_bf16(int64_t n, const float* src, bf16_t* dst, hipStream_t s) {
-  const int64_t n8 = n / 8, need = (n8 + 255) / 256;
-  hipLaunchKernelGGL(round_bf16_kernel, dim3((unsigned)(need < 4096 ? need : 4096)), dim3(256), 0, s, n8, src, dst);
+hipError_t head_gather(int64_t T, int H, const int32_t* slot, const bf16_t* h, const int32_t* targets, const float* lse,
+                       bf16_t* hc, int32_t* tc, float* lc, hipStream_t s) {
+  hipLaunchKernelGGL(head_gather_kernel, dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, T, H, slot, h, targets, lse,
+                     hc, tc, lc);
+  return hipGetLastError();
+}
+
+hipError_t head_scatter(int64_t T, int H, const int32_t* slot, const float* coef, const float* dhc, bf16_t* dh,
+                        hipStream_t s) {
+  hipLaunchKernelGGL(head_scatter_kernel, dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, T, H, slot, coef, dhc, dh);
   return hipGetLastError();
 }
 

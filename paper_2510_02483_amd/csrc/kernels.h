@@ -27,7 +27,10 @@ enum Epilogue {
   EPI_F32 = 5,      // F (fp32, rows split over up to three buffers) (+)= acc
   EPI_PART = 6,     // kpart[slice] = acc: a slice of a split K (256 x 256 tiles; set by gemm())
   EPI_LSE = 7,      // acc are logits: maximum and sum of exponentials per row and column block, target logits
-  EPI_DZ = 8,       // C (bf16) = the cross-entropy's gradient of the logits acc
+  EPI_DZ = 8,       // C (bf16) = softmax(acc) - onehot
+  EPI_DH = 9,       // F (fp32) (+)= acc
+  EPI_DE = 10,      // F (fp32) (+)= coef acc
+  EPI_DE16 = 11,    // C (bf16) = coef acc
 };
 
 struct GemmArgs {
@@ -50,7 +53,7 @@ struct GemmArgs {
   bf16_t* act = nullptr;          // EPI_GLU_FWD: [M][I]
   const bf16_t* gu_in = nullptr;  // EPI_GLU_BWD: saved [M][2I]
   int glu_I = 0;
-  float* F[3] = {nullptr, nullptr, nullptr};  // EPI_F32
+  float* F[3] = {nullptr, nullptr, nullptr};  // EPI_F32; EPI_DH, EPI_DE: F[0]
   int f_start[3] = {0, 1 << 30, 1 << 30};
   int64_t ldf = 0;
   int accumulate = 0;
@@ -60,7 +63,10 @@ struct GemmArgs {
   float* stats = nullptr;       // EPI_LSE: [column block][M] (max, sum of exp(z - max)); two blocks per tile column
   float* zt = nullptr;          // EPI_LSE: [M], the logit of a row's target where this product has it
   const float* lse = nullptr;   // EPI_DZ: [M]
-  const float* coef = nullptr;  // EPI_DZ: one factor of all gradients
+  const float* coef = nullptr;  // EPI_DE, EPI_DE16: one factor of the results (on the device)
+  // The token rows that count, on the device, at most as many as the host says: rows of C (M) of EPI_DZ and
+  // EPI_DH, the depth K of EPI_DE and EPI_DE16.
+  const int* rows = nullptr;
   // fp32 workspace for splitting K over workgroups when the output tiles alone
   // would leave compute units idle (slices * M * N floats, one slice fewer for
   // EPI_F32, see gemm_kpart_floats); null or smaller means fewer slices or none.
@@ -175,10 +181,16 @@ hipError_t ce_loss(int64_t T, const float* row_loss, const int* counts, float* l
 // outside [-1, V)), and loss = sum(row_loss) / max(rows with a target in [0, V), 1).
 hipError_t head_rows(int64_t T, int V, int64_t blocks, const float* stats, const float* zt, const int32_t* targets,
                      float* lse, float* row_loss, float* loss, hipStream_t s);
-// coef[0] = dloss[0] (null: 1) / max(rows with a target in [0, V), 1).
-hipError_t head_coef(int64_t T, int V, const int32_t* targets, const float* dloss, float* coef, hipStream_t s);
-// dst = src rounded to bf16, n a multiple of 8.
-hipError_t round_bf16(int64_t n, const float* src, bf16_t* dst, hipStream_t s);
+// The rows that have a target (any but -1), in their order: slot[t] = row t's place among them or -1, rows[0] = how
+// many, coef[0] = dloss[0] (null: 1) / max(rows with a target in [0, V), 1).
+hipError_t head_slots(int64_t T, int V, const int32_t* targets, const float* dloss, int32_t* slot, int* rows,
+                      float* coef, hipStream_t s);
+// h, targets and lse of those rows, gathered.
+hipError_t head_gather(int64_t T, int H, const int32_t* slot, const bf16_t* h, const int32_t* targets, const float* lse,
+                       bf16_t* hc, int32_t* tc, float* lc, hipStream_t s);
+// dh[t] = coef dhc[slot[t]] rounded to bf16, 0 for a row without a target.
+hipError_t head_scatter(int64_t T, int H, const int32_t* slot, const float* coef, const float* dhc, bf16_t* dh,
+                        hipStream_t s);
 
 // ---- optimizer ------------------------------------------------------------------
 struct AdamwHyper {

@@ -191,6 +191,34 @@ def test_a_row_of_nan_stays_in_its_row():
     assert torch.isnan(x.lse[33]) and torch.isnan(x.loss).all() and torch.isnan(x.dh[33]).all()
 
 
+@pytest.mark.parametrize("T,H,V", [(100, 64, 500), (700, 256, 9000)])
+def test_rows_without_a_target_may_hold_anything(T, H, V):
+    """Padding behind the last sequence: its h is NaN and reaches neither the loss nor a gradient."""
+    need_gpu()
+    x, y = Head(T, H, V, masked=0.6, seed=31), Head(T, H, V, masked=0.6, seed=31)
+    none = x.t == -1
+    assert bool(none.any()) and not bool(none.all())
+    x.h[none] = float("nan")
+    for a in (x, y):
+        a.fwd().bwd(a.de).bwd(a.low, dh=False)
+    assert torch.equal(x.loss, y.loss) and torch.equal(x.rows, y.rows)
+    assert torch.equal(x.dh, y.dh) and not x.dh[none].any()
+    assert torch.equal(x.de, y.de) and torch.equal(x.low, y.low)
+
+
+@pytest.mark.parametrize("last", [True, False])
+def test_a_single_target(last):
+    need_gpu()
+    x = Head(900, 256, 4000, masked=1.1, seed=33)
+    x.t[899 if last else 0] = 77
+    r = x.fwd().reference()
+    check_fwd(x, r)
+    x.bwd(x.de).bwd(x.low)
+    within("dh", x.dh, r["dh"], r["tol_dh"] + 1e-300)
+    within("d_embed", x.de, r["de"], r["tol_de"] + 1e-300)
+    within("d_embed bf16", x.low, r["de"], r["tol_de"] * (1 + U) + U * r["de"].abs() + 1e-300)
+
+
 def test_deterministic_and_no_stale_workspace():
     need_gpu()
     x = Head(333, 256, 4001, seed=21)
