@@ -191,17 +191,16 @@ struct FragAddr {
 // matrices, whose values of head h (log-sum-exp, D) start at vec0 of a vector
 // with one entry per token of a head.  Equal sequences (batch x seq) follow
 // from the workgroup's number, packed ones from the plan's list of tiles, which
-// is in order of falling work too; there S = 0 means that there is no tile (the
-// grid is as large as the list can be).
+// is in order of falling work too (packed.h); S = 0: no tile.
 struct QTile {
   int qt, h, S;
   int64_t row0, vec0;
 };
 template <bool PACKED>
-LS_DEV QTile q_tile(const AttnShape& sh, const PackedTile* tiles) {
+LS_DEV QTile q_tile(const AttnShape& sh, const PackedView& pk) {
   const int x = (int)blockIdx.x;
   if constexpr (PACKED) {
-    const PackedTile t = packed_tile(tiles, x / sh.nq, sh.seq);
+    const PackedTile t = packed_entry(pk.tiles, x / sh.nq, sh.seq);
     const int h = x % sh.nq;
     return QTile{t.rank, h, t.len, t.start, (int64_t)h * sh.seq + t.start};
   } else {
@@ -219,10 +218,87 @@ LS_DEV QTile q_tile(const AttnShape& sh, const PackedTile* tiles) {
 // log-sum-exp m + log2 l, does not depend on the reference point.
 constexpr float LAG = 8.0f;
 
+// A wave's own 32-row tile in LDS, from the rows that its lanes hold as MFMA
+// operands (lane: row lr, d = 16s + 8lh .. +7), for transposing reads.
+template <int D>
+LS_DEV void put_rows(bf16_t* t, const u32x4 (&f)[D / 16], int lr, int lh) {
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) *(u32x4*)(t + lr * D + 8 * ((2 * s + lh) ^ tile_swz<D>(lr))) = f[s];
+}
+template <int D>
+LS_DEV void get_rows(u32x4 (&f)[D / 16], const bf16_t* row, bool ok, int lh) {
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) f[s] = ok ? load16(row + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
+}
+// Orders a wave's own LDS writes before its later reads (the LDS serves a wave's accesses in order).
+LS_DEV void wave_lds_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Forward of one head of a packed sequence of up to 32 rows by one wave: every
+// operand straight from global memory, V through the wave's own LDS tile `vt` for
+// its transpose.  A workgroup's four waves work on four sequences, without
+// barriers, where a 128-row tile would leave three of them idle and wait
+// for one sequence's loads at a time: 301 sequences of 27 rows on average (179 at
+// most), 16 heads of 128: forward 50 -> 35 us, backward 176 -> 110 us.
+template <int D>
+LS_DEV void short_fwd(const AttnShape& sh, const PackedTile& t, int h, const bf16_t* __restrict__ qkv,
+                      bf16_t* __restrict__ o, float* __restrict__ lse, float sl2, bf16_t* vt) {
+  const int nq = sh.nq, nkv = sh.nkv, kvh = h / (nq / nkv);
+  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
+  const bool ok = lr < t.len;
+  const bf16_t* row = qkv + (t.start + (int64_t)(ok ? lr : 0)) * ld;
+  u32x4 qf[D / 16], kf[D / 16], vf[D / 16];
+  get_rows<D>(vf, row + (nq + nkv + kvh) * D, ok, lh);
+  get_rows<D>(qf, row + h * D, ok, lh);
+  get_rows<D>(kf, row + (nq + kvh) * D, ok, lh);
+  put_rows<D>(vt, vf, lr, lh);
+  f32x16 s{};
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) s = mfma32(kf[c], qf[c], s);
+  // lane holds query lr, keys 8(r/4) + 4lh + r%4
+  float mx = -INFINITY;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    if (8 * (r >> 2) + 4 * lh + (r & 3) > lr) s[r] = -INFINITY;
+    mx = fmaxf(mx, s[r]);
+  }
+  const float m = halves_max(mx) * sl2;
+  float sum = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    s[r] = ex2(fmaf(s[r], sl2, -m));
+    sum += s[r];
+  }
+  const float l = halves_sum(sum);
+  wave_lds_order();
+  f32x16 oacc[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) oacc[i] = f32x16{};
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const u32x4 pf = pack_frag(s, 8 * c);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) oacc[i] = mfma32(colt_frag<D>(vt, 32 * i, c, lane), pf, oacc[i]);
+  }
+  if (!ok) return;
+  const float inv = 1.0f / l;
+  bf16_t* orow = o + (t.start + (int64_t)lr) * nq * D + h * D;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int rq = 0; rq < 4; ++rq)
+      *(u32x2*)(orow + 32 * i + 8 * rq + 4 * lh) = u32x2{pack_bf2(oacc[i][4 * rq] * inv, oacc[i][4 * rq + 1] * inv),
+                                                         pack_bf2(oacc[i][4 * rq + 2] * inv, oacc[i][4 * rq + 3] * inv)};
+  if (lh == 0) lse[(int64_t)h * sh.seq + t.start + lr] = (m + log2f(l)) * LN2;
+}
+
 template <int D, bool PACKED>
-__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, const PackedTile* __restrict__ tiles,
-                                                           const bf16_t* __restrict__ qkv, bf16_t* __restrict__ o,
-                                                           float* __restrict__ lse, float sl2) {
+__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, PackedView pk, const bf16_t* __restrict__ qkv,
+                                                           bf16_t* __restrict__ o, float* __restrict__ lse,
+                                                           float sl2) {
   __shared__ __attribute__((aligned(1024))) bf16_t Ks[2][BKV * D];
   __shared__ __attribute__((aligned(1024))) bf16_t Vs[2][BKV * D];
   // the scale in a register before the loop: a scalar load still in flight
@@ -230,7 +306,17 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, const Pa
   asm volatile("" : "+s"(sl2));
 
   const int nq = sh.nq, nkv = sh.nkv;
-  const QTile qtile = q_tile<PACKED>(sh, tiles);
+  if constexpr (PACKED) {
+    static_assert(sizeof(Ks) >= 4 * PACKED_SHORT * D * sizeof(bf16_t), "a tile of V per wave");
+    const int unit = (int)blockIdx.x / nq, ntiles = packed_tiles(pk);
+    if (unit >= ntiles) {
+      const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+      const PackedTile t = packed_short(pk, unit, ntiles, w, sh.seq);
+      if (t.len > 0) short_fwd<D>(sh, t, (int)blockIdx.x % nq, qkv, o, lse, sl2, &Ks[0][0] + w * PACKED_SHORT * D);
+      return;
+    }
+  }
+  const QTile qtile = q_tile<PACKED>(sh, pk);
   if (PACKED && qtile.S == 0) return;
   const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv);
   const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
@@ -434,6 +520,118 @@ LS_DEV void unrotate_store(const f32x16 (&acc)[D / 32], float scale, const float
     }
 }
 
+// Backward of one kv head of a packed sequence of up to 32 rows by one wave: dQ of
+// its query heads hq0 .. hq0 + heads - 1, and dK and dV summed over them (fp32
+// partial sums into `part` row by row if given, for attn_bwd_dkdv_reduce).
+// Scores and dP are formed both ways round, with the lanes owning keys for dK and
+// dV and owning queries for dQ: two more small products instead of transposing
+// dS.  K, Q and dO go through the wave's own LDS tiles for their transposes.
+template <int D>
+constexpr int short_lds_bytes() {
+  return 3 * PACKED_SHORT * D * 2 + 2 * PACKED_SHORT * 4;
+}
+template <int D>
+LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, int hq0, int heads,
+                      const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
+                      const float* __restrict__ Dv, bf16_t* __restrict__ dqkv, float scale, float sl2, float* part,
+                      char* lds) {
+  constexpr int NSD = D / 16, NI = D / 32;
+  const int nq = sh.nq, nkv = sh.nkv;
+  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * D, ldo = (int64_t)nq * D;
+  const bool ok = lr < t.len;
+  const int64_t r0 = t.start + (int64_t)(ok ? lr : 0);
+  bf16_t *kt = (bf16_t*)lds, *qt = kt + PACKED_SHORT * D, *ot = qt + PACKED_SHORT * D;
+  float *lv = (float*)(ot + PACKED_SHORT * D), *dvv = lv + PACKED_SHORT;
+  u32x4 kf[NSD], vf[NSD], qf[NSD], of[NSD];
+  get_rows<D>(kf, qkv + r0 * ld + (nq + kvh) * D, ok, lh);
+  get_rows<D>(vf, qkv + r0 * ld + (nq + nkv + kvh) * D, ok, lh);
+  f32x16 dk[NI], dv[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) dk[i] = dv[i] = f32x16{};
+  for (int h = hq0; h < hq0 + heads; ++h) {
+    get_rows<D>(qf, qkv + r0 * ld + h * D, ok, lh);
+    get_rows<D>(of, dout + r0 * ldo + h * D, ok, lh);
+    const int64_t v0 = (int64_t)h * sh.seq + t.start;
+    const float L = ok ? lse2[v0 + lr] : 0.f, Dr = ok ? Dv[v0 + lr] : 0.f;
+    if (h == hq0) put_rows<D>(kt, kf, lr, lh);
+    put_rows<D>(qt, qf, lr, lh);
+    put_rows<D>(ot, of, lr, lh);
+    if (lh == 0) {
+      lv[lr] = L;
+      dvv[lr] = Dr;
+    }
+    wave_lds_order();
+    {  // lanes own keys: element r is query 8(r/4) + 4lh + r%4
+      f32x16 s{}, p{};
+#pragma unroll
+      for (int c = 0; c < NSD; ++c) {
+        s = mfma32(qf[c], kf[c], s);
+        p = mfma32(of[c], vf[c], p);
+      }
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        const f32x4 lq = *(const f32x4*)&lv[8 * rq + 4 * lh], dq4 = *(const f32x4*)&dvv[8 * rq + 4 * lh];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * rq + e;
+          if (8 * rq + 4 * lh + e < lr) s[r] = -INFINITY;
+          s[r] = ex2(fmaf(s[r], sl2, -lq[e]));
+          p[r] = s[r] * (p[r] - dq4[e]);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const u32x4 pf = pack_frag(s, 8 * c), sf = pack_frag(p, 8 * c);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          dv[i] = mfma32(colt_frag<D>(ot, 32 * i, c, lane), pf, dv[i]);
+          dk[i] = mfma32(colt_frag<D>(qt, 32 * i, c, lane), sf, dk[i]);
+        }
+      }
+    }
+    {  // lanes own queries: element r is key 8(r/4) + 4lh + r%4
+      f32x16 s{}, p{}, dq[NI];
+#pragma unroll
+      for (int c = 0; c < NSD; ++c) {
+        s = mfma32(kf[c], qf[c], s);
+        p = mfma32(vf[c], of[c], p);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float e = ex2(fmaf(s[r], sl2, -L));
+        if (8 * (r >> 2) + 4 * lh + (r & 3) > lr) e = 0.f;
+        p[r] = e * (p[r] - Dr);
+      }
+#pragma unroll
+      for (int i = 0; i < NI; ++i) dq[i] = f32x16{};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const u32x4 sf = pack_frag(p, 8 * c);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) dq[i] = mfma32(colt_frag<D>(kt, 32 * i, c, lane), sf, dq[i]);
+      }
+      if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * D);
+    }
+    wave_lds_order();
+  }
+  if (!ok) return;
+  if (part) {
+    float* row = part + (r0 * nkv + kvh) * (2 * D);
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        const int c = 32 * i + 8 * rq + 4 * lh;
+        *(f32x4*)(row + c) = f32x4{dk[i][4 * rq], dk[i][4 * rq + 1], dk[i][4 * rq + 2], dk[i][4 * rq + 3]};
+        *(f32x4*)(row + D + c) = f32x4{dv[i][4 * rq], dv[i][4 * rq + 1], dv[i][4 * rq + 2], dv[i][4 * rq + 3]};
+      }
+  } else {
+    unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * D);
+    unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * D);
+  }
+}
+
 // dK and dV for 128 keys of one kv head (4 waves x 32 keys), summed over the
 // query heads of the group, no atomics.  The 1-D grid runs the key tiles with
 // the most queries after them (lowest key index) first.  With few kv heads
@@ -453,7 +651,7 @@ LS_DEV void unrotate_store(const f32x16 (&acc)[D / 32], float scale, const float
 // and for the other waves (whose reads of tile t-1 are then done), and the
 // loads of tile t+2 go into tile t-1's stage.
 template <int D, bool SPLIT, bool PACKED>
-__global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, const PackedTile* __restrict__ tiles,
+__global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, PackedView pk,
                                                                 const bf16_t* __restrict__ qkv,
                                                                 const bf16_t* __restrict__ dout,
                                                                 const float* __restrict__ lse2,
@@ -486,7 +684,18 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, con
   int kvt = x / per, S = sh.seq;
   int64_t row0 = (int64_t)b * S, vec0 = (int64_t)b * nq * S;  // this sequence's first row; its entry of head 0's vectors
   if constexpr (PACKED) {
-    const PackedTile t = packed_tile(tiles, x / per, sh.seq);
+    static_assert(sizeof(stg) >= 4 * short_lds_bytes<D>(), "the tiles of a short sequence per wave");
+    const int unit = x / per, ntiles = packed_tiles(pk);
+    if (unit >= ntiles) {
+      const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+      const PackedTile t = packed_short(pk, unit, ntiles, w, sh.seq);
+      if (t.len > 0)
+        short_bwd<D>(sh, t, kvh, kvh * G + hs * Gs, Gs, qkv, dout, lse2, Dv, dqkv, scale, sl2,
+                     SPLIT ? part + (int64_t)hs * sh.seq * nkv * (2 * D) : nullptr,
+                     (char*)&stg[0] + w * short_lds_bytes<D>());
+      return;
+    }
+    const PackedTile t = packed_entry(pk.tiles, unit, sh.seq);
     if (t.len == 0) return;
     kvt = (t.len + BWD_BKV - 1) / BWD_BKV - 1 - t.rank;  // the most work: the first keys
     S = t.len;
@@ -725,7 +934,7 @@ __global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, const 
 // of registers within the tile; two workgroups per compute unit keep the
 // matrix cores busy across tile boundaries and while one wave waits.
 template <int D, bool PACKED>
-__global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, const PackedTile* __restrict__ tiles,
+__global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, PackedView pk,
                                                               const bf16_t* __restrict__ qkv,
                                                               const bf16_t* __restrict__ dout,
                                                               const float* __restrict__ lse2,
@@ -742,7 +951,8 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, const
   __shared__ __attribute__((aligned(1024))) bf16_t Vs[2][BKV * D];
 
   const int nq = sh.nq, nkv = sh.nkv;
-  const QTile qtile = q_tile<PACKED>(sh, tiles);
+  if (PACKED && (int)blockIdx.x / nq >= packed_tiles(pk)) return;  // (short sequences: with dK and dV)
+  const QTile qtile = q_tile<PACKED>(sh, pk);
   if (PACKED && qtile.S == 0) return;
   const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv);
   const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
@@ -857,33 +1067,30 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, const
   unrotate_store<D>(dq, scale, rope_cs, S, qrow, lh, dqkv + (qtile.row0 + qrow) * ld + h * D);
 }
 
-// What a launch of packed sequences takes from the plan (all null or 0 for equal ones).
-struct PackedView {
-  const PackedTile* tiles = nullptr;
-  const int32_t* pos = nullptr;
-  int64_t ntiles = 0;
-};
+// Units of work of a launch over packed sequences: every sequence takes its tiles, or
+// a quarter of a unit if it is short.
+int64_t packed_units(const PackedView& pk) { return (int64_t)pk.max_tiles + 1; }
 
 template <int D, bool PACKED>
 hipError_t attn_fwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, bf16_t* o, float* lse,
                       hipStream_t s) {
-  const unsigned grid = PACKED ? (unsigned)(pk.ntiles * sh.nq) : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
+  const unsigned grid = PACKED ? (unsigned)(packed_units(pk) * sh.nq) : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
   const float sl2 = LOG2E / sqrtf((float)(sh.d_scale > 0 ? sh.d_scale : D));
-  hipLaunchKernelGGL((attn_fwd_kernel<D, PACKED>), dim3(grid), dim3(256), 0, s, sh, pk.tiles, qkv, o, lse, sl2);
+  hipLaunchKernelGGL((attn_fwd_kernel<D, PACKED>), dim3(grid), dim3(256), 0, s, sh, pk, qkv, o, lse, sl2);
   return hipGetLastError();
 }
 
-// Key tiles of all sequences (packed ones: as many as there can be).
-int64_t key_tiles(const AttnShape& sh, int64_t ntiles) {
-  return ntiles > 0 ? ntiles : (int64_t)((sh.seq + BWD_BKV - 1) / BWD_BKV) * sh.batch;
+// Key tiles of all sequences (units: of packed ones, 0 for equal ones).
+int64_t key_tiles(const AttnShape& sh, int64_t units) {
+  return units > 0 ? units : (int64_t)((sh.seq + BWD_BKV - 1) / BWD_BKV) * sh.batch;
 }
 
 // Split of each kv head's query-head group over workgroups of the dK/dV
 // kernel: the smallest divisor of the group size that gives at least two
 // workgroups per compute unit (256 CUs), or the whole group.
-int dkdv_split(const AttnShape& sh, int64_t ntiles) {
+int dkdv_split(const AttnShape& sh, int64_t units) {
   const int G = sh.nq / sh.nkv;
-  const int64_t g1 = key_tiles(sh, ntiles) * sh.nkv;
+  const int64_t g1 = key_tiles(sh, units) * sh.nkv;
   for (int h = 1; h < G; ++h)
     if (G % h == 0 && g1 * h >= 512) return h;
   return G;
@@ -894,10 +1101,10 @@ int64_t bwd_ws_head(const AttnShape& sh) {
   return 2 * (int64_t)sh.batch * sh.seq * sh.nq * (int64_t)sizeof(float);
 }
 
-size_t bwd_workspace(const AttnShape& sh, int64_t ntiles) {
+size_t bwd_workspace(const AttnShape& sh, int64_t units) {
   // D and the base-2 log-sum-exp of every query, then (when the dK/dV group
   // is split) the fp32 partial dK | dV rows of every split
-  const int hsplit = dkdv_split(sh, ntiles);
+  const int hsplit = dkdv_split(sh, units);
   const int64_t part = hsplit > 1 ? (int64_t)hsplit * sh.batch * sh.seq * sh.nkv * 2 * sh.d * (int64_t)sizeof(float) : 0;
   return (size_t)(bwd_ws_head(sh) + part);
 }
@@ -913,14 +1120,15 @@ hipError_t attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* q
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const float scale = 1.0f / sqrtf((float)(sh.d_scale > 0 ? sh.d_scale : D));
-  const int hsplit = dkdv_split(sh, pk.ntiles);
+  const int64_t units = PACKED ? packed_units(pk) : 0;
+  const int hsplit = dkdv_split(sh, units);
   float* part = hsplit > 1 ? (float*)((char*)ws + bwd_ws_head(sh)) : nullptr;
-  const unsigned gkv = (unsigned)(key_tiles(sh, pk.ntiles) * sh.nkv * hsplit);
+  const unsigned gkv = (unsigned)(key_tiles(sh, units) * sh.nkv * hsplit);
   if (part)
-    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, true, PACKED>), dim3(gkv), dim3(256), 0, s, sh, pk.tiles, qkv, dout,
+    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, true, PACKED>), dim3(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
                        (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E, hsplit, part);
   else
-    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, PACKED>), dim3(gkv), dim3(256), 0, s, sh, pk.tiles, qkv, dout,
+    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, PACKED>), dim3(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
                        (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E, 1, nullptr);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -932,16 +1140,13 @@ hipError_t attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* q
     if (e != hipSuccess) return e;
   }
   const unsigned gq =
-      PACKED ? (unsigned)(pk.ntiles * sh.nq) : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
-  hipLaunchKernelGGL((attn_bwd_dq_kernel<D, PACKED>), dim3(gq), dim3(256), 0, s, sh, pk.tiles, qkv, dout,
+      PACKED ? (unsigned)(pk.max_tiles * sh.nq) : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
+  hipLaunchKernelGGL((attn_bwd_dq_kernel<D, PACKED>), dim3(gq), dim3(256), 0, s, sh, pk, qkv, dout,
                      (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E);
   return hipGetLastError();
 }
 
 AttnShape packed_shape(const PackedShape& p) { return AttnShape{1, (int)p.total, p.nq, p.nkv, p.d}; }
-PackedView packed_view(const PackedShape& p, const void* plan) {
-  return PackedView{packed_tiles(plan), packed_pos(p, plan), packed_max_tiles(p)};
-}
 
 }  // namespace
 
@@ -968,7 +1173,9 @@ hipError_t packed_attn_fwd(const PackedShape& p, const void* plan, const bf16_t*
   return hipErrorInvalidValue;
 }
 
-size_t packed_attn_bwd_workspace(const PackedShape& p) { return bwd_workspace(packed_shape(p), packed_max_tiles(p)); }
+size_t packed_attn_bwd_workspace(const PackedShape& p) {
+  return bwd_workspace(packed_shape(p), packed_units(packed_view(p, nullptr)));
+}
 
 hipError_t packed_attn_bwd(const PackedShape& p, const void* plan, const bf16_t* qkv, const bf16_t* o, const float* lse,
                            const bf16_t* dout, bf16_t* dqkv, void* ws, hipStream_t s) {

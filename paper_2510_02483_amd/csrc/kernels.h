@@ -134,12 +134,11 @@ hipError_t attn_bwd(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, con
 // ---- packed sequences -------------------------------------------------------------
 // `total` rows hold n_seqs sequences end to end; see packed.h for the plan.
 constexpr int PACKED_ROWS = 128;  // rows of a tile of the plan (query and key tiles of the attention kernels)
+constexpr int PACKED_SHORT = 32;  // sequences of up to so many rows are one wave's work each
 struct PackedShape {
   int64_t total;
   int n_seqs, nq, nkv, d;
 };
-int64_t packed_max_tiles(const PackedShape& p);
-size_t packed_tile_bytes(const PackedShape& p);  // bytes of the plan before the rows' positions
 size_t packed_plan_bytes(const PackedShape& p);
 hipError_t packed_plan(const PackedShape& p, const int32_t* cu, void* plan, hipStream_t s);
 // dst = q and k of src turned (v copied unless dst == src); rows of no sequence are left alone.

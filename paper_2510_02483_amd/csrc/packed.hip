@@ -36,9 +36,10 @@ LS_DEV int seq_len(const int32_t* cu, int s, int total, int& start) {
   return a >= 0 && b > a && b <= total ? b - a : 0;
 }
 
-// Workgroup 0 lists the tiles, the others find the rows' positions.
+// Workgroup 0 lists the tiles and the short sequences, the others find the rows'
+// positions.
 //
-// The list is a counting sort by rank (a tile's work), the highest first: ranks
+// The list of tiles is a counting sort by rank (a tile's work), the highest first: ranks
 // are counted with one range update per sequence in a difference array, whose
 // prefix sum is the number of tiles per class of 2^shift ranks (the classes
 // are single ranks up to 524288 rows).  Inside a class the order is that of
@@ -46,7 +47,9 @@ LS_DEV int seq_len(const int32_t* cu, int s, int total, int& start) {
 //
 // Bound by latency: one pass over cu_seqlens, two scans, one more pass.
 __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, int n, const int32_t* __restrict__ cu,
+                                                                   PackedHead* __restrict__ head,
                                                                    PackedTile* __restrict__ tiles, int max_tiles,
+                                                                   PackedTile* __restrict__ shorts, int max_shorts,
                                                                    int32_t* __restrict__ pos) {
   const int tid = threadIdx.x;
   if (blockIdx.x > 0) {
@@ -65,16 +68,18 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   }
   __shared__ int level[LEVELS + 1];
   __shared__ int part[PLAN_WAVES];
+  __shared__ int nshort;
   const int max_rank = (total - 1) / PACKED_ROWS;
   int shift = 0;
   while (max_rank >> shift >= LEVELS) ++shift;
   for (int i = tid; i <= LEVELS; i += PLAN_THREADS) level[i] = 0;
+  if (tid == 0) nshort = 0;
   __syncthreads();
   const int per = 1 << shift;
   for (int s = tid; s < n; s += PLAN_THREADS) {
     int start;
     const int len = seq_len(cu, s, total, start);
-    if (len == 0) continue;
+    if (len <= PACKED_SHORT) continue;
     // classes 0 .. top-1 get `per` ranks each, class `top` the rest
     const int m = (len - 1) / PACKED_ROWS + 1, top = (m - 1) >> shift, rest = m - (top << shift);
     atomicAdd(&level[0], per);
@@ -116,6 +121,15 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
     const int s = s0 + tid;
     int start = 0, len = 0;
     if (s < n) len = seq_len(cu, s, total, start);
+    const unsigned long long few = __ballot(len > 0 && len <= PACKED_SHORT);
+    if (few) {
+      const int lane = tid & 63;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&nshort, __popcll(few));
+      at = __shfl(at, 0) + __popcll(few & ((1ull << lane) - 1));
+      if ((few >> lane & 1) && at < max_shorts) shorts[at] = PackedTile{start, len, 0, 0};
+    }
+    if (len <= PACKED_SHORT) len = 0;
     const int m = len > 0 ? (len - 1) / PACKED_ROWS + 1 : 0;
     for (int r = 0; r < m && r < FEW; ++r) enter(start, len, r);
     unsigned long long longer = __ballot(m > FEW);
@@ -126,7 +140,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
       for (int r = FEW + (tid & 63); r < wm; r += 64) enter(wstart, wlen, r);
     }
   }
-  for (int i = (all > 0 ? all : 0) + tid; i < max_tiles; i += PLAN_THREADS) tiles[i] = PackedTile{0, 0, 0, 0};
+  __syncthreads();
+  if (tid == 0) *head = PackedHead{min(max(all, 0), max_tiles), min(nshort, max_shorts)};
 }
 
 // q and k of one row turned by its position: pairs (i, i + D/2) of every head,
@@ -189,20 +204,15 @@ __global__ __launch_bounds__(64 * ROPE_WAVES) void packed_rope_kernel(int total,
 
 }  // namespace
 
-int64_t packed_max_tiles(const PackedShape& p) {
-  // a sequence of n rows has at most (n + PACKED_ROWS - 1) / PACKED_ROWS tiles
-  const int64_t filled = p.n_seqs < p.total ? p.n_seqs : p.total;
-  return (p.total + (PACKED_ROWS - 1) * filled) / PACKED_ROWS;
-}
-size_t packed_tile_bytes(const PackedShape& p) {
-  return ((size_t)packed_max_tiles(p) * sizeof(PackedTile) + 255) & ~(size_t)255;
-}
-size_t packed_plan_bytes(const PackedShape& p) { return packed_tile_bytes(p) + (((size_t)p.total * 4 + 255) & ~(size_t)255); }
+size_t packed_plan_bytes(const PackedShape& p) { return packed_layout(p).total; }
 
 hipError_t packed_plan(const PackedShape& p, const int32_t* cu, void* plan, hipStream_t s) {
   const unsigned grid = 1 + (unsigned)((p.total + PLAN_THREADS - 1) / PLAN_THREADS);
+  const PackedLayout l = packed_layout(p);
+  char* b = (char*)plan;
   hipLaunchKernelGGL(packed_plan_kernel, dim3(grid), dim3(PLAN_THREADS), 0, s, (int)p.total, p.n_seqs, cu,
-                     (PackedTile*)plan, (int)packed_max_tiles(p), (int32_t*)packed_pos(p, plan));
+                     (PackedHead*)b, (PackedTile*)(b + l.tiles), (int)l.max_tiles, (PackedTile*)(b + l.shorts),
+                     (int)l.max_shorts, (int32_t*)(b + l.pos));
   return hipGetLastError();
 }
 
@@ -210,7 +220,7 @@ hipError_t packed_rope(const PackedShape& p, const void* plan, double theta, int
                        bf16_t* dst, hipStream_t s) {
   const int64_t need = (p.total + ROPE_WAVES - 1) / ROPE_WAVES;
   const dim3 grid((unsigned)(need < 8192 ? need : 8192)), block(64 * ROPE_WAVES);
-  const int32_t* pos = packed_pos(p, plan);
+  const int32_t* pos = packed_view(p, plan).pos;
   if (p.d == 128)
     hipLaunchKernelGGL((packed_rope_kernel<128>), grid, block, 0, s, (int)p.total, p.nq, p.nkv, log2(theta), inverse,
                        pos, src, dst);
