@@ -329,9 +329,8 @@ typedef struct {
 
 /* The plan of one batch (opaque, device): where every row lies in its sequence
  * and the tiles of all sequences in order of falling work.  Made once per batch
- * and read by the calls below, forward and backward, of every layer; it depends
- * on total, n_seqs and the contents of cu_seqlens only, and a call must be given
- * the plan of its own total and n_seqs.  ls_packed_plan_bytes: 0 for a *cfg that
+ * and read by the calls below, forward and backward, of every layer; a call
+ * must be given the plan of its own *cfg.  ls_packed_plan_bytes: 0 for a *cfg that
  * the calls refuse. */
 size_t ls_packed_plan_bytes(const ls_packed_cfg* cfg);
 int ls_packed_plan(const ls_packed_cfg* cfg, const int32_t* cu_seqlens, void* plan, size_t plan_bytes,
@@ -348,10 +347,11 @@ int ls_packed_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes
 
 /* Causal attention inside every sequence on q and k already rotated:
  * ls_attn_core_fwd / _bwd with the mask start of i's sequence <= j <= i.  What a
- * sequence gives does not depend on its neighbours, bit for bit, nor on where
- * in the row it lies (of dk and dv: for a given total and n_seqs, which decide over
- * how many workgroups a kv head's query heads are spread).  The backward takes o and lse of the forward call;
- * workspace: at least ls_packed_attn_bwd_workspace(cfg) bytes. */
+ * sequence gives does not depend on what its neighbours hold, bit for bit, nor on
+ * where in the row it lies; the lengths of all sequences decide over how many
+ * workgroups the sums of a long one's dk and dv are spread, and so the order in
+ * which they are added.  The backward takes o and lse of the forward call; workspace:
+ * at least ls_packed_attn_bwd_workspace(cfg) bytes. */
 int ls_packed_attn_fwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, const ls_bf16* qkv,
                        ls_bf16* o, float* lse, void* stream);
 size_t ls_packed_attn_bwd_workspace(const ls_packed_cfg* cfg);

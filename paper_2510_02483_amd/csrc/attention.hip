@@ -38,6 +38,8 @@
 // first, which balances the triangular work over the compute units.
 #include <math.h>
 
+#include <algorithm>
+
 #include "packed.h"
 
 namespace ls {
@@ -196,18 +198,13 @@ struct QTile {
   int qt, h, S;
   int64_t row0, vec0;
 };
-template <bool PACKED>
-LS_DEV QTile q_tile(const AttnShape& sh, const PackedView& pk) {
-  const int x = (int)blockIdx.x;
-  if constexpr (PACKED) {
-    const PackedTile t = packed_entry(pk.tiles, x / sh.nq, sh.seq);
-    const int h = x % sh.nq;
-    return QTile{t.rank, h, t.len, t.start, (int64_t)h * sh.seq + t.start};
-  } else {
-    const int nqt = (sh.seq + BQ - 1) / BQ, per = sh.nq * sh.batch;
-    const int h = (x % per) % sh.nq, b = (x % per) / sh.nq;
-    return QTile{nqt - 1 - x / per, h, sh.seq, (int64_t)b * sh.seq, ((int64_t)b * sh.nq + h) * sh.seq};
-  }
+LS_DEV QTile q_tile(const AttnShape& sh) {
+  const int nqt = (sh.seq + BQ - 1) / BQ, per = sh.nq * sh.batch;
+  const int x = (int)blockIdx.x, h = (x % per) % sh.nq, b = (x % per) / sh.nq;
+  return QTile{nqt - 1 - x / per, h, sh.seq, (int64_t)b * sh.seq, ((int64_t)b * sh.nq + h) * sh.seq};
+}
+LS_DEV QTile q_tile(const AttnShape& sh, const PackedTile& t, int h) {
+  return QTile{t.rank, h, t.len, t.start, (int64_t)h * sh.seq + t.start};
 }
 
 // Online softmax with a lagging reference maximum: the running reference m
@@ -306,18 +303,22 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, PackedVi
   asm volatile("" : "+s"(sl2));
 
   const int nq = sh.nq, nkv = sh.nkv;
+  QTile qtile;
   if constexpr (PACKED) {
     static_assert(sizeof(Ks) >= 4 * PACKED_SHORT * D * sizeof(bf16_t), "a tile of V per wave");
-    const int unit = (int)blockIdx.x / nq, ntiles = packed_tiles(pk);
-    if (unit >= ntiles) {
+    PackedTile t;
+    const int x = (int)blockIdx.x, head = x % nq;
+    const bool whole = packed_unit(pk, x / nq, sh.seq, t);
+    if (t.len == 0) return;
+    if (!whole) {
       const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-      const PackedTile t = packed_short(pk, unit, ntiles, w, sh.seq);
-      if (t.len > 0) short_fwd<D>(sh, t, (int)blockIdx.x % nq, qkv, o, lse, sl2, &Ks[0][0] + w * PACKED_SHORT * D);
+      short_fwd<D>(sh, t, head, qkv, o, lse, sl2, &Ks[0][0] + w * PACKED_SHORT * D);
       return;
     }
+    qtile = q_tile(sh, t, head);
+  } else {
+    qtile = q_tile(sh);
   }
-  const QTile qtile = q_tile<PACKED>(sh, pk);
-  if (PACKED && qtile.S == 0) return;
   const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv);
   const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
   const bf16_t* base = qkv + qtile.row0 * ld;
@@ -521,8 +522,7 @@ LS_DEV void unrotate_store(const f32x16 (&acc)[D / 32], float scale, const float
 }
 
 // Backward of one kv head of a packed sequence of up to 32 rows by one wave: dQ of
-// its query heads hq0 .. hq0 + heads - 1, and dK and dV summed over them (fp32
-// partial sums into `part` row by row if given, for attn_bwd_dkdv_reduce).
+// its query heads, and dK and dV summed over them.
 // Scores and dP are formed both ways round, with the lanes owning keys for dK and
 // dV and owning queries for dQ: two more small products instead of transposing
 // dS.  K, Q and dO go through the wave's own LDS tiles for their transposes.
@@ -531,12 +531,11 @@ constexpr int short_lds_bytes() {
   return 3 * PACKED_SHORT * D * 2 + 2 * PACKED_SHORT * 4;
 }
 template <int D>
-LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, int hq0, int heads,
-                      const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
-                      const float* __restrict__ Dv, bf16_t* __restrict__ dqkv, float scale, float sl2, float* part,
-                      char* lds) {
+LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf16_t* __restrict__ qkv,
+                      const bf16_t* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ Dv,
+                      bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds) {
   constexpr int NSD = D / 16, NI = D / 32;
-  const int nq = sh.nq, nkv = sh.nkv;
+  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv);
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * D, ldo = (int64_t)nq * D;
   const bool ok = lr < t.len;
@@ -549,7 +548,7 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, int hq0
   f32x16 dk[NI], dv[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) dk[i] = dv[i] = f32x16{};
-  for (int h = hq0; h < hq0 + heads; ++h) {
+  for (int h = hq0; h < hq0 + nq / nkv; ++h) {
     get_rows<D>(qf, qkv + r0 * ld + h * D, ok, lh);
     get_rows<D>(of, dout + r0 * ldo + h * D, ok, lh);
     const int64_t v0 = (int64_t)h * sh.seq + t.start;
@@ -616,20 +615,8 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, int hq0
     wave_lds_order();
   }
   if (!ok) return;
-  if (part) {
-    float* row = part + (r0 * nkv + kvh) * (2 * D);
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-      for (int rq = 0; rq < 4; ++rq) {
-        const int c = 32 * i + 8 * rq + 4 * lh;
-        *(f32x4*)(row + c) = f32x4{dk[i][4 * rq], dk[i][4 * rq + 1], dk[i][4 * rq + 2], dk[i][4 * rq + 3]};
-        *(f32x4*)(row + D + c) = f32x4{dv[i][4 * rq], dv[i][4 * rq + 1], dv[i][4 * rq + 2], dv[i][4 * rq + 3]};
-      }
-  } else {
-    unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * D);
-    unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * D);
-  }
+  unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * D);
+  unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * D);
 }
 
 // dK and dV for 128 keys of one kv head (4 waves x 32 keys), summed over the
@@ -650,6 +637,10 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, int hq0
 // slots before the end of tile t each wave waits for its loads of tile t+1
 // and for the other waves (whose reads of tile t-1 are then done), and the
 // loads of tile t+2 go into tile t-1's stage.
+//
+// Packed sequences: a workgroup takes a piece of the plan's work on tiles (a key tile and kv
+// head, or a part of its 64-query steps of all heads of the group, whose partial
+// sums go to a slot of `part`), or past those four short sequences and a kv head.
 template <int D, bool SPLIT, bool PACKED>
 __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, PackedView pk,
                                                                 const bf16_t* __restrict__ qkv,
@@ -683,20 +674,19 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, Pac
   const int hs = (x % per) % hsplit, kvh = ((x % per) / hsplit) % nkv, b = ((x % per) / hsplit) / nkv;
   int kvt = x / per, S = sh.seq;
   int64_t row0 = (int64_t)b * S, vec0 = (int64_t)b * nq * S;  // this sequence's first row; its entry of head 0's vectors
+  int parts = 1, part_no = 0, slot = 0;
   if constexpr (PACKED) {
     static_assert(sizeof(stg) >= 4 * short_lds_bytes<D>(), "the tiles of a short sequence per wave");
-    const int unit = x / per, ntiles = packed_tiles(pk);
-    if (unit >= ntiles) {
+    PackedTile t;
+    const bool whole = packed_piece(pk, kvt, sh.seq, t, part_no);
+    if (t.len == 0) return;
+    if (!whole) {
       const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-      const PackedTile t = packed_short(pk, unit, ntiles, w, sh.seq);
-      if (t.len > 0)
-        short_bwd<D>(sh, t, kvh, kvh * G + hs * Gs, Gs, qkv, dout, lse2, Dv, dqkv, scale, sl2,
-                     SPLIT ? part + (int64_t)hs * sh.seq * nkv * (2 * D) : nullptr,
-                     (char*)&stg[0] + w * short_lds_bytes<D>());
+      short_bwd<D>(sh, t, kvh, qkv, dout, lse2, Dv, dqkv, scale, sl2, (char*)&stg[0] + w * short_lds_bytes<D>());
       return;
     }
-    const PackedTile t = packed_entry(pk.tiles, unit, sh.seq);
-    if (t.len == 0) return;
+    parts = __builtin_amdgcn_readfirstlane((int)t.parts);
+    slot = __builtin_amdgcn_readfirstlane((int)t.slot);
     kvt = (t.len + BWD_BKV - 1) / BWD_BKV - 1 - t.rank;  // the most work: the first keys
     S = t.len;
     row0 = vec0 = t.start;
@@ -713,7 +703,14 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, Pac
   // tiles t = 0 .. Gs*nqt-1: query head kvh*G + hs*Gs + t/nqt, queries q_begin + (t%nqt)*BWD_BQ ..
   const int q_begin = kv0;  // earlier queries see none of these keys
   const int nqt = (S - q_begin + BWD_BQ - 1) / BWD_BQ;
-  const int ntiles = Gs * nqt;
+  int tbegin = 0, ntiles = Gs * nqt;  // (packed: this part's)
+  if constexpr (PACKED) {
+    if (parts > 1) {
+      tbegin = (int)((int64_t)ntiles * part_no / parts);
+      ntiles = (int)((int64_t)ntiles * (part_no + 1) / parts);
+      if (tbegin == ntiles) --tbegin;  // (no part is empty: a plan has at most a part per PACKED_STEPS tiles)
+    }
+  }
   const TileLoader<D, BWD_BQ> tlq(ld, wave, lane), tlo(ldo, wave, lane);
   auto issue = [&](int t, int st) {
     const int h = kvh * G + hs * Gs + t / nqt, q0 = q_begin + (t % nqt) * BWD_BQ;
@@ -723,8 +720,8 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, Pac
     if (wave == 0) load_vec64(rsrc(lse2 + v0, (uint32_t)S * 4), q0, S, stg[st].l, lane);
     if (wave == 1) load_vec64(rsrc(Dv + v0, (uint32_t)S * 4), q0, S, stg[st].d, lane);
   };
-  issue(0, 0);
-  if (ntiles > 1) issue(1, 1);
+  issue(tbegin, 0);
+  if (tbegin + 1 < ntiles) issue(tbegin + 1, 1);
 
   u32x4 kf[NSD], vf[NSD];
 #pragma unroll
@@ -832,7 +829,7 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, Pac
   asm volatile("" ::: "memory");
   static_for<RA>([&](auto j_c) { ring[decltype(j_c)::value] = operand(j_c, 0); });
   int st = 0, st1 = 1, st2 = 2;
-  for (int t = 0; t < ntiles; ++t) {
+  for (int t = tbegin; t < ntiles; ++t) {
     tile(t, st, st1, st2);
     const int tmp = st;
     st = st1;
@@ -842,8 +839,10 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, Pac
 
   // dK = scale * dS^T Q (un-rotated), dV = P^T dO.  Lane holds key kvrow.
   if (kvrow >= S) return;
-  if constexpr (SPLIT) {  // partial sums of this workgroup's heads; lane holds columns 32i + 8(r/4) + 4lh + r%4
-    float* row = part + (((int64_t)hs * sh.batch * sh.seq + row0 + kvrow) * nkv + kvh) * (2 * D);
+  if (SPLIT || (PACKED && parts > 1)) {  // this workgroup's partial sums; lane holds columns 32i + 8(r/4) + 4lh + r%4
+    float* row = part;
+    if constexpr (SPLIT) row += (((int64_t)hs * sh.batch * sh.seq + row0 + kvrow) * nkv + kvh) * (2 * D);
+    else row += (((int64_t)slot + part_no) * nkv + kvh) * (PACKED_ROWS * 2 * D) + (32 * wave + lr) * (2 * D);
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -858,15 +857,51 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, Pac
   }
 }
 
+// dK and dV of packed key tile `tile`, if its work was cut into parts, and kv head
+// kvh: the parts' sums added in their order, scaled and rounded.  A wave takes 8
+// rows at a time, their loads in flight together, a lane 2D / 64 columns of [dK | dV].
+template <int D>
+LS_DEV void join_parts(const AttnShape& sh, const PackedView& pk, int tile, int kvh, const float* __restrict__ part,
+                       bf16_t* __restrict__ dqkv, float scale) {
+  constexpr int E = 2 * D / 64, ROWS = 8;
+  const int nkv = sh.nkv;
+  const PackedHead head = *pk.head;
+  const PackedTile t = packed_checked(pk.tiles[tile], sh.seq);  // (one of max_tiles)
+  if (tile >= min(packed_count(head.tiles, pk.max_tiles), packed_count(head.split, pk.max_tiles))) return;
+  const int parts = __builtin_amdgcn_readfirstlane((int)t.parts), slot = __builtin_amdgcn_readfirstlane((int)t.slot);
+  if (t.len == 0 || slot + parts > pk.max_slots) return;
+  const int kv0 = ((t.len - 1) / BWD_BKV - t.rank) * BWD_BKV;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = E * lane;
+  typedef float fE __attribute__((ext_vector_type(E)));
+  const int64_t ld = (int64_t)(sh.nq + 2 * nkv) * D, step = (int64_t)nkv * (PACKED_ROWS * 2 * D);
+  const bool is_k = c0 < D;
+  const float c = is_k ? scale : 1.0f;
+  const float* src = part + ((int64_t)slot * nkv + kvh) * (PACKED_ROWS * 2 * D) + c0;
+  bf16_t* dst = dqkv + (t.start + (int64_t)kv0) * ld + (int64_t)(sh.nq + (is_k ? 0 : nkv) + kvh) * D + (is_k ? c0 : c0 - D);
+  for (int r0 = ROWS * wave; r0 < BWD_BKV && kv0 + r0 < t.len; r0 += 4 * ROWS) {
+    fE v[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) v[k] = fE{};
+    // (rows past the end of the sequence are in the slot, unwritten, and go nowhere)
+    for (int p = 0; p < parts; ++p)
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k) v[k] += *(const fE*)(src + p * step + (r0 + k) * (2 * D));
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      if (kv0 + r0 + k >= t.len) break;
+      bf16_t* y = dst + (r0 + k) * ld;
+      if constexpr (E == 4) *(u32x2*)y = u32x2{pack_bf2(v[k][0] * c, v[k][1] * c), pack_bf2(v[k][2] * c, v[k][3] * c)};
+      else *(uint32_t*)y = pack_bf2(v[k][0] * c, v[k][1] * c);
+    }
+  }
+}
+
 // Sum of the hsplit partial dK / dV rows of attn_bwd_dkdv_kernel, in split
 // order, then scale and inverse RoPE for dK, bf16 stores into dqkv.  One wave
 // per (token, kv head): lane l holds columns 4l .. 4l+3 of [dK | dV] (D = 128)
 // or 2l .. 2l+1 (D = 64); the RoPE partner of dK column c < D/2 is c + D/2.
-// rows_pos: null, or of packed sequences each row's position, negative where the
-// row belongs to none (and has no partial sums).
 template <int D>
-__global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, const int32_t* __restrict__ rows_pos,
-                                                            int hsplit, const float* __restrict__ part,
+__global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, int hsplit, const float* __restrict__ part,
                                                             bf16_t* __restrict__ dqkv, const float* __restrict__ rope_cs,
                                                             float scale) {
   constexpr int E = 2 * D / 64;  // columns per lane
@@ -876,7 +911,6 @@ __global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, const 
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (token, kv head)
   if (w >= T * sh.nkv) return;
   const int64_t t = w / sh.nkv;
-  if (rows_pos && rows_pos[t] < 0) return;
   const int kvh = (int)(w % sh.nkv), pos = (int)(t % sh.seq);
   const int c0 = E * lane;  // first of this lane's columns in [dK | dV]
   float v[E];
@@ -940,7 +974,7 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, Packe
                                                               const float* __restrict__ lse2,
                                                               const float* __restrict__ Dv, bf16_t* __restrict__ dqkv,
                                                               const float* __restrict__ rope_cs, float scale,
-                                                              float sl2) {
+                                                              float sl2, const float* __restrict__ part) {
   constexpr int NSD = D / 16, NI = D / 32;
   constexpr int PS = 2 * NSD;                // slots of one block's S^T and dP^T (interleaved)
   constexpr int PQ = 2 * NI;                 // slots of one block's dQ^T
@@ -951,9 +985,20 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, Packe
   __shared__ __attribute__((aligned(1024))) bf16_t Vs[2][BKV * D];
 
   const int nq = sh.nq, nkv = sh.nkv;
-  if (PACKED && (int)blockIdx.x / nq >= packed_tiles(pk)) return;  // (short sequences: with dK and dV)
-  const QTile qtile = q_tile<PACKED>(sh, pk);
-  if (PACKED && qtile.S == 0) return;
+  QTile qtile;
+  if constexpr (PACKED) {
+    // the first workgroups finish dK and dV; short sequences have their dQ already
+    const int joins = packed_max_split(pk) * nkv, x = (int)blockIdx.x;
+    if (x < joins) {
+      join_parts<D>(sh, pk, x / nkv, x % nkv, part, dqkv, scale);
+      return;
+    }
+    PackedTile t;
+    if (!packed_unit(pk, (x - joins) / nq, sh.seq, t) || t.len == 0) return;
+    qtile = q_tile(sh, t, (x - joins) % nq);
+  } else {
+    qtile = q_tile(sh);
+  }
   const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv);
   const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
   const int64_t ldo = (int64_t)nq * D;
@@ -1067,30 +1112,22 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, Packe
   unrotate_store<D>(dq, scale, rope_cs, S, qrow, lh, dqkv + (qtile.row0 + qrow) * ld + h * D);
 }
 
-// Units of work of a launch over packed sequences: every sequence takes its tiles, or
-// a quarter of a unit if it is short.
-int64_t packed_units(const PackedView& pk) { return (int64_t)pk.max_tiles + 1; }
-
 template <int D, bool PACKED>
 hipError_t attn_fwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, bf16_t* o, float* lse,
                       hipStream_t s) {
-  const unsigned grid = PACKED ? (unsigned)(packed_units(pk) * sh.nq) : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
+  const unsigned grid = PACKED ? (unsigned)(pk.max_tiles + 1) * sh.nq
+                               : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
   const float sl2 = LOG2E / sqrtf((float)(sh.d_scale > 0 ? sh.d_scale : D));
   hipLaunchKernelGGL((attn_fwd_kernel<D, PACKED>), dim3(grid), dim3(256), 0, s, sh, pk, qkv, o, lse, sl2);
   return hipGetLastError();
 }
 
-// Key tiles of all sequences (units: of packed ones, 0 for equal ones).
-int64_t key_tiles(const AttnShape& sh, int64_t units) {
-  return units > 0 ? units : (int64_t)((sh.seq + BWD_BKV - 1) / BWD_BKV) * sh.batch;
-}
-
 // Split of each kv head's query-head group over workgroups of the dK/dV
 // kernel: the smallest divisor of the group size that gives at least two
 // workgroups per compute unit (256 CUs), or the whole group.
-int dkdv_split(const AttnShape& sh, int64_t units) {
+int dkdv_split(const AttnShape& sh) {
   const int G = sh.nq / sh.nkv;
-  const int64_t g1 = key_tiles(sh, units) * sh.nkv;
+  const int64_t g1 = (int64_t)((sh.seq + BWD_BKV - 1) / BWD_BKV) * sh.nkv * sh.batch;
   for (int h = 1; h < G; ++h)
     if (G % h == 0 && g1 * h >= 512) return h;
   return G;
@@ -1101,17 +1138,9 @@ int64_t bwd_ws_head(const AttnShape& sh) {
   return 2 * (int64_t)sh.batch * sh.seq * sh.nq * (int64_t)sizeof(float);
 }
 
-size_t bwd_workspace(const AttnShape& sh, int64_t units) {
-  // D and the base-2 log-sum-exp of every query, then (when the dK/dV group
-  // is split) the fp32 partial dK | dV rows of every split
-  const int hsplit = dkdv_split(sh, units);
-  const int64_t part = hsplit > 1 ? (int64_t)hsplit * sh.batch * sh.seq * sh.nkv * 2 * sh.d * (int64_t)sizeof(float) : 0;
-  return (size_t)(bwd_ws_head(sh) + part);
-}
-
-template <int D, bool PACKED>
-hipError_t attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, const bf16_t* o, const float* lse,
-                      const bf16_t* dout, bf16_t* dqkv, const float* rope_cs, void* ws, hipStream_t s) {
+template <int D>
+hipError_t attn_bwd_t(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, const float* lse, const bf16_t* dout,
+                      bf16_t* dqkv, const float* rope_cs, void* ws, hipStream_t s) {
   const int64_t T = (int64_t)sh.batch * sh.seq;
   float* Dv = (float*)ws;
   float* lse2 = Dv + T * sh.nq;
@@ -1120,29 +1149,51 @@ hipError_t attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* q
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const float scale = 1.0f / sqrtf((float)(sh.d_scale > 0 ? sh.d_scale : D));
-  const int64_t units = PACKED ? packed_units(pk) : 0;
-  const int hsplit = dkdv_split(sh, units);
+  const int hsplit = dkdv_split(sh);
   float* part = hsplit > 1 ? (float*)((char*)ws + bwd_ws_head(sh)) : nullptr;
-  const unsigned gkv = (unsigned)(key_tiles(sh, units) * sh.nkv * hsplit);
+  const unsigned gkv = (unsigned)((sh.seq + BWD_BKV - 1) / BWD_BKV) * sh.nkv * sh.batch * hsplit;
+  const PackedView none;
   if (part)
-    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, true, PACKED>), dim3(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
+    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, true, false>), dim3(gkv), dim3(256), 0, s, sh, none, qkv, dout,
                        (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E, hsplit, part);
   else
-    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, PACKED>), dim3(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
+    hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, false>), dim3(gkv), dim3(256), 0, s, sh, none, qkv, dout,
                        (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E, 1, nullptr);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (part) {
     const int64_t rows = T * sh.nkv;  // one wave each, four per workgroup
-    hipLaunchKernelGGL((attn_bwd_dkdv_reduce<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, sh, pk.pos, hsplit,
+    hipLaunchKernelGGL((attn_bwd_dkdv_reduce<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, sh, hsplit,
                        (const float*)part, dqkv, rope_cs, scale);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const unsigned gq =
-      PACKED ? (unsigned)(pk.max_tiles * sh.nq) : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
-  hipLaunchKernelGGL((attn_bwd_dq_kernel<D, PACKED>), dim3(gq), dim3(256), 0, s, sh, pk, qkv, dout,
-                     (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E);
+  const unsigned gq = (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
+  hipLaunchKernelGGL((attn_bwd_dq_kernel<D, false>), dim3(gq), dim3(256), 0, s, sh, none, qkv, dout,
+                     (const float*)lse2, (const float*)Dv, dqkv, rope_cs, scale, scale * LOG2E, (const float*)nullptr);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, const bf16_t* o,
+                             const float* lse, const bf16_t* dout, bf16_t* dqkv, void* ws, hipStream_t s) {
+  const int64_t T = sh.seq;
+  float* Dv = (float*)ws;
+  float* lse2 = Dv + T * sh.nq;
+  float* part = (float*)((char*)ws + bwd_ws_head(sh));
+  hipLaunchKernelGGL((attn_bwd_pre_kernel<D>), dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, sh, o, dout, lse, Dv,
+                     lse2);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const float scale = 1.0f / sqrtf((float)D);
+  const unsigned gkv = (unsigned)(pk.max_items + 1) * sh.nkv;
+  hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, true>), dim3(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
+                     (const float*)lse2, (const float*)Dv, dqkv, (const float*)nullptr, scale, scale * LOG2E, 1, part);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const unsigned gq = (unsigned)packed_max_split(pk) * sh.nkv + (unsigned)pk.max_tiles * sh.nq;
+  hipLaunchKernelGGL((attn_bwd_dq_kernel<D, true>), dim3(gq), dim3(256), 0, s, sh, pk, qkv, dout, (const float*)lse2,
+                     (const float*)Dv, dqkv, (const float*)nullptr, scale, scale * LOG2E, (const float*)part);
   return hipGetLastError();
 }
 
@@ -1156,12 +1207,18 @@ hipError_t attn_fwd(const AttnShape& sh, const bf16_t* qkv, bf16_t* o, float* ls
   return hipErrorInvalidValue;
 }
 
-size_t attn_bwd_workspace(const AttnShape& sh) { return bwd_workspace(sh, 0); }
+size_t attn_bwd_workspace(const AttnShape& sh) {
+  // D and the base-2 log-sum-exp of every query, then (when the dK/dV group
+  // is split) the fp32 partial dK | dV rows of every split
+  const int hsplit = dkdv_split(sh);
+  const int64_t part = hsplit > 1 ? (int64_t)hsplit * sh.batch * sh.seq * sh.nkv * 2 * sh.d * (int64_t)sizeof(float) : 0;
+  return (size_t)(bwd_ws_head(sh) + part);
+}
 
 hipError_t attn_bwd(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, const float* lse, const bf16_t* dout,
                     bf16_t* dqkv, const float* rope_cs, void* ws, hipStream_t s) {
-  if (sh.d == 128) return attn_bwd_t<128, false>(sh, {}, qkv, o, lse, dout, dqkv, rope_cs, ws, s);
-  if (sh.d == 64) return attn_bwd_t<64, false>(sh, {}, qkv, o, lse, dout, dqkv, rope_cs, ws, s);
+  if (sh.d == 128) return attn_bwd_t<128>(sh, qkv, o, lse, dout, dqkv, rope_cs, ws, s);
+  if (sh.d == 64) return attn_bwd_t<64>(sh, qkv, o, lse, dout, dqkv, rope_cs, ws, s);
   return hipErrorInvalidValue;
 }
 
@@ -1174,14 +1231,15 @@ hipError_t packed_attn_fwd(const PackedShape& p, const void* plan, const bf16_t*
 }
 
 size_t packed_attn_bwd_workspace(const PackedShape& p) {
-  return bwd_workspace(packed_shape(p), packed_units(packed_view(p, nullptr)));
+  // D and the base-2 log-sum-exp of every row and head, then the slots of partial dK | dV
+  return (size_t)(bwd_ws_head(packed_shape(p)) + packed_layout(p).max_slots * p.nkv * PACKED_ROWS * 2 * p.d * 4);
 }
 
 hipError_t packed_attn_bwd(const PackedShape& p, const void* plan, const bf16_t* qkv, const bf16_t* o, const float* lse,
                            const bf16_t* dout, bf16_t* dqkv, void* ws, hipStream_t s) {
   const AttnShape sh = packed_shape(p);
-  if (p.d == 128) return attn_bwd_t<128, true>(sh, packed_view(p, plan), qkv, o, lse, dout, dqkv, nullptr, ws, s);
-  if (p.d == 64) return attn_bwd_t<64, true>(sh, packed_view(p, plan), qkv, o, lse, dout, dqkv, nullptr, ws, s);
+  if (p.d == 128) return packed_attn_bwd_t<128>(sh, packed_view(p, plan), qkv, o, lse, dout, dqkv, ws, s);
+  if (p.d == 64) return packed_attn_bwd_t<64>(sh, packed_view(p, plan), qkv, o, lse, dout, dqkv, ws, s);
   return hipErrorInvalidValue;
 }
 

@@ -3,9 +3,11 @@
 //   PackedTile of every PACKED_ROWS rows of every sequence that is not short, in
 //     order of falling work, packed_max_tiles() of them at most;
 //   PackedTile (rank 0) of every short sequence, of up to PACKED_SHORT rows;
+//   PackedItem of every piece of work of the dK/dV kernel on tiles: a key tile, or
+//     a part of the queries of one with many, in the tiles' order;
 //   one int32 per row: its position in its sequence, or -1.
 // The lengths are known on the device only, so the attention's launches cover as
-// many units of work as there can be: unit u is tile u, or, past the tiles, four short
+// much work as there can be: unit u is tile u, or, past the tiles, four short
 // sequences, one per wave.
 #pragma once
 #include "common.h"
@@ -14,22 +16,36 @@
 namespace ls {
 
 struct PackedHead {
-  int32_t tiles, shorts;
+  int32_t tiles, shorts, items, split;  // split: the first tiles, whose work is cut into parts
 };
 
 // Tile `rank` (0-based, rows PACKED_ROWS * rank .. of the sequence) of the sequence of
 // `len` rows from row `start` on.  A query tile of rank r sees r + 1 tiles of
 // keys; the key tile with r tiles of queries after it does the same work, so one
 // list serves both: it is key tile (tiles of the sequence) - 1 - r.
+// parts, slot: how many workgroups share the tile's dK/dV per kv head, and, when
+// there are several, where their partial sums lie (slots slot .. slot + parts - 1).
 struct PackedTile {
-  int32_t start, len, rank, pad;
+  int32_t start, len, rank;
+  uint32_t parts : 10, slot : 22;
+};
+// A piece of dK/dV work: part `part` of a tile.
+struct PackedItem {
+  PackedTile tile;
+  int32_t part, pad[3];
 };
 
 // Where the parts of a plan lie.
 struct PackedLayout {
-  int64_t max_tiles, max_shorts;
-  size_t tiles, shorts, pos, total;
+  int64_t max_tiles, max_shorts, max_items, max_slots;
+  size_t tiles, shorts, items, pos, total;
 };
+// A key tile of rank r is r + 1 units of dK/dV work per kv head (128 queries of every
+// head of the group each).  A tile with more than half of a compute unit's share
+// of all work is cut into parts of at most that, of two heads' units or more.
+// So there are at most 2 PACKED_CUS / nkv parts more than tiles, and as many tiles
+// that are cut.
+constexpr int PACKED_CUS = 256, PACKED_PART = 2;
 inline PackedLayout packed_layout(const PackedShape& p) {
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   PackedLayout l;
@@ -38,7 +54,10 @@ inline PackedLayout packed_layout(const PackedShape& p) {
   l.max_tiles = (p.total + (PACKED_ROWS - 1) * l.max_shorts) / PACKED_ROWS;
   l.tiles = 256;
   l.shorts = l.tiles + up((size_t)l.max_tiles * sizeof(PackedTile));
-  l.pos = l.shorts + up((size_t)l.max_shorts * sizeof(PackedTile));
+  l.max_items = l.max_tiles + 2 * PACKED_CUS / p.nkv;
+  l.max_slots = 2 * (2 * PACKED_CUS / p.nkv);
+  l.items = l.shorts + up((size_t)l.max_shorts * sizeof(PackedTile));
+  l.pos = l.items + up((size_t)l.max_items * sizeof(PackedItem));
   l.total = l.pos + up((size_t)p.total * 4);
   return l;
 }
@@ -48,38 +67,70 @@ struct PackedView {
   const PackedHead* head = nullptr;
   const PackedTile* tiles = nullptr;
   const PackedTile* shorts = nullptr;
-  const int32_t* pos = nullptr;
-  int max_tiles = 0, max_shorts = 0;
+  const PackedItem* items = nullptr;
+  int max_tiles = 0, max_shorts = 0, max_items = 0, max_slots = 0;
 };
 inline PackedView packed_view(const PackedShape& p, const void* plan) {
   const PackedLayout l = packed_layout(p);
   const char* b = (const char*)plan;
   return PackedView{(const PackedHead*)b, (const PackedTile*)(b + l.tiles), (const PackedTile*)(b + l.shorts),
-                    (const int32_t*)(b + l.pos), (int)l.max_tiles, (int)l.max_shorts};
+                    (const PackedItem*)(b + l.items), (int)l.max_tiles, (int)l.max_shorts, (int)l.max_items,
+                    (int)l.max_slots};
+}
+// Tiles whose dK/dV work may be cut into parts (two slots each at least).
+__host__ __device__ inline int packed_max_split(const PackedView& v) {
+  return v.max_tiles < v.max_slots / 2 ? v.max_tiles : v.max_slots / 2;
+}
+inline const int32_t* packed_pos(const PackedShape& p, const void* plan) {
+  return (const int32_t*)((const char*)plan + packed_layout(p).pos);
 }
 
 // Whatever a plan holds (lengths that were not in order, memory that was never
 // filled), the counts and entries returned lie inside the plan and the `total`
 // rows, so that nothing outside a buffer is touched.  All uniform over a wave.
-LS_DEV int packed_tiles(const PackedView& v) {
-  return max(0, min(v.max_tiles, __builtin_amdgcn_readfirstlane(v.head->tiles)));
-}
-LS_DEV PackedTile packed_entry(const PackedTile* list, int i, int total) {
-  PackedTile t = list[i];
+LS_DEV int packed_count(int n, int most) { return max(0, min(most, __builtin_amdgcn_readfirstlane(n))); }
+LS_DEV PackedTile packed_checked(PackedTile t, int total) {
   t.start = __builtin_amdgcn_readfirstlane(t.start);
   t.len = __builtin_amdgcn_readfirstlane(t.len);
   t.rank = __builtin_amdgcn_readfirstlane(t.rank);
   if (t.start < 0 || t.start >= total || t.len <= 0 || t.len > total - t.start || t.rank < 0 ||
       t.rank > (t.len - 1) / PACKED_ROWS)
-    t = PackedTile{0, 0, 0, 0};
+    t = PackedTile{};
   return t;
 }
-// Short sequence of `wave` (0..3) of unit u >= tiles; len 0 where there is none.
-LS_DEV PackedTile packed_short(const PackedView& v, int unit, int tiles, int wave, int total) {
-  const int i = __builtin_amdgcn_readfirstlane(4 * (unit - tiles) + wave);
-  if (i >= min(v.max_shorts, __builtin_amdgcn_readfirstlane(v.head->shorts))) return PackedTile{0, 0, 0, 0};
-  const PackedTile t = packed_entry(v.shorts, i, total);
-  return t.len > PACKED_SHORT ? PackedTile{0, 0, 0, 0} : t;
+// Unit u of a launch over tiles and short sequences: tile u (true), or this wave's
+// sequence of the four that unit u holds (false); len 0 where there is none.
+// Counts and both entries are loaded at once, not one after the other.
+LS_DEV bool packed_unit(const PackedView& v, int u, int total, PackedTile& t) {
+  const PackedHead h = *v.head;
+  const PackedTile a = v.tiles[min(u, v.max_tiles - 1)];
+  const int tiles = packed_count(h.tiles, v.max_tiles);
+  if (u < tiles) {
+    t = packed_checked(a, total);
+    return true;
+  }
+  const int i = __builtin_amdgcn_readfirstlane(4 * (u - tiles) + ((int)threadIdx.x >> 6));
+  t = PackedTile{};
+  if (i < packed_count(h.shorts, v.max_shorts)) t = packed_checked(v.shorts[i], total);
+  if (t.len > PACKED_SHORT) t = PackedTile{};
+  return false;
+}
+// The same for dK/dV: piece u of the tiles' work, or a short sequence.
+LS_DEV bool packed_piece(const PackedView& v, int u, int total, PackedTile& t, int& part) {
+  const PackedHead h = *v.head;
+  const PackedItem a = v.items[min(u, v.max_items - 1)];
+  const int items = packed_count(h.items, v.max_items);
+  if (u < items) {
+    t = packed_checked(a.tile, total);
+    part = __builtin_amdgcn_readfirstlane(a.part);
+    if (part < 0 || part >= (int)t.parts || (t.parts > 1 && (int)(t.slot + t.parts) > v.max_slots)) t = PackedTile{};
+    return true;
+  }
+  const int i = __builtin_amdgcn_readfirstlane(4 * (u - items) + ((int)threadIdx.x >> 6));
+  t = PackedTile{};
+  if (i < packed_count(h.shorts, v.max_shorts)) t = packed_checked(v.shorts[i], total);
+  if (t.len > PACKED_SHORT) t = PackedTile{};
+  return false;
 }
 
 }  // namespace ls

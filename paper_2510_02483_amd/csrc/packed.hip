@@ -8,25 +8,40 @@ namespace ls {
 
 namespace {
 
-constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_THREADS = 512;
 constexpr int PLAN_WAVES = PLAN_THREADS / 64;
 constexpr int LEVELS = 4 * PLAN_THREADS;  // classes of work that the list of tiles is ordered by
 constexpr int FEW = 4;                    // tiles of a sequence that one thread enters by itself
 
-// Inclusive prefix sum over the workgroup's threads.
-LS_DEV int block_scan(int v, int* part) {
+// Inclusive prefix sums of N values over the workgroup's threads, and their totals.
+// (`part` may be used again after a barrier.)
+template <int N>
+LS_DEV void block_scan(int (&v)[N], int (&all)[N], int (*part)[PLAN_WAVES]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o);
-    if (lane >= o) v += u;
+  for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int u = __shfl_up(v[k], o);
+      if (lane >= o) v[k] += u;
+    }
+  if (lane == 63) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) part[k][wave] = v[k];
   }
-  if (lane == 63) part[wave] = v;
   __syncthreads();
-  int before = 0;
-  for (int w = 0; w < wave; ++w) before += part[w];
-  __syncthreads();
-  return v + before;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    all[k] = 0;
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < PLAN_WAVES; ++w) {
+      const int p = part[k][w];
+      before += w < wave ? p : 0;
+      all[k] += p;
+    }
+    v[k] += before;
+  }
 }
 
 // Rows of sequence s, 0 for an empty one or one that does not lie inside the total.
@@ -36,21 +51,33 @@ LS_DEV int seq_len(const int32_t* cu, int s, int total, int& start) {
   return a >= 0 && b > a && b <= total ? b - a : 0;
 }
 
-// Workgroup 0 lists the tiles and the short sequences, the others find the rows'
-// positions.
+// Sum over the workgroup (every thread gets it).
+LS_DEV long long block_sum(long long v, long long* part) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  long long s = 0;
+#pragma unroll
+  for (int w = 0; w < PLAN_WAVES; ++w) s += part[w];
+  return s;
+}
+
+// Workgroup 0 lists the tiles, the short sequences and the pieces of dK/dV work, the
+// others find the rows' positions.
 //
-// The list of tiles is a counting sort by rank (a tile's work), the highest first: ranks
-// are counted with one range update per sequence in a difference array, whose
-// prefix sum is the number of tiles per class of 2^shift ranks (the classes
-// are single ranks up to 524288 rows).  Inside a class the order is that of
-// the LDS atomics; it decides when a tile is computed, never what.
+// The list of tiles is a counting sort by rank (a tile's work), the highest first:
+// ranks are counted with one range update per sequence in a difference array,
+// whose prefix sum is the number of tiles per class of 2^shift ranks (the
+// classes are single ranks up to 262144 rows).  Inside a class the order is that
+// of the LDS atomics; it decides when a tile is computed, never what.  Tiles of a
+// class are cut into the same number of parts, so that a tile's place among the
+// pieces and its slots follow from its place in its class.
 //
-// Bound by latency: one pass over cu_seqlens, two scans, one more pass.
-__global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, int n, const int32_t* __restrict__ cu,
-                                                                   PackedHead* __restrict__ head,
-                                                                   PackedTile* __restrict__ tiles, int max_tiles,
-                                                                   PackedTile* __restrict__ shorts, int max_shorts,
-                                                                   int32_t* __restrict__ pos) {
+// Bound by latency: one pass over cu_seqlens, two scans and a sum, one more pass.
+__global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, int n, int nkv, int group,
+                                                                   const int32_t* __restrict__ cu, char* plan,
+                                                                   PackedLayout lay) {
   const int tid = threadIdx.x;
   if (blockIdx.x > 0) {
     const int row = ((int)blockIdx.x - 1) * PLAN_THREADS + tid;
@@ -63,17 +90,22 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
       else lo = mid + 1;
     }
     const int start = lo >= 1 ? cu[lo - 1] : 0;
-    pos[row] = lo >= 1 && lo <= n && start >= 0 && start <= row ? row - start : -1;
+    ((int32_t*)(plan + lay.pos))[row] = lo >= 1 && lo <= n && start >= 0 && start <= row ? row - start : -1;
     return;
   }
-  __shared__ int level[LEVELS + 1];
-  __shared__ int part[PLAN_WAVES];
-  __shared__ int nshort;
+  PackedTile* tiles = (PackedTile*)(plan + lay.tiles);
+  PackedTile* shorts = (PackedTile*)(plan + lay.shorts);
+  PackedItem* items = (PackedItem*)(plan + lay.items);
+  // per class: counts of ranks, then tiles entered so far; first tile; first piece; first slot
+  __shared__ int level[LEVELS + 1], first[LEVELS], piece[LEVELS], slot[LEVELS];
+  __shared__ int part[1][PLAN_WAVES], part3[3][PLAN_WAVES];
+  __shared__ long long part64[PLAN_WAVES];
+  __shared__ int nshort, nsplit;
   const int max_rank = (total - 1) / PACKED_ROWS;
   int shift = 0;
   while (max_rank >> shift >= LEVELS) ++shift;
   for (int i = tid; i <= LEVELS; i += PLAN_THREADS) level[i] = 0;
-  if (tid == 0) nshort = 0;
+  if (tid == 0) nshort = nsplit = 0;
   __syncthreads();
   const int per = 1 << shift;
   for (int s = tid; s < n; s += PLAN_THREADS) {
@@ -87,34 +119,64 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
     atomicAdd(&level[top + 1], -rest);
   }
   __syncthreads();
-  // tiles per class, then the first slot of each class (the highest class first)
-  int c[4], sum = 0;
+  constexpr int PT = LEVELS / PLAN_THREADS;  // classes per thread
+  int c[PT], sum[1] = {0}, unused[1];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    sum += level[4 * tid + k];
-    c[k] = sum;
+  for (int k = 0; k < PT; ++k) {
+    sum[0] += level[PT * tid + k];
+    c[k] = sum[0];
   }
-  int before = block_scan(sum, part) - sum, tiles_here = 0;
+  const int mine = sum[0];
+  block_scan(sum, unused, part);
+  const int before = sum[0] - mine;
+  // work of a class's last rank, and of a part at most
+  auto units = [&](int l) { return (unsigned)(l + 1) << shift; };
+  long long work = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < PT; ++k) {
     c[k] += before;
-    tiles_here += c[k];
+    work += (long long)c[k] * units(PT * tid + k);
   }
-  const int upto = block_scan(tiles_here, part);
-  if (tid == PLAN_THREADS - 1) level[LEVELS] = upto;
-  __syncthreads();
-  const int all = level[LEVELS];
-  int slot = all - upto + tiles_here;  // tiles of this thread's classes and all higher ones
+  work = (block_sum(work, part64) * nkv + 2 * PACKED_CUS - 1) / (2 * PACKED_CUS);
+  const unsigned least = (PACKED_PART + group - 1) / group, most = 1u << 30;
+  const unsigned target = work < least ? least : work > most ? most : (unsigned)work;
+  auto parts_of = [&](int l) { return (int)min((units(l) + target - 1) / target, 1023u); };
+  // the first tile, piece and slot of each class, the highest class first
+  int own[3] = {0, 0, 0}, all[3];  // tiles, pieces, slots
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    slot -= c[k];
-    level[4 * tid + k] = slot;
+  for (int k = 0; k < PT; ++k) {
+    if (c[k] == 0) continue;
+    const int p = parts_of(PT * tid + k);
+    own[0] += c[k];
+    own[1] += c[k] * p;
+    own[2] += p > 1 ? c[k] * p : 0;
+    if (p > 1) atomicAdd(&nsplit, c[k]);
+  }
+  int upto_here[3] = {own[0], own[1], own[2]};
+  block_scan(upto_here, all, part3);
+  int at_t = all[0] - upto_here[0] + own[0], at_p = all[1] - upto_here[1] + own[1],
+      at_s = all[2] - upto_here[2] + own[2];
+#pragma unroll
+  for (int k = 0; k < PT; ++k) {
+    const int l = PT * tid + k;
+    level[l] = 0;
+    if (c[k] == 0) continue;
+    const int p = parts_of(l);
+    first[l] = at_t -= c[k];
+    piece[l] = at_p -= c[k] * p;
+    slot[l] = at_s -= p > 1 ? c[k] * p : 0;
   }
   __syncthreads();
   auto enter = [&](int start, int len, int rank) {
-    const int at = atomicAdd(&level[rank >> shift], 1);
-    // (lengths that are out of order may give more tiles than the list has room for)
-    if (at >= 0 && at < max_tiles) tiles[at] = PackedTile{start, len, rank, 0};
+    const int l = rank >> shift, p = parts_of(l);
+    const int i = atomicAdd(&level[l], 1), at = first[l] + i, q = piece[l] + i * p;
+    // (lengths that are out of order may give more tiles than the lists have room for)
+    if (at < 0 || at >= lay.max_tiles || q < 0 || q + p > lay.max_items) return;
+    PackedTile t{start, len, rank, 1, 0};
+    t.parts = (unsigned)p;
+    t.slot = p > 1 ? (unsigned)(slot[l] + i * p) : 0u;
+    tiles[at] = t;
+    for (int j = 0; j < p; ++j) items[q + j] = PackedItem{t, j, {0, 0, 0}};
   };
   // a thread enters the first tiles of its sequence, the wave the rest of a long one
   for (int s0 = 0; s0 < n; s0 += PLAN_THREADS) {
@@ -127,7 +189,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
       int at = 0;
       if (lane == 0) at = atomicAdd(&nshort, __popcll(few));
       at = __shfl(at, 0) + __popcll(few & ((1ull << lane) - 1));
-      if ((few >> lane & 1) && at < max_shorts) shorts[at] = PackedTile{start, len, 0, 0};
+      if ((few >> lane & 1) && at < lay.max_shorts) shorts[at] = PackedTile{start, len, 0, 1, 0};
     }
     if (len <= PACKED_SHORT) len = 0;
     const int m = len > 0 ? (len - 1) / PACKED_ROWS + 1 : 0;
@@ -141,7 +203,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
     }
   }
   __syncthreads();
-  if (tid == 0) *head = PackedHead{min(max(all, 0), max_tiles), min(nshort, max_shorts)};
+  if (tid == 0) {
+    auto upto = [](int v, int64_t most) { return (int)(v < 0 ? 0 : v > most ? most : v); };
+    *(PackedHead*)plan = PackedHead{upto(all[0], lay.max_tiles), upto(nshort, lay.max_shorts),
+                                    upto(all[1], lay.max_items), upto(nsplit, lay.max_tiles)};
+  }
 }
 
 // q and k of one row turned by its position: pairs (i, i + D/2) of every head,
@@ -208,11 +274,8 @@ size_t packed_plan_bytes(const PackedShape& p) { return packed_layout(p).total; 
 
 hipError_t packed_plan(const PackedShape& p, const int32_t* cu, void* plan, hipStream_t s) {
   const unsigned grid = 1 + (unsigned)((p.total + PLAN_THREADS - 1) / PLAN_THREADS);
-  const PackedLayout l = packed_layout(p);
-  char* b = (char*)plan;
-  hipLaunchKernelGGL(packed_plan_kernel, dim3(grid), dim3(PLAN_THREADS), 0, s, (int)p.total, p.n_seqs, cu,
-                     (PackedHead*)b, (PackedTile*)(b + l.tiles), (int)l.max_tiles, (PackedTile*)(b + l.shorts),
-                     (int)l.max_shorts, (int32_t*)(b + l.pos));
+  hipLaunchKernelGGL(packed_plan_kernel, dim3(grid), dim3(PLAN_THREADS), 0, s, (int)p.total, p.n_seqs, p.nkv,
+                     p.nq / p.nkv, cu, (char*)plan, packed_layout(p));
   return hipGetLastError();
 }
 
@@ -220,7 +283,7 @@ hipError_t packed_rope(const PackedShape& p, const void* plan, double theta, int
                        bf16_t* dst, hipStream_t s) {
   const int64_t need = (p.total + ROPE_WAVES - 1) / ROPE_WAVES;
   const dim3 grid((unsigned)(need < 8192 ? need : 8192)), block(64 * ROPE_WAVES);
-  const int32_t* pos = packed_view(p, plan).pos;
+  const int32_t* pos = packed_pos(p, plan);
   if (p.d == 128)
     hipLaunchKernelGGL((packed_rope_kernel<128>), grid, block, 0, s, (int)p.total, p.nq, p.nkv, log2(theta), inverse,
                        pos, src, dst);

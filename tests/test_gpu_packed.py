@@ -101,8 +101,8 @@ def test_peaked_scores(d):
 
 @pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (3, 1, 128)])
 def test_equal_lengths_are_the_attention_core(nq, nkv, d):
-    """Sequences of one length give what ls_attn_core_fwd gives, bit for bit; so does the backward where
-    the heads of a group are spread alike."""
+    """Sequences of one length give what ls_attn_core_fwd gives, bit for bit, and the dq of ls_attn_core_bwd; its
+    dk and dv may be added in another order."""
     need_gpu()
     n, S = 3, 257
     b = Batch([S] * n, nq, nkv, d, seed=7).run()
@@ -114,7 +114,8 @@ def test_equal_lengths_are_the_attention_core(nq, nkv, d):
     dqkv = torch.empty_like(b.dqkv)
     ws = torch.empty(L.ls_attn_core_bwd_workspace(c), dtype=torch.uint8, device="cuda")
     L.ls_attn_core_bwd(c, b.qkv, o, lse, b.dout, dqkv, ws)
-    assert torch.equal(dqkv, b.dqkv)
+    assert torch.equal(dqkv[:, :nq * d], b.dqkv[:, :nq * d])
+    check(b)
 
 
 def test_neighbours_do_not_matter():
@@ -172,6 +173,13 @@ def test_rope_far_positions():
         lo, hi = x[:, 64 * h:64 * h + 32], x[:, 64 * h + 32:64 * h + 64]
         ref = lo * np.cos(ang) - hi * np.sin(ang)
         assert np.all(np.abs(got[:, 64 * h:64 * h + 32] - ref) <= R.U * np.abs(ref) * 1.01 + 2.0 ** -21 * (abs(lo) + abs(hi)))
+
+
+@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (2, 2, 128), (8, 1, 128)])
+def test_one_long_sequence_among_others(nq, nkv, d):
+    """The dK/dV work of the long sequence's first keys is cut into parts."""
+    need_gpu()
+    check(Batch([40, 2500, 3, 100], nq, nkv, d, tail=2, seed=27).run())
 
 
 def test_many_sequences_and_every_row_once():
