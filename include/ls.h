@@ -472,8 +472,8 @@ int ls_gemm_tile_override(int32_t bm, int32_t bn);
  * "output projection", "gate/up projection", "down projection", "dact",
  * "dWd", "dh2", "dWg/dWu", "rmsnorm bwd", "dO", "dWo", "attention bwd",
  * "dh1", "dWqkv", "packed plan", "packed rope", "packed attention fwd",
- * "packed attention bwd", "head loss logits", "head loss rows", "head loss slots",
- * "head loss gather", "head loss dz", "head loss dh", "head loss dE", "head loss scatter", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
+ * "packed attention bwd", "head loss logits", "head loss rows", "head loss gather",
+ * "head loss dz", "head loss dh", "head loss dE", "head loss scatter", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
  * "logits", "cross-entropy", "dh head", "dE head", "loss", "embedding bwd",
  * and "adamw" for ls_adamw_step),
  * creating up to max_launches event pairs up front;

@@ -1674,8 +1674,8 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
   bf16_t* dz = at<bf16_t>(workspace, w.dz);
   float* dh32 = at<float>(workspace, w.dh);
   float* kpart = at<float>(workspace, w.kpart);
-  LS_STEP("head loss slots", st, ls::head_slots(T, (int)V, targets, dloss, slot, rows, coef, st));
-  LS_STEP("head loss gather", st, ls::head_gather(T, (int)H, slot, (const bf16_t*)h, targets, lse, hc, tc, lc, st));
+  LS_STEP("head loss gather", st,
+          ls::head_gather(T, (int)H, (int)V, targets, dloss, (const bf16_t*)h, lse, slot, rows, coef, hc, tc, lc, st));
   for (int64_t c0 = 0; c0 < V; c0 += w.bwd_piece) {
     const int64_t cols = std::min(w.bwd_piece, V - c0);
     {

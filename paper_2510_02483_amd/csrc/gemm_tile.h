@@ -359,8 +359,8 @@ constexpr float EPI_LOG2E = 1.4426950408889634f;
 // a block without any finite logit gets the maximum -inf and the sum 0.  In
 // fp32 throughout; v_exp_f32 flushes terms below 2^-126 of the row's largest,
 // which are nothing next to it.
-template <int TM, int TN>
-LS_DEV void lse_epilogue(const GemmArgs& p, f32x16 (&acc)[TM][TN], int mw, int nw, int block, int lr, int lh) {
+template <int TM, int TN, bool EDGE>
+LS_DEV void lse_rows(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw, int nw, int block, int lr, int lh) {
   int t[TM];  // target as a column of the wave's
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
@@ -368,28 +368,25 @@ LS_DEV void lse_epilogue(const GemmArgs& p, f32x16 (&acc)[TM][TN], int mw, int n
     t[i] = m < p.M ? p.target[m] : -1;
     t[i] = t[i] < 0 ? -1 : t[i] - p.col0 - nw;
   }
+  const int cols = p.N - nw - 4 * lh;  // EDGE: the lane's columns 32j + 8q + e below this count
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int m = mw + 32 * i + lr;
-    if (nw + 32 * TN > p.N) {
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (nw + 32 * j + 8 * (r >> 2) + 4 * lh + (r & 3) >= p.N) acc[i][j][r] = -INFINITY;
-    }
+    auto z = [&](int j, int r) {
+      return EDGE && 32 * j + 8 * (r >> 2) + (r & 3) >= cols ? -INFINITY : acc[i][j][r];
+    };
     float mx = -INFINITY;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, z(j, r));
     mx = halves_max(mx);
     const float mb = mx == -INFINITY ? 0.f : mx * EPI_LOG2E;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r & 3] += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], EPI_LOG2E, -mb));
+      for (int r = 0; r < 16; ++r) s[r & 3] += __builtin_amdgcn_exp2f(fmaf(z(j, r), EPI_LOG2E, -mb));
     const float sum = halves_sum((s[0] + s[1]) + (s[2] + s[3]));
     if (lh == 0 && m < p.M) *(float2*)(p.stats + 2 * ((int64_t)block * p.M + m)) = make_float2(mx, sum);
     if (__builtin_amdgcn_ballot_w64(t[i] >= 0 && t[i] < 32 * TN)) {
@@ -399,7 +396,15 @@ LS_DEV void lse_epilogue(const GemmArgs& p, f32x16 (&acc)[TM][TN], int mw, int n
         for (int r = 0; r < 16; ++r)
           if (32 * j + 8 * (r >> 2) + 4 * lh + (r & 3) == t[i]) p.zt[m] = acc[i][j][r];
     }
+    __builtin_amdgcn_sched_barrier(0);  // one row block's values in vector registers at a time
   }
+}
+// The last columns' tile by code of its own: masks in the common one, though never
+// taken there, cost it copies and register spills.
+template <int TM, int TN>
+LS_DEV void lse_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw, int nw, int block, int lr, int lh) {
+  if (nw + 32 * TN > p.N) lse_rows<TM, TN, true>(p, acc, mw, nw, block, lr, lh);
+  else lse_rows<TM, TN, false>(p, acc, mw, nw, block, lr, lh);
 }
 
 // EPI_DZ: what a row's logits become: softmax(z) - onehot, NaN in a row whose
@@ -420,9 +425,8 @@ struct DzRow {
     t -= p.col0;
   }
   // logit z of the product's column n
-  LS_DEV float operator()(float z, int n) const {
-    return __builtin_amdgcn_exp2f(fmaf(z, EPI_LOG2E, -l2)) - (n == t ? 1.f : 0.f);
-  }
+  LS_DEV float operator()(float z, int n) const { return p(z) - (n == t ? 1.f : 0.f); }
+  LS_DEV float p(float z) const { return __builtin_amdgcn_exp2f(fmaf(z, EPI_LOG2E, -l2)); }
 };
 
 // Epilogue of a 128-column tile (all but the fp32 weight gradients): 8 columns
@@ -1127,9 +1131,8 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
             if constexpr (EPI == EPI_DZ) {
-              const int n = nw + 32 * j + 8 * q + 4 * lh;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) v[e] = n + e < p.N ? dzr[i](v[e], n + e) : 0.f;
+              for (int e = 0; e < 4; ++e) v[e] = dzr[i].p(v[e]);
             }
             if constexpr (EPI == EPI_DE16) {
 #pragma unroll
@@ -1137,6 +1140,21 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
             }
             put4(32 * i + lr, 32 * j + 8 * q + 4 * lh, v);
           }
+        if constexpr (EPI == EPI_DZ) {
+          // the few targets among these columns, over their staged probabilities; then
+          // zeros in the columns from N to the next multiple of 8
+          const int c = dzr[i].t - nw;
+          if (__builtin_amdgcn_ballot_w64(c >= 0 && c < WN)) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (32 * j + 8 * (r >> 2) + 4 * lh + (r & 3) == c)
+                  stg[sb(32 * i + lr, c)] = (bf16_t)f2bf(dzr[i].p(acc[i][j][r]) - 1.f);
+          }
+          for (int z = p.N - nw; z >= 0 && z < WN && (z & 7); ++z)
+            if (lh == 0) stg[sb(32 * i + lr, z)] = 0;
+        }
       }
     }
     flush_bf16(p.C, p.ldc, nw, p.N - nw);

@@ -28,7 +28,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int HL_THREADS = 1024;
 constexpr int HL_WAVES = HL_THREADS / 64;
-constexpr int HL_ROWS = 64;  // rows per workgroup, one per lane
+constexpr int HL_ROWS = 64;     // rows per workgroup, one per lane
+constexpr int HL_FEW = 1024;    // up to so many rows a wave takes each
+constexpr int HL_GATHER = 512;  // threads of the gathering workgroups
 
 LS_DEV bool has_target(int t, int V) { return t >= 0 && t < V; }
 
@@ -54,55 +56,95 @@ LS_DEV void block_sums(double& v, int& n, double* vp, int* np) {
   }
 }
 
-// 64 rows per workgroup: wave w joins column blocks w, w + 16, .. of its lanes'
-// rows, then wave 0 joins the waves.  A lone workgroup also forms the loss.
-__global__ __launch_bounds__(HL_THREADS) void head_rows_kernel(int64_t T, int V, int64_t blocks,
-                                                               const float2* __restrict__ stats,
-                                                               const float* __restrict__ zt,
-                                                               const int32_t* __restrict__ targets,
-                                                               float* __restrict__ lse, float* __restrict__ row_loss,
-                                                               float* __restrict__ loss) {
-  __shared__ float pm[HL_WAVES][HL_ROWS], ps[HL_WAVES][HL_ROWS];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = (int64_t)blockIdx.x * HL_ROWS + lane;
+// A row's maximum and sum of exponentials, joined from its column blocks.  A block
+// without finite logits (max -inf, sum 0) changes nothing.
+struct RowStat {
   float m = -INFINITY, s = 0.f;
-  // a block without finite logits (max -inf, sum 0) changes nothing
-  auto join = [&](float bm, float bs) {
+  LS_DEV void join(float bm, float bs) {
     const float hi = fmaxf(m, bm);
     const float ref = hi == -INFINITY ? 0.f : hi;
     s = s * __builtin_amdgcn_exp2f((m - ref) * kLog2e) + bs * __builtin_amdgcn_exp2f((bm - ref) * kLog2e);
     m = hi;
-  };
-  if (row < T) {
-#pragma unroll 4
-    for (int64_t b = wave; b < blocks; b += HL_WAVES) {
-      const float2 x = stats[b * T + row];
-      join(x.x, x.y);
-    }
   }
-  pm[wave][lane] = m;
-  ps[wave][lane] = s;
-  __syncthreads();
-  if (wave != 0) return;
-  for (int w = 1; w < HL_WAVES; ++w) join(pm[w][lane], ps[w][lane]);
-  double sum = 0.0;
-  int n = 0;
-  if (row < T) {
+  // Writes the row's results; returns its loss and whether it counts.
+  LS_DEV float finish(int64_t row, int V, const float* zt, const int32_t* targets, float* lse, float* row_loss,
+                      int& n) const {
     const float l = m + __log2f(s) * kLn2;
     const int t = targets[row];
     const float r = t == -1 ? 0.f : has_target(t, V) ? l - zt[row] : NAN;
     lse[row] = l;
     row_loss[row] = r;
-    sum = r;
     n = has_target(t, V);
+    return r;
   }
-  if (gridDim.x == 1) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-      sum += __shfl_xor(sum, o);
-      n += __shfl_xor(n, o);
+};
+
+// 64 rows per workgroup: wave w joins column blocks w, w + 16, .. of its lanes'
+// rows, then wave 0 joins the waves.
+__global__ __launch_bounds__(HL_THREADS) void head_rows_kernel(int64_t T, int V, int64_t blocks,
+                                                               const float2* __restrict__ stats,
+                                                               const float* __restrict__ zt,
+                                                               const int32_t* __restrict__ targets,
+                                                               float* __restrict__ lse, float* __restrict__ row_loss) {
+  __shared__ float pm[HL_WAVES][HL_ROWS], ps[HL_WAVES][HL_ROWS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * HL_ROWS + lane;
+  RowStat st;
+  if (row < T) {
+#pragma unroll 4
+    for (int64_t b = wave; b < blocks; b += HL_WAVES) {
+      const float2 x = stats[b * T + row];
+      st.join(x.x, x.y);
     }
-    if (lane == 0) loss[0] = (float)(sum / (double)max(n, 1));
+  }
+  pm[wave][lane] = st.m;
+  ps[wave][lane] = st.s;
+  __syncthreads();
+  if (wave != 0 || row >= T) return;
+  for (int w = 1; w < HL_WAVES; ++w) st.join(pm[w][lane], ps[w][lane]);
+  int n;
+  st.finish(row, V, zt, targets, lse, row_loss, n);
+}
+
+// The same with a wave per row, its lanes at every 64th column block: for few rows,
+// whose blocks a lane would walk through one load after the other.  A lone
+// workgroup also forms the loss.
+__global__ __launch_bounds__(HL_THREADS) void head_rows_few_kernel(int64_t T, int V, int64_t blocks,
+                                                                   const float2* __restrict__ stats,
+                                                                   const float* __restrict__ zt,
+                                                                   const int32_t* __restrict__ targets,
+                                                                   float* __restrict__ lse,
+                                                                   float* __restrict__ row_loss,
+                                                                   float* __restrict__ loss) {
+  __shared__ float vp[HL_WAVES];
+  __shared__ int np[HL_WAVES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * HL_WAVES + wave;
+  RowStat st;
+  if (row < T) {
+#pragma unroll 4
+    for (int64_t b = lane; b < blocks; b += 64) {
+      const float2 x = stats[b * T + row];
+      st.join(x.x, x.y);
+    }
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) st.join(__shfl_xor(st.m, o), __shfl_xor(st.s, o));
+  if (lane == 0) {
+    int n = 0;
+    vp[wave] = row < T ? st.finish(row, V, zt, targets, lse, row_loss, n) : 0.f;
+    np[wave] = n;
+  }
+  if (gridDim.x > 1) return;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double v = 0.0;
+    int n = 0;
+    for (int w = 0; w < HL_WAVES; ++w) {
+      v += (double)vp[w];
+      n += np[w];
+    }
+    loss[0] = (float)(v / (double)max(n, 1));
   }
 }
 
@@ -122,56 +164,78 @@ __global__ __launch_bounds__(HL_THREADS) void head_mean_kernel(int64_t T, int V,
   if (threadIdx.x == 0) loss[0] = (float)(v / (double)max(n, 1));
 }
 
-// One workgroup: every row's place among the rows that have a target (kept in their
-// order), their number, and the factor of all gradients.
-__global__ __launch_bounds__(HL_THREADS) void head_slots_kernel(int64_t T, int V, const int32_t* __restrict__ targets,
+// The rows that have a target (any but -1), gathered in their order: every row's
+// place among them (-1: none), their number, their targets, lse and h, and the
+// factor of all gradients.  A workgroup takes `per` rows and counts the targets before
+// them by itself (4 bytes a row, from the L2), so that one launch does it all; the
+// last one sees every row and leaves the number and the factor.
+// Bound by HBM bandwidth: h is read once and written once.
+__global__ __launch_bounds__(HL_GATHER) void head_gather_kernel(int64_t T, int H, int V, int64_t per,
+                                                                const int32_t* __restrict__ targets,
                                                                 const float* __restrict__ dloss,
+                                                                const bf16_t* __restrict__ h,
+                                                                const float* __restrict__ lse,
                                                                 int32_t* __restrict__ slot, int* __restrict__ rows,
-                                                                float* __restrict__ coef) {
-  __shared__ int part[2][HL_WAVES];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int before = 0, valid = 0, buf = 0;
-  for (int64_t t0 = 0; t0 < T; t0 += HL_THREADS, buf ^= 1) {
-    const int64_t t = t0 + threadIdx.x;
-    const int g = t < T ? targets[t] : -1;
+                                                                float* __restrict__ coef, bf16_t* __restrict__ hc,
+                                                                int32_t* __restrict__ tc, float* __restrict__ lc) {
+  constexpr int WAVES = HL_GATHER / 64;
+  __shared__ int part[2][WAVES], place[HL_GATHER];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t r0 = (int64_t)blockIdx.x * per, r1 = r0 + per < T ? r0 + per : T;
+  int before = 0, valid = 0;
+  for (int64_t t = tid; t < r0; t += HL_GATHER) {
+    const int g = targets[t];
+    before += g != -1;
+    valid += has_target(g, V);
+  }
+  auto sum = [&](int v, int* p) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+    if (lane == 0) p[wave] = v;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) all += p[w];
+    return all;
+  };
+  before = sum(before, part[0]);
+  for (int64_t c0 = r0; c0 < r1; c0 += HL_GATHER) {
+    const int64_t t = c0 + tid;
+    const int g = t < r1 ? targets[t] : -1;
     valid += has_target(g, V);
     const unsigned long long in = __ballot(g != -1);
-    if (lane == 0) part[buf][wave] = __popcll(in);
-    __syncthreads();  // (two buffers: the next round's writes meet no reads of this one)
-    int at = before;
-    for (int w = 0; w < HL_WAVES; ++w) {
-      if (w < wave) at += part[buf][w];
-      before += part[buf][w];
+    if (lane == 0) part[1][wave] = __popcll(in);
+    __syncthreads();
+    int at = before + __popcll(in & ((1ull << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      at += w < wave ? part[1][w] : 0;
+      before += part[1][w];
     }
-    if (t < T) slot[t] = g == -1 ? -1 : at + __popcll(in & ((1ull << lane) - 1));
+    place[tid] = g == -1 ? -1 : at;
+    if (t < r1) {
+      slot[t] = place[tid];
+      if (g != -1) {
+        tc[at] = g;
+        lc[at] = lse[t];
+      }
+    }
+    __syncthreads();
+    const int n = (int)(r1 - c0 < HL_GATHER ? r1 - c0 : HL_GATHER);
+    for (int k = wave; k < n; k += WAVES) {
+      const int to = place[k];
+      if (to < 0) continue;
+      const u32x4* src = (const u32x4*)(h + (c0 + k) * H);
+      u32x4* dst = (u32x4*)(hc + (int64_t)to * H);
+      for (int c = lane; c < H / 8; c += 64) dst[c] = src[c];
+    }
+    __syncthreads();
   }
-  __shared__ double vp[HL_WAVES];
-  __shared__ int np[HL_WAVES];
-  double v = 0.0;
-  block_sums(v, valid, vp, np);
-  if (threadIdx.x == 0) {
+  if (blockIdx.x + 1 < gridDim.x) return;
+  valid = sum(valid, part[0]);
+  if (tid == 0) {
     rows[0] = before;
     coef[0] = (dloss ? dloss[0] : 1.0f) / (float)max(valid, 1);
-  }
-}
-
-// One wave per row.  Bound by HBM bandwidth: h is read once and written once.
-__global__ __launch_bounds__(256) void head_gather_kernel(int64_t T, int H, const int32_t* __restrict__ slot,
-                                                          const bf16_t* __restrict__ h,
-                                                          const int32_t* __restrict__ targets,
-                                                          const float* __restrict__ lse, bf16_t* __restrict__ hc,
-                                                          int32_t* __restrict__ tc, float* __restrict__ lc) {
-  const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t >= T) return;
-  const int at = slot[t];
-  if (at < 0) return;
-  const u32x4* src = (const u32x4*)(h + t * H);
-  u32x4* dst = (u32x4*)(hc + (int64_t)at * H);
-  for (int c = lane; c < H / 8; c += 64) dst[c] = src[c];
-  if (lane == 0) {
-    tc[at] = targets[t];
-    lc[at] = lse[t];
   }
 }
 
@@ -200,25 +264,29 @@ __global__ __launch_bounds__(256) void head_scatter_kernel(int64_t T, int H, con
 
 hipError_t head_rows(int64_t T, int V, int64_t blocks, const float* stats, const float* zt, const int32_t* targets,
                      float* lse, float* row_loss, float* loss, hipStream_t s) {
-  const unsigned grid = (unsigned)((T + HL_ROWS - 1) / HL_ROWS);
-  hipLaunchKernelGGL(head_rows_kernel, dim3(grid), dim3(HL_THREADS), 0, s, T, V, blocks, (const float2*)stats, zt,
-                     targets, lse, row_loss, loss);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || grid == 1) return e;
+  if (T <= HL_FEW) {
+    const unsigned grid = (unsigned)((T + HL_WAVES - 1) / HL_WAVES);
+    hipLaunchKernelGGL(head_rows_few_kernel, dim3(grid), dim3(HL_THREADS), 0, s, T, V, blocks, (const float2*)stats, zt,
+                       targets, lse, row_loss, loss);
+    if (grid == 1) return hipGetLastError();
+  } else {
+    hipLaunchKernelGGL(head_rows_kernel, dim3((unsigned)((T + HL_ROWS - 1) / HL_ROWS)), dim3(HL_THREADS), 0, s, T, V,
+                       blocks, (const float2*)stats, zt, targets, lse, row_loss);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL(head_mean_kernel, dim3(1), dim3(HL_THREADS), 0, s, T, V, targets, row_loss, loss);
   return hipGetLastError();
 }
 
-hipError_t head_slots(int64_t T, int V, const int32_t* targets, const float* dloss, int32_t* slot, int* rows,
-                      float* coef, hipStream_t s) {
-  hipLaunchKernelGGL(head_slots_kernel, dim3(1), dim3(HL_THREADS), 0, s, T, V, targets, dloss, slot, rows, coef);
-  return hipGetLastError();
-}
-
-hipError_t head_gather(int64_t T, int H, const int32_t* slot, const bf16_t* h, const int32_t* targets, const float* lse,
-                       bf16_t* hc, int32_t* tc, float* lc, hipStream_t s) {
-  hipLaunchKernelGGL(head_gather_kernel, dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, T, H, slot, h, targets, lse,
-                     hc, tc, lc);
+hipError_t head_gather(int64_t T, int H, int V, const int32_t* targets, const float* dloss, const bf16_t* h,
+                       const float* lse, int32_t* slot, int* rows, float* coef, bf16_t* hc, int32_t* tc, float* lc,
+                       hipStream_t s) {
+  // a row per wave, or as many as leave 512 workgroups
+  int64_t per = (T + 511) / 512;
+  if (per < HL_GATHER / 64) per = HL_GATHER / 64;
+  hipLaunchKernelGGL(head_gather_kernel, dim3((unsigned)((T + per - 1) / per)), dim3(HL_GATHER), 0, s, T, H, V, per,
+                     targets, dloss, h, lse, slot, rows, coef, hc, tc, lc);
   return hipGetLastError();
 }
 

@@ -180,13 +180,11 @@ hipError_t ce_loss(int64_t T, const float* row_loss, const int* counts, float* l
 // outside [-1, V)), and loss = sum(row_loss) / max(rows with a target in [0, V), 1).
 hipError_t head_rows(int64_t T, int V, int64_t blocks, const float* stats, const float* zt, const int32_t* targets,
                      float* lse, float* row_loss, float* loss, hipStream_t s);
-// The rows that have a target (any but -1), in their order: slot[t] = row t's place among them or -1, rows[0] = how
-// many, coef[0] = dloss[0] (null: 1) / max(rows with a target in [0, V), 1).
-hipError_t head_slots(int64_t T, int V, const int32_t* targets, const float* dloss, int32_t* slot, int* rows,
-                      float* coef, hipStream_t s);
-// h, targets and lse of those rows, gathered.
-hipError_t head_gather(int64_t T, int H, const int32_t* slot, const bf16_t* h, const int32_t* targets, const float* lse,
-                       bf16_t* hc, int32_t* tc, float* lc, hipStream_t s);
+// The rows that have a target (any but -1), gathered in their order: slot[t] = row t's place among them or -1,
+// rows[0] = how many, coef[0] = dloss[0] (null: 1) / max(rows with a target in [0, V), 1), and their h, targets, lse.
+hipError_t head_gather(int64_t T, int H, int V, const int32_t* targets, const float* dloss, const bf16_t* h,
+                       const float* lse, int32_t* slot, int* rows, float* coef, bf16_t* hc, int32_t* tc, float* lc,
+                       hipStream_t s);
 // dh[t] = coef dhc[slot[t]] rounded to bf16, 0 for a row without a target.
 hipError_t head_scatter(int64_t T, int H, const int32_t* slot, const float* coef, const float* dhc, bf16_t* dh,
                         hipStream_t s);
