@@ -38,8 +38,6 @@
 // first, which balances the triangular work over the compute units.
 #include <math.h>
 
-#include <algorithm>
-
 #include "packed.h"
 
 namespace ls {
@@ -233,63 +231,77 @@ LS_DEV void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Forward of one head of a packed sequence of up to 32 rows by one wave: every
+// Forward of one head of a packed sequence of up to 32 NB rows by one wave: every
 // operand straight from global memory, V through the wave's own LDS tile `vt` for
 // its transpose.  A workgroup's four waves work on four sequences, without
-// barriers, where a 128-row tile would leave three of them idle and wait
+// barriers, where a 128-row tile would leave most of them idle and wait
 // for one sequence's loads at a time: 301 sequences of 27 rows on average (179 at
-// most), 16 heads of 128: forward 50 -> 35 us, backward 176 -> 110 us.
-template <int D>
+// most), 16 heads of 128: forward 50 us in tiles, 33 so.
+template <int D, int NB>
 LS_DEV void short_fwd(const AttnShape& sh, const PackedTile& t, int h, const bf16_t* __restrict__ qkv,
                       bf16_t* __restrict__ o, float* __restrict__ lse, float sl2, bf16_t* vt) {
   const int nq = sh.nq, nkv = sh.nkv, kvh = h / (nq / nkv);
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
-  const bool ok = lr < t.len;
-  const bf16_t* row = qkv + (t.start + (int64_t)(ok ? lr : 0)) * ld;
-  u32x4 qf[D / 16], kf[D / 16], vf[D / 16];
-  get_rows<D>(vf, row + (nq + nkv + kvh) * D, ok, lh);
-  get_rows<D>(qf, row + h * D, ok, lh);
-  get_rows<D>(kf, row + (nq + kvh) * D, ok, lh);
-  put_rows<D>(vt, vf, lr, lh);
-  f32x16 s{};
+  auto row = [&](int b) { return qkv + (t.start + (int64_t)min(32 * b + lr, t.len - 1)) * ld; };
+  u32x4 qf[D / 16], kf[NB][D / 16];
+  get_rows<D>(qf, row(0) + h * D, lr < t.len, lh);
 #pragma unroll
-  for (int c = 0; c < D / 16; ++c) s = mfma32(kf[c], qf[c], s);
-  // lane holds query lr, keys 8(r/4) + 4lh + r%4
-  float mx = -INFINITY;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    if (8 * (r >> 2) + 4 * lh + (r & 3) > lr) s[r] = -INFINITY;
-    mx = fmaxf(mx, s[r]);
+  for (int b = 0; b < NB; ++b) {
+    u32x4 vf[D / 16];
+    get_rows<D>(kf[b], row(b) + (nq + kvh) * D, 32 * b + lr < t.len, lh);
+    get_rows<D>(vf, row(b) + (nq + nkv + kvh) * D, 32 * b + lr < t.len, lh);
+    put_rows<D>(vt + 32 * b * D, vf, lr, lh);
   }
-  const float m = halves_max(mx) * sl2;
-  float sum = 0.f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    s[r] = ex2(fmaf(s[r], sl2, -m));
-    sum += s[r];
-  }
-  const float l = halves_sum(sum);
   wave_lds_order();
-  f32x16 oacc[D / 32];
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) oacc[i] = f32x16{};
+  for (int qb = 0; qb < NB; ++qb) {
+    if (qb > 0) get_rows<D>(qf, row(qb) + h * D, 32 * qb + lr < t.len, lh);
+    f32x16 s[NB];
+    float mx = -INFINITY;
+    // lane holds query 32qb + lr, keys 32b + 8(r/4) + 4lh + r%4
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const u32x4 pf = pack_frag(s, 8 * c);
+    for (int b = 0; b <= qb; ++b) {
+      s[b] = f32x16{};
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) oacc[i] = mfma32(colt_frag<D>(vt, 32 * i, c, lane), pf, oacc[i]);
+      for (int c = 0; c < D / 16; ++c) s[b] = mfma32(kf[b][c], qf[c], s[b]);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (b == qb && 8 * (r >> 2) + 4 * lh + (r & 3) > lr) s[b][r] = -INFINITY;
+        mx = fmaxf(mx, s[b][r]);
+      }
+    }
+    const float m = halves_max(mx) * sl2;
+    float sum = 0.f;
+    f32x16 oacc[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) oacc[i] = f32x16{};
+#pragma unroll
+    for (int b = 0; b <= qb; ++b) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[b][r] = ex2(fmaf(s[b][r], sl2, -m));
+        sum += s[b][r];
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const u32x4 pf = pack_frag(s[b], 8 * c);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) oacc[i] = mfma32(colt_frag<D>(vt + 32 * b * D, 32 * i, c, lane), pf, oacc[i]);
+      }
+    }
+    const float l = halves_sum(sum);
+    if (32 * qb + lr >= t.len) continue;
+    const float inv = 1.0f / l;
+    bf16_t* orow = o + (t.start + (int64_t)(32 * qb + lr)) * nq * D + h * D;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq)
+        *(u32x2*)(orow + 32 * i + 8 * rq + 4 * lh) = u32x2{pack_bf2(oacc[i][4 * rq] * inv, oacc[i][4 * rq + 1] * inv),
+                                                           pack_bf2(oacc[i][4 * rq + 2] * inv, oacc[i][4 * rq + 3] * inv)};
+    if (lh == 0) lse[(int64_t)h * sh.seq + t.start + 32 * qb + lr] = (m + log2f(l)) * LN2;
   }
-  if (!ok) return;
-  const float inv = 1.0f / l;
-  bf16_t* orow = o + (t.start + (int64_t)lr) * nq * D + h * D;
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int rq = 0; rq < 4; ++rq)
-      *(u32x2*)(orow + 32 * i + 8 * rq + 4 * lh) = u32x2{pack_bf2(oacc[i][4 * rq] * inv, oacc[i][4 * rq + 1] * inv),
-                                                         pack_bf2(oacc[i][4 * rq + 2] * inv, oacc[i][4 * rq + 3] * inv)};
-  if (lh == 0) lse[(int64_t)h * sh.seq + t.start + lr] = (m + log2f(l)) * LN2;
 }
 
 template <int D, bool PACKED>
@@ -305,14 +317,16 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, PackedVi
   const int nq = sh.nq, nkv = sh.nkv;
   QTile qtile;
   if constexpr (PACKED) {
-    static_assert(sizeof(Ks) >= 4 * PACKED_SHORT * D * sizeof(bf16_t), "a tile of V per wave");
+    static_assert(sizeof(Ks) >= 2 * PACKED_MID * D * sizeof(bf16_t), "a tile of V per wave");
     PackedTile t;
     const int x = (int)blockIdx.x, head = x % nq;
     const bool whole = packed_unit(pk, x / nq, sh.seq, t);
     if (t.len == 0) return;
     if (!whole) {
       const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-      short_fwd<D>(sh, t, head, qkv, o, lse, sl2, &Ks[0][0] + w * PACKED_SHORT * D);
+      bf16_t* vt = (w < 2 ? &Ks[0][0] : &Vs[0][0]) + (w & 1) * PACKED_MID * D;
+      if (t.len <= PACKED_SHORT) short_fwd<D, 1>(sh, t, head, qkv, o, lse, sl2, vt);
+      else short_fwd<D, 2>(sh, t, head, qkv, o, lse, sl2, vt);
       return;
     }
     qtile = q_tile(sh, t, head);
@@ -619,6 +633,116 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const b
   unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * D);
 }
 
+// The same for a middle sequence, of up to 64 rows, by a pair of waves: wave j of the
+// pair owns keys and queries 32j .. 32j + 31, takes the other's Q, dO and K rows
+// from the pair's LDS tiles, and (wave 1) V of the first rows from global memory.
+// The barriers are the workgroup's, so both pairs go through all heads; a pair
+// without a sequence (len 0) only waits.
+template <int D>
+constexpr int mid_lds_bytes() {
+  return 3 * PACKED_MID * D * 2 + 2 * PACKED_MID * 4;
+}
+template <int D>
+LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf16_t* __restrict__ qkv,
+                    const bf16_t* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ Dv,
+                    bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds) {
+  constexpr int NSD = D / 16, NI = D / 32;
+  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv);
+  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
+  const int j = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) & 1, row = 32 * j + lr;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * D, ldo = (int64_t)nq * D;
+  const bool ok = row < t.len;
+  const int64_t r0 = t.start + (int64_t)(ok ? row : 0);
+  bf16_t *kt = (bf16_t*)lds, *qt = kt + PACKED_MID * D, *ot = qt + PACKED_MID * D;
+  float *lv = (float*)(ot + PACKED_MID * D), *dvv = lv + PACKED_MID;
+  u32x4 kf[NSD], vf[NSD], qf[NSD], of[NSD];
+  get_rows<D>(kf, qkv + r0 * ld + (nq + kvh) * D, ok, lh);
+  get_rows<D>(vf, qkv + r0 * ld + (nq + nkv + kvh) * D, ok, lh);
+  f32x16 dk[NI], dv[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) dk[i] = dv[i] = f32x16{};
+  for (int h = hq0; h < hq0 + nq / nkv; ++h) {
+    get_rows<D>(qf, qkv + r0 * ld + h * D, ok, lh);
+    get_rows<D>(of, dout + r0 * ldo + h * D, ok, lh);
+    const int64_t v = (int64_t)h * sh.seq + t.start;
+    const float L = ok ? lse2[v + row] : 0.f, Dr = ok ? Dv[v + row] : 0.f;
+    if (h > hq0) sync_lds();  // the tiles of the head before are read
+    if (h == hq0) put_rows<D>(kt + 32 * j * D, kf, lr, lh);
+    put_rows<D>(qt + 32 * j * D, qf, lr, lh);
+    put_rows<D>(ot + 32 * j * D, of, lr, lh);
+    if (lh == 0) {
+      lv[row] = L;
+      dvv[row] = Dr;
+    }
+    sync_lds();
+    if (t.len == 0) continue;
+    // the wave's keys, queries of block b: element r is query 32b + 8(r/4) + 4lh + r%4
+    for (int b = j; b < 2; ++b) {
+      f32x16 s{}, p{};
+#pragma unroll
+      for (int c = 0; c < NSD; ++c) {
+        s = mfma32(row_frag<D>(qt, 32 * b + lr, c, lh), kf[c], s);
+        p = mfma32(row_frag<D>(ot, 32 * b + lr, c, lh), vf[c], p);
+      }
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        const int at = 32 * b + 8 * rq + 4 * lh;
+        const f32x4 lq = *(const f32x4*)&lv[at], dq4 = *(const f32x4*)&dvv[at];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * rq + e;
+          if (at + e < row) s[r] = -INFINITY;
+          s[r] = ex2(fmaf(s[r], sl2, -lq[e]));
+          p[r] = s[r] * (p[r] - dq4[e]);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const u32x4 pf = pack_frag(s, 8 * c), sf = pack_frag(p, 8 * c);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          dv[i] = mfma32(colt_frag<D>(ot + 32 * b * D, 32 * i, c, lane), pf, dv[i]);
+          dk[i] = mfma32(colt_frag<D>(qt + 32 * b * D, 32 * i, c, lane), sf, dk[i]);
+        }
+      }
+    }
+    // the wave's queries, keys of block b: element r is key 32b + 8(r/4) + 4lh + r%4
+    f32x16 dq[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) dq[i] = f32x16{};
+    for (int b = 0; b <= j; ++b) {
+      f32x16 s{}, p{};
+      if (b == j) {
+#pragma unroll
+        for (int c = 0; c < NSD; ++c) p = mfma32(vf[c], of[c], p);
+      } else {  // (a middle sequence has all of its first 32 rows)
+        u32x4 v0[NSD];
+        get_rows<D>(v0, qkv + (t.start + (int64_t)lr) * ld + (nq + nkv + kvh) * D, lr < t.len, lh);
+#pragma unroll
+        for (int c = 0; c < NSD; ++c) p = mfma32(v0[c], of[c], p);
+      }
+#pragma unroll
+      for (int c = 0; c < NSD; ++c) s = mfma32(row_frag<D>(kt, 32 * b + lr, c, lh), qf[c], s);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float e = ex2(fmaf(s[r], sl2, -L));
+        if (32 * b + 8 * (r >> 2) + 4 * lh + (r & 3) > row) e = 0.f;
+        p[r] = e * (p[r] - Dr);
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const u32x4 sf = pack_frag(p, 8 * c);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) dq[i] = mfma32(colt_frag<D>(kt + 32 * b * D, 32 * i, c, lane), sf, dq[i]);
+      }
+    }
+    if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * D);
+  }
+  if (!ok) return;
+  unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * D);
+  unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * D);
+}
+
 // dK and dV for 128 keys of one kv head (4 waves x 32 keys), summed over the
 // query heads of the group, no atomics.  The 1-D grid runs the key tiles with
 // the most queries after them (lowest key index) first.  With few kv heads
@@ -642,7 +766,7 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const b
 // head, or a part of its 64-query steps of all heads of the group, whose partial
 // sums go to a slot of `part`), or past those four short sequences and a kv head.
 template <int D, bool SPLIT, bool PACKED>
-__global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, PackedView pk,
+__global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_kernel(AttnShape sh, PackedView pk,
                                                                 const bf16_t* __restrict__ qkv,
                                                                 const bf16_t* __restrict__ dout,
                                                                 const float* __restrict__ lse2,
@@ -676,11 +800,17 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(AttnShape sh, Pac
   int64_t row0 = (int64_t)b * S, vec0 = (int64_t)b * nq * S;  // this sequence's first row; its entry of head 0's vectors
   int parts = 1, part_no = 0, slot = 0;
   if constexpr (PACKED) {
-    static_assert(sizeof(stg) >= 4 * short_lds_bytes<D>(), "the tiles of a short sequence per wave");
+    static_assert(sizeof(stg) >= 4 * short_lds_bytes<D>() && sizeof(stg) >= 2 * mid_lds_bytes<D>(),
+                  "the tiles of small sequences");
     PackedTile t;
-    const bool whole = packed_piece(pk, kvt, sh.seq, t, part_no);
+    const PackedKind kind = packed_piece(pk, kvt, sh.seq, t, part_no);
+    if (kind == PACKED_IS_MID) {
+      const int pair = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 7);
+      mid_bwd<D>(sh, t, kvh, qkv, dout, lse2, Dv, dqkv, scale, sl2, (char*)&stg[0] + pair * mid_lds_bytes<D>());
+      return;
+    }
     if (t.len == 0) return;
-    if (!whole) {
+    if (kind == PACKED_IS_SHORT) {
       const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
       short_bwd<D>(sh, t, kvh, qkv, dout, lse2, Dv, dqkv, scale, sl2, (char*)&stg[0] + w * short_lds_bytes<D>());
       return;
@@ -1115,7 +1245,7 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, Packe
 template <int D, bool PACKED>
 hipError_t attn_fwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, bf16_t* o, float* lse,
                       hipStream_t s) {
-  const unsigned grid = PACKED ? (unsigned)(pk.max_tiles + 1) * sh.nq
+  const unsigned grid = PACKED ? (unsigned)pk.max_units * sh.nq
                                : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
   const float sl2 = LOG2E / sqrtf((float)(sh.d_scale > 0 ? sh.d_scale : D));
   hipLaunchKernelGGL((attn_fwd_kernel<D, PACKED>), dim3(grid), dim3(256), 0, s, sh, pk, qkv, o, lse, sl2);
@@ -1186,7 +1316,7 @@ hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const float scale = 1.0f / sqrtf((float)D);
-  const unsigned gkv = (unsigned)(pk.max_items + 1) * sh.nkv;
+  const unsigned gkv = (unsigned)(pk.max_units + pk.max_items - pk.max_tiles) * sh.nkv;
   hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, true>), dim3(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
                      (const float*)lse2, (const float*)Dv, dqkv, (const float*)nullptr, scale, scale * LOG2E, 1, part);
   e = hipGetLastError();

@@ -2,21 +2,27 @@
 //   PackedHead, how many tiles and short sequences there are;
 //   PackedTile of every PACKED_ROWS rows of every sequence that is not short, in
 //     order of falling work, packed_max_tiles() of them at most;
-//   PackedTile (rank 0) of every short sequence, of up to PACKED_SHORT rows;
+//   PackedTile (rank 0) of every middle sequence, of more than PACKED_SHORT and up to
+//     PACKED_MID rows, and of every short one, of up to PACKED_SHORT;
 //   PackedItem of every piece of work of the dK/dV kernel on tiles: a key tile, or
 //     a part of the queries of one with many, in the tiles' order;
 //   one int32 per row: its position in its sequence, or -1.
 // The lengths are known on the device only, so the attention's launches cover as
-// much work as there can be: unit u is tile u, or, past the tiles, four short
-// sequences, one per wave.
+// much work as there can be: unit u is tile u, or, past the tiles, middle and short
+// sequences: four, one per wave, of the forward kernel; of the dK/dV kernel two middle ones,
+// two waves each, or four short ones.
 #pragma once
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 
 namespace ls {
 
+constexpr int PACKED_MID = 64;
+
 struct PackedHead {
-  int32_t tiles, shorts, items, split;  // split: the first tiles, whose work is cut into parts
+  int32_t tiles, mids, shorts, items, split;  // split: the first tiles, whose work is cut into parts
 };
 
 // Tile `rank` (0-based, rows PACKED_ROWS * rank .. of the sequence) of the sequence of
@@ -37,8 +43,8 @@ struct PackedItem {
 
 // Where the parts of a plan lie.
 struct PackedLayout {
-  int64_t max_tiles, max_shorts, max_items, max_slots;
-  size_t tiles, shorts, items, pos, total;
+  int64_t max_tiles, max_mids, max_shorts, max_items, max_slots, max_units;
+  size_t tiles, mids, shorts, items, pos, total;
 };
 // A key tile of rank r is r + 1 units of dK/dV work per kv head (128 queries of every
 // head of the group each).  A tile with more than half of a compute unit's share
@@ -50,10 +56,19 @@ inline PackedLayout packed_layout(const PackedShape& p) {
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   PackedLayout l;
   l.max_shorts = p.n_seqs < p.total ? p.n_seqs : p.total;
-  // a sequence of n rows has at most (n + PACKED_ROWS - 1) / PACKED_ROWS tiles
-  l.max_tiles = (p.total + (PACKED_ROWS - 1) * l.max_shorts) / PACKED_ROWS;
+  // At most `big` sequences are long enough for tiles, and one of n rows has at most 1 + n / PACKED_ROWS.
+  const int64_t big = std::min(l.max_shorts, p.total / (PACKED_MID + 1));
+  l.max_tiles = std::max<int64_t>(big + p.total / PACKED_ROWS, 1);
+  // The work that all sequences can make, in units: a sequence of tiles takes its tiles, a middle one half a unit and
+  // more than half as many rows as the shortest of tiles, a short one a quarter.  So most units come from as many
+  // sequences of tiles as the rows allow, and short ones for the rest.  (A workgroup without work costs about a
+  // microsecond of its compute unit, which it must have to itself in the dK/dV kernel.)
+  l.max_units = l.max_tiles + (l.max_shorts - big) / 4 + 2;
+  const int64_t mids = (p.total + PACKED_SHORT) / (PACKED_SHORT + 1);
+  l.max_mids = l.max_shorts < mids ? l.max_shorts : mids;
   l.tiles = 256;
-  l.shorts = l.tiles + up((size_t)l.max_tiles * sizeof(PackedTile));
+  l.mids = l.tiles + up((size_t)l.max_tiles * sizeof(PackedTile));
+  l.shorts = l.mids + up((size_t)l.max_mids * sizeof(PackedTile));
   l.max_items = l.max_tiles + 2 * PACKED_CUS / p.nkv;
   l.max_slots = 2 * (2 * PACKED_CUS / p.nkv);
   l.items = l.shorts + up((size_t)l.max_shorts * sizeof(PackedTile));
@@ -66,16 +81,17 @@ inline PackedLayout packed_layout(const PackedShape& p) {
 struct PackedView {
   const PackedHead* head = nullptr;
   const PackedTile* tiles = nullptr;
+  const PackedTile* mids = nullptr;
   const PackedTile* shorts = nullptr;
   const PackedItem* items = nullptr;
-  int max_tiles = 0, max_shorts = 0, max_items = 0, max_slots = 0;
+  int max_tiles = 0, max_mids = 0, max_shorts = 0, max_items = 0, max_slots = 0, max_units = 0;
 };
 inline PackedView packed_view(const PackedShape& p, const void* plan) {
   const PackedLayout l = packed_layout(p);
   const char* b = (const char*)plan;
-  return PackedView{(const PackedHead*)b, (const PackedTile*)(b + l.tiles), (const PackedTile*)(b + l.shorts),
-                    (const PackedItem*)(b + l.items), (int)l.max_tiles, (int)l.max_shorts, (int)l.max_items,
-                    (int)l.max_slots};
+  return PackedView{(const PackedHead*)b, (const PackedTile*)(b + l.tiles), (const PackedTile*)(b + l.mids),
+                    (const PackedTile*)(b + l.shorts), (const PackedItem*)(b + l.items), (int)l.max_tiles,
+                    (int)l.max_mids, (int)l.max_shorts, (int)l.max_items, (int)l.max_slots, (int)l.max_units};
 }
 // Tiles whose dK/dV work may be cut into parts (two slots each at least).
 __host__ __device__ inline int packed_max_split(const PackedView& v) {
@@ -98,9 +114,9 @@ LS_DEV PackedTile packed_checked(PackedTile t, int total) {
     t = PackedTile{};
   return t;
 }
-// Unit u of a launch over tiles and short sequences: tile u (true), or this wave's
-// sequence of the four that unit u holds (false); len 0 where there is none.
-// Counts and both entries are loaded at once, not one after the other.
+// Unit u of the forward and dQ kernels: tile u (true), or this wave's sequence of
+// the four that unit u holds, middle ones first (false); len 0 where there is none.
+// Counts and entry are loaded at once, not one after the other.
 LS_DEV bool packed_unit(const PackedView& v, int u, int total, PackedTile& t) {
   const PackedHead h = *v.head;
   const PackedTile a = v.tiles[min(u, v.max_tiles - 1)];
@@ -109,14 +125,18 @@ LS_DEV bool packed_unit(const PackedView& v, int u, int total, PackedTile& t) {
     t = packed_checked(a, total);
     return true;
   }
-  const int i = __builtin_amdgcn_readfirstlane(4 * (u - tiles) + ((int)threadIdx.x >> 6));
+  int i = __builtin_amdgcn_readfirstlane(4 * (u - tiles) + ((int)threadIdx.x >> 6));
+  const int mids = packed_count(h.mids, v.max_mids);
   t = PackedTile{};
-  if (i < packed_count(h.shorts, v.max_shorts)) t = packed_checked(v.shorts[i], total);
-  if (t.len > PACKED_SHORT) t = PackedTile{};
+  if (i < mids) t = packed_checked(v.mids[i], total);
+  else if ((i -= mids) < packed_count(h.shorts, v.max_shorts)) t = packed_checked(v.shorts[i], total);
+  if (t.len > PACKED_MID) t = PackedTile{};
   return false;
 }
-// The same for dK/dV: piece u of the tiles' work, or a short sequence.
-LS_DEV bool packed_piece(const PackedView& v, int u, int total, PackedTile& t, int& part) {
+// Unit u of the dK/dV kernel: a piece of the tiles' work, two middle sequences (this
+// wave's: that of its pair) or four short ones.
+enum PackedKind { PACKED_IS_TILE, PACKED_IS_MID, PACKED_IS_SHORT };
+LS_DEV PackedKind packed_piece(const PackedView& v, int u, int total, PackedTile& t, int& part) {
   const PackedHead h = *v.head;
   const PackedItem a = v.items[min(u, v.max_items - 1)];
   const int items = packed_count(h.items, v.max_items);
@@ -124,13 +144,22 @@ LS_DEV bool packed_piece(const PackedView& v, int u, int total, PackedTile& t, i
     t = packed_checked(a.tile, total);
     part = __builtin_amdgcn_readfirstlane(a.part);
     if (part < 0 || part >= (int)t.parts || (t.parts > 1 && (int)(t.slot + t.parts) > v.max_slots)) t = PackedTile{};
-    return true;
+    return PACKED_IS_TILE;
   }
-  const int i = __builtin_amdgcn_readfirstlane(4 * (u - items) + ((int)threadIdx.x >> 6));
+  u -= items;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int mids = packed_count(h.mids, v.max_mids), units = (mids + 1) / 2;
   t = PackedTile{};
-  if (i < packed_count(h.shorts, v.max_shorts)) t = packed_checked(v.shorts[i], total);
+  if (u < units) {
+    const int i = 2 * u + (wave >> 1);
+    if (i < mids) t = packed_checked(v.mids[i], total);
+    if (t.len > PACKED_MID) t = PackedTile{};
+    return PACKED_IS_MID;
+  }
+  const int i = 4 * (u - units) + wave;
+  if (i >= 0 && i < packed_count(h.shorts, v.max_shorts)) t = packed_checked(v.shorts[i], total);
   if (t.len > PACKED_SHORT) t = PackedTile{};
-  return false;
+  return PACKED_IS_SHORT;
 }
 
 }  // namespace ls

@@ -63,7 +63,7 @@ LS_DEV long long block_sum(long long v, long long* part) {
   return s;
 }
 
-// Workgroup 0 lists the tiles, the short sequences and the pieces of dK/dV work, the
+// Workgroup 0 lists the tiles, the middle and short sequences and the pieces of dK/dV work, the
 // others find the rows' positions.
 //
 // The list of tiles is a counting sort by rank (a tile's work), the highest first:
@@ -94,24 +94,25 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
     return;
   }
   PackedTile* tiles = (PackedTile*)(plan + lay.tiles);
+  PackedTile* mids = (PackedTile*)(plan + lay.mids);
   PackedTile* shorts = (PackedTile*)(plan + lay.shorts);
   PackedItem* items = (PackedItem*)(plan + lay.items);
   // per class: counts of ranks, then tiles entered so far; first tile; first piece; first slot
   __shared__ int level[LEVELS + 1], first[LEVELS], piece[LEVELS], slot[LEVELS];
   __shared__ int part[1][PLAN_WAVES], part3[3][PLAN_WAVES];
   __shared__ long long part64[PLAN_WAVES];
-  __shared__ int nshort, nsplit;
+  __shared__ int nmid, nshort, nsplit;
   const int max_rank = (total - 1) / PACKED_ROWS;
   int shift = 0;
   while (max_rank >> shift >= LEVELS) ++shift;
   for (int i = tid; i <= LEVELS; i += PLAN_THREADS) level[i] = 0;
-  if (tid == 0) nshort = nsplit = 0;
+  if (tid == 0) nmid = nshort = nsplit = 0;
   __syncthreads();
   const int per = 1 << shift;
   for (int s = tid; s < n; s += PLAN_THREADS) {
     int start;
     const int len = seq_len(cu, s, total, start);
-    if (len <= PACKED_SHORT) continue;
+    if (len <= PACKED_MID) continue;
     // classes 0 .. top-1 get `per` ranks each, class `top` the rest
     const int m = (len - 1) / PACKED_ROWS + 1, top = (m - 1) >> shift, rest = m - (top << shift);
     atomicAdd(&level[0], per);
@@ -183,15 +184,18 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
     const int s = s0 + tid;
     int start = 0, len = 0;
     if (s < n) len = seq_len(cu, s, total, start);
-    const unsigned long long few = __ballot(len > 0 && len <= PACKED_SHORT);
-    if (few) {
+    auto enter_small = [&](bool in, int* count, PackedTile* list, int64_t room) {
+      const unsigned long long few = __ballot(in);
+      if (!few) return;
       const int lane = tid & 63;
       int at = 0;
-      if (lane == 0) at = atomicAdd(&nshort, __popcll(few));
+      if (lane == 0) at = atomicAdd(count, __popcll(few));
       at = __shfl(at, 0) + __popcll(few & ((1ull << lane) - 1));
-      if ((few >> lane & 1) && at < lay.max_shorts) shorts[at] = PackedTile{start, len, 0, 1, 0};
-    }
-    if (len <= PACKED_SHORT) len = 0;
+      if (in && at < room) list[at] = PackedTile{start, len, 0, 1, 0};
+    };
+    enter_small(len > PACKED_SHORT && len <= PACKED_MID, &nmid, mids, lay.max_mids);
+    enter_small(len > 0 && len <= PACKED_SHORT, &nshort, shorts, lay.max_shorts);
+    if (len <= PACKED_MID) len = 0;
     const int m = len > 0 ? (len - 1) / PACKED_ROWS + 1 : 0;
     for (int r = 0; r < m && r < FEW; ++r) enter(start, len, r);
     unsigned long long longer = __ballot(m > FEW);
@@ -205,7 +209,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   __syncthreads();
   if (tid == 0) {
     auto upto = [](int v, int64_t most) { return (int)(v < 0 ? 0 : v > most ? most : v); };
-    *(PackedHead*)plan = PackedHead{upto(all[0], lay.max_tiles), upto(nshort, lay.max_shorts),
+    *(PackedHead*)plan = PackedHead{upto(all[0], lay.max_tiles), upto(nmid, lay.max_mids), upto(nshort, lay.max_shorts),
                                     upto(all[1], lay.max_items), upto(nsplit, lay.max_tiles)};
   }
 }

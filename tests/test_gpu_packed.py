@@ -72,6 +72,7 @@ LENGTHS = {
     "rows_of_one": dict(lens=[1] * 70, tail=3),
     "empty_ones": dict(lens=[0, 5, 0, 0, 131, 0], first=7, tail=9),
     "around_a_tile": dict(lens=[127, 128, 129, 63, 64, 65]),
+    "small_ones": dict(lens=[31, 32, 33, 34, 63, 64, 65, 40, 48, 2, 64]),
     "mixed": dict(lens=[300, 1, 0, 513, 33, 2], tail=130),
     "all_empty": dict(lens=[0, 0], first=3, tail=140),
 }
