@@ -1086,6 +1086,7 @@ static int check_packed_cfg(const ls_packed_cfg* c, ls::PackedShape& p) {
   // rows and positions are 32-bit, a row's byte offset inside a 64-row tile too, and
   // there is a workgroup per tile and head
   if (c->total >= (int64_t)1 << 28) return fail(LS_ERR_SHAPE, "total (%lld) reaches 2^28", (long long)c->total);
+  if (c->n_seqs >= 1 << 28) return fail(LS_ERR_SHAPE, "n_seqs (%d) reaches 2^28", c->n_seqs);
   if (((int64_t)c->n_q_heads + 2 * (int64_t)c->n_kv_heads) * c->head_dim >= (int64_t)1 << 20)
     return fail(LS_ERR_SHAPE, "a row of q, k and v reaches 2^20 features");
   if (c->total * c->n_q_heads >= (int64_t)1 << 31)

@@ -213,6 +213,12 @@ LS_DEV QTile q_tile(const AttnShape& sh, const PackedTile& t, int h) {
 // log-sum-exp m + log2 l, does not depend on the reference point.
 constexpr float LAG = 8.0f;
 
+// Query head of the y-th workgroup of a packed tile or unit: the kv heads one after the
+// other, so that where their number allows, all readers of one kv head's keys and
+// values run on the same XCD (workgroups go to the 8 XCDs in turn) and find them
+// in its L2 (24/8 heads of 128, 8135 rows: forward 166 -> 164 us, training pass 710 -> 703).
+LS_DEV int packed_head(int y, int nq, int nkv) { return y % nkv * (nq / nkv) + y / nkv; }
+
 // A wave's own 32-row tile in LDS, from the rows that its lanes hold as MFMA
 // operands (lane: row lr, d = 16s + 8lh .. +7), for transposing reads.
 template <int D>
@@ -319,7 +325,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, PackedVi
   if constexpr (PACKED) {
     static_assert(sizeof(Ks) >= 2 * PACKED_MID * D * sizeof(bf16_t), "a tile of V per wave");
     PackedTile t;
-    const int x = (int)blockIdx.x, head = x % nq;
+    const int x = (int)blockIdx.x, head = packed_head(x % nq, nq, nkv);
     const bool whole = packed_unit(pk, x / nq, sh.seq, t);
     if (t.len == 0) return;
     if (!whole) {
@@ -1125,7 +1131,7 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, Packe
     }
     PackedTile t;
     if (!packed_unit(pk, (x - joins) / nq, sh.seq, t) || t.len == 0) return;
-    qtile = q_tile(sh, t, (x - joins) % nq);
+    qtile = q_tile(sh, t, packed_head((x - joins) % nq, nq, nkv));
   } else {
     qtile = q_tile(sh);
   }

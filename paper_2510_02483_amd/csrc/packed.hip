@@ -11,7 +11,6 @@ namespace {
 constexpr int PLAN_THREADS = 512;
 constexpr int PLAN_WAVES = PLAN_THREADS / 64;
 constexpr int LEVELS = 4 * PLAN_THREADS;  // classes of work that the list of tiles is ordered by
-constexpr int FEW = 4;                    // tiles of a sequence that one thread enters by itself
 
 // Inclusive prefix sums of N values over the workgroup's threads, and their totals.
 // (`part` may be used again after a barrier.)
@@ -179,7 +178,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
     tiles[at] = t;
     for (int j = 0; j < p; ++j) items[q + j] = PackedItem{t, j, {0, 0, 0}};
   };
-  // a thread enters the first tiles of its sequence, the wave the rest of a long one
+  // a wave takes 64 sequences at a time and enters 64 of their tiles at a time
   for (int s0 = 0; s0 < n; s0 += PLAN_THREADS) {
     const int s = s0 + tid;
     int start = 0, len = 0;
@@ -197,13 +196,20 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
     enter_small(len > 0 && len <= PACKED_SHORT, &nshort, shorts, lay.max_shorts);
     if (len <= PACKED_MID) len = 0;
     const int m = len > 0 ? (len - 1) / PACKED_ROWS + 1 : 0;
-    for (int r = 0; r < m && r < FEW; ++r) enter(start, len, r);
-    unsigned long long longer = __ballot(m > FEW);
-    while (longer) {
-      const int l = __builtin_ctzll(longer);
-      longer &= longer - 1;
-      const int wstart = __shfl(start, l), wlen = __shfl(len, l), wm = __shfl(m, l);
-      for (int r = FEW + (tid & 63); r < wm; r += 64) enter(wstart, wlen, r);
+    int upto = m;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(upto, o);
+      if ((tid & 63) >= o) upto += u;
+    }
+    const int in_wave = __shfl(upto, 63);
+    for (int f = tid & 63; f - (tid & 63) < in_wave; f += 64) {
+      int l = 0;  // sequences of the wave whose tiles all come before the f-th
+#pragma unroll
+      for (int b = 32; b >= 1; b >>= 1)
+        if (__shfl(upto, l + b - 1) <= f) l += b;
+      const int lstart = __shfl(start, l), llen = __shfl(len, l), first_f = __shfl(upto - m, l);
+      if (f < in_wave) enter(lstart, llen, f - first_f);
     }
   }
   __syncthreads();

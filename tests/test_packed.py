@@ -47,7 +47,7 @@ CALLS = (plan, rope, fwd, bwd)
 @pytest.mark.parametrize("bad,status", [
     (dict(total=0), SHAPE), (dict(total=-5), SHAPE), (dict(n_seqs=0), SHAPE), (dict(nq=0), SHAPE), (dict(nkv=0), SHAPE),
     (dict(nq=3, nkv=2), SHAPE), (dict(d=104), UNSUPPORTED), (dict(d=32), UNSUPPORTED), (dict(d=0), SHAPE),
-    (dict(total=1 << 28), SHAPE), (dict(total=(1 << 28) - 1, nq=16, nkv=8), SHAPE), (dict(nq=1 << 14, nkv=1), SHAPE),
+    (dict(total=1 << 28), SHAPE), (dict(n_seqs=1 << 28), SHAPE), (dict(total=(1 << 28) - 1, nq=16, nkv=8), SHAPE), (dict(nq=1 << 14, nkv=1), SHAPE),
 ])
 def test_shapes_refused(call, bad, status):
     assert call(cfg(**bad), nbytes=BIG) == status
