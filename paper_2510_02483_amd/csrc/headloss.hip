@@ -28,8 +28,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int HL_THREADS = 1024;
 constexpr int HL_WAVES = HL_THREADS / 64;
-constexpr int HL_ROWS = 64;     // rows per workgroup, one per lane
-constexpr int HL_FEW = 1024;    // up to so many rows a wave takes each
+constexpr int HL_ROWS = 16;     // rows per workgroup of head_rows_kernel
 constexpr int HL_GATHER = 512;  // threads of the gathering workgroups
 
 LS_DEV bool has_target(int t, int V) { return t >= 0 && t < V; }
@@ -79,73 +78,47 @@ struct RowStat {
   }
 };
 
-// 64 rows per workgroup: wave w joins column blocks w, w + 16, .. of its lanes'
-// rows, then wave 0 joins the waves.
+// 16 rows per workgroup and 64 threads per row, each at every 64th column block (16
+// neighbouring rows' 8 bytes are one 128-byte line); then wave 0 joins the 64.  A
+// lone workgroup also forms the loss.  Bound by latency (few rows: the walk over
+// the blocks) and by reading 8 bytes per row and block: with the mean's launch 11 to
+// 14 us for 256 to 4096 rows of 1002 blocks; 64 rows per workgroup took 15 to 17.
 __global__ __launch_bounds__(HL_THREADS) void head_rows_kernel(int64_t T, int V, int64_t blocks,
                                                                const float2* __restrict__ stats,
                                                                const float* __restrict__ zt,
                                                                const int32_t* __restrict__ targets,
-                                                               float* __restrict__ lse, float* __restrict__ row_loss) {
-  __shared__ float pm[HL_WAVES][HL_ROWS], ps[HL_WAVES][HL_ROWS];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = (int64_t)blockIdx.x * HL_ROWS + lane;
+                                                               float* __restrict__ lse, float* __restrict__ row_loss,
+                                                               float* __restrict__ loss) {
+  constexpr int PER = HL_THREADS / HL_ROWS;  // threads per row
+  __shared__ float pm[PER][HL_ROWS], ps[PER][HL_ROWS];
+  const int lane = threadIdx.x & 63, r = threadIdx.x % HL_ROWS, k = threadIdx.x / HL_ROWS;
+  const int64_t row = (int64_t)blockIdx.x * HL_ROWS + r;
   RowStat st;
   if (row < T) {
 #pragma unroll 4
-    for (int64_t b = wave; b < blocks; b += HL_WAVES) {
+    for (int64_t b = k; b < blocks; b += PER) {
       const float2 x = stats[b * T + row];
       st.join(x.x, x.y);
     }
   }
-  pm[wave][lane] = st.m;
-  ps[wave][lane] = st.s;
+  pm[k][r] = st.m;
+  ps[k][r] = st.s;
   __syncthreads();
-  if (wave != 0 || row >= T) return;
-  for (int w = 1; w < HL_WAVES; ++w) st.join(pm[w][lane], ps[w][lane]);
-  int n;
-  st.finish(row, V, zt, targets, lse, row_loss, n);
-}
-
-// The same with a wave per row, its lanes at every 64th column block: for few rows,
-// whose blocks a lane would walk through one load after the other.  A lone
-// workgroup also forms the loss.
-__global__ __launch_bounds__(HL_THREADS) void head_rows_few_kernel(int64_t T, int V, int64_t blocks,
-                                                                   const float2* __restrict__ stats,
-                                                                   const float* __restrict__ zt,
-                                                                   const int32_t* __restrict__ targets,
-                                                                   float* __restrict__ lse,
-                                                                   float* __restrict__ row_loss,
-                                                                   float* __restrict__ loss) {
-  __shared__ float vp[HL_WAVES];
-  __shared__ int np[HL_WAVES];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = (int64_t)blockIdx.x * HL_WAVES + wave;
-  RowStat st;
-  if (row < T) {
-#pragma unroll 4
-    for (int64_t b = lane; b < blocks; b += 64) {
-      const float2 x = stats[b * T + row];
-      st.join(x.x, x.y);
-    }
-  }
+  if (threadIdx.x >= 64) return;
+  for (int w = k + 64 / HL_ROWS; w < PER; w += 64 / HL_ROWS) st.join(pm[w][r], ps[w][r]);
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) st.join(__shfl_xor(st.m, o), __shfl_xor(st.s, o));
-  if (lane == 0) {
-    int n = 0;
-    vp[wave] = row < T ? st.finish(row, V, zt, targets, lse, row_loss, n) : 0.f;
-    np[wave] = n;
-  }
+  for (int o = HL_ROWS; o < 64; o <<= 1) st.join(__shfl_xor(st.m, o), __shfl_xor(st.s, o));
+  int n = 0;
+  float v = 0.f;
+  if (lane < HL_ROWS && row < T) v = st.finish(row, V, zt, targets, lse, row_loss, n);
   if (gridDim.x > 1) return;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double v = 0.0;
-    int n = 0;
-    for (int w = 0; w < HL_WAVES; ++w) {
-      v += (double)vp[w];
-      n += np[w];
-    }
-    loss[0] = (float)(v / (double)max(n, 1));
+  double sum = (double)v;
+#pragma unroll
+  for (int o = 1; o < HL_ROWS; o <<= 1) {
+    sum += __shfl_xor(sum, o);
+    n += __shfl_xor(n, o);
   }
+  if (lane == 0) loss[0] = (float)(sum / (double)max(n, 1));
 }
 
 // One workgroup: loss = sum of row losses over the rows that have a target, in fp64 in a fixed order.
@@ -264,15 +237,10 @@ __global__ __launch_bounds__(256) void head_scatter_kernel(int64_t T, int H, con
 
 hipError_t head_rows(int64_t T, int V, int64_t blocks, const float* stats, const float* zt, const int32_t* targets,
                      float* lse, float* row_loss, float* loss, hipStream_t s) {
-  if (T <= HL_FEW) {
-    const unsigned grid = (unsigned)((T + HL_WAVES - 1) / HL_WAVES);
-    hipLaunchKernelGGL(head_rows_few_kernel, dim3(grid), dim3(HL_THREADS), 0, s, T, V, blocks, (const float2*)stats, zt,
-                       targets, lse, row_loss, loss);
-    if (grid == 1) return hipGetLastError();
-  } else {
-    hipLaunchKernelGGL(head_rows_kernel, dim3((unsigned)((T + HL_ROWS - 1) / HL_ROWS)), dim3(HL_THREADS), 0, s, T, V,
-                       blocks, (const float2*)stats, zt, targets, lse, row_loss);
-  }
+  const unsigned grid = (unsigned)((T + HL_ROWS - 1) / HL_ROWS);
+  hipLaunchKernelGGL(head_rows_kernel, dim3(grid), dim3(HL_THREADS), 0, s, T, V, blocks, (const float2*)stats, zt,
+                     targets, lse, row_loss, loss);
+  if (grid == 1) return hipGetLastError();
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(head_mean_kernel, dim3(1), dim3(HL_THREADS), 0, s, T, V, targets, row_loss, loss);

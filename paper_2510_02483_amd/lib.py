@@ -245,6 +245,11 @@ def _bytes(t) -> int:
     return t.numel() * t.element_size()
 
 
+def _need_int32(name, t, n):
+    if t.dtype != torch.int32 or t.numel() != n:
+        raise ValueError(f"{name} must hold {n} int32, not {t.numel()} {t.dtype}")
+
+
 def ls_packed_plan_bytes(c) -> int:
     cfg = make_packed_cfg(c)
     return lib().ls_packed_plan_bytes(ctypes.byref(cfg))
@@ -252,6 +257,7 @@ def ls_packed_plan_bytes(c) -> int:
 
 def ls_packed_plan(c, cu_seqlens, plan, stream=None):
     """cu_seqlens: n_seqs + 1 int32 on the device; plan: a uint8 buffer of ls_packed_plan_bytes(c)."""
+    _need_int32("cu_seqlens", cu_seqlens, c.n_seqs + 1)
     cfg = make_packed_cfg(c)
     _check(lib().ls_packed_plan(ctypes.byref(cfg), _p(cu_seqlens), _p(plan), _bytes(plan), _stream(stream)),
            "ls_packed_plan")
@@ -361,6 +367,7 @@ def ls_head_loss_workspace(tokens: int, hidden: int, vocab: int, piece: int = 0)
 
 def ls_head_loss_fwd(h, embed, targets, loss, row_loss, lse, workspace, stream=None):
     T, H = h.shape
+    _need_int32("targets", targets, T)
     _check(lib().ls_head_loss_fwd(T, H, embed.shape[0], _p(h), _p(embed), _p(targets), _p(loss), _p(row_loss), _p(lse),
                                   _p(workspace), _bytes(workspace), _stream(stream)), "ls_head_loss_fwd")
 
@@ -369,6 +376,7 @@ def ls_head_loss_bwd(h, embed, targets, lse, dloss, dh, d_embed, accumulate, wor
     """dloss: one fp32 or None (1); dh or d_embed may be None; d_embed: fp32, added to with
     ``accumulate``, or bf16, always overwritten."""
     T, H = h.shape
+    _need_int32("targets", targets, T)
     low = d_embed is not None and d_embed.dtype == torch.bfloat16
     if low and accumulate:
         raise ValueError("a bf16 d_embed is overwritten, never added to")

@@ -82,7 +82,7 @@ def check_fwd(x, r):
 
 # one token; fewer rows than a tile and a vocabulary of any size; the rows around a workgroup's 64; whole tiles;
 # more than one tile of every kind
-SHAPES = [(1, 64, 100), (1, 2048, 3001), (7, 72, 1003), (64, 128, 129), (65, 128, 5), (130, 256, 512), (257, 128, 2049),
+SHAPES = [(1, 64, 100), (1, 2048, 3001), (3, 8, 50), (33, 24, 7), (5, 16, 1), (17, 40, 65), (7, 72, 1003), (64, 128, 129), (65, 128, 5), (130, 256, 512), (257, 128, 2049),
           (300, 320, 5000), (1025, 64, 20003)]
 
 
@@ -121,6 +121,25 @@ def test_pieces(piece):
     x.bwd(x.de, piece=piece)
     within("dh", x.dh, r["dh"], r["tol_dh"])
     within("d_embed", x.de, r["de"], r["tol_de"])
+
+
+@pytest.mark.parametrize("bm,bn", [(256, 256), (256, 192), (192, 256), (192, 192)])
+def test_forced_tiles(bm, bn):
+    """Whatever tile shape is forced on the products, with the workspace of the automatic choice."""
+    need_gpu()
+    x = Head(300, 256, 5003, seed=35)
+    r = x.reference()
+    ws = x.workspace()
+    L.ls_gemm_tile_override(bm, bn)
+    try:
+        x.fwd(ws).bwd(x.de, ws=ws).bwd(x.low, dh=False, ws=ws)
+        torch.cuda.synchronize()
+    finally:
+        L.ls_gemm_tile_override(0, 0)
+    check_fwd(x, r)
+    within("dh", x.dh, r["dh"], r["tol_dh"])
+    within("d_embed", x.de, r["de"], r["tol_de"])
+    within("d_embed bf16", x.low, r["de"], r["tol_de"] * (1 + U) + U * r["de"].abs())
 
 
 def test_accumulate_and_wanted_outputs():

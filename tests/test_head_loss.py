@@ -50,9 +50,15 @@ def test_backward_refusals():
     assert bwd(dh=A) == ALIAS and bwd(de=2 * A) == ALIAS and bwd(de=None, low=6 * A) == ALIAS and bwd(dh=5 * A) == ALIAS
     assert bwd(dh=6 * A + 2) == ALIGN and bwd(dloss=5 * A + 4) == ALIGN
     assert bwd(n=need() // 2) == WORKSPACE
+    t = torch.zeros(1, dtype=torch.int32)
     with pytest.raises(ValueError):
-        L.ls_head_loss_bwd(torch.zeros(1, 8), torch.zeros(3, 8), None, None, None, None,
+        L.ls_head_loss_bwd(torch.zeros(1, 8), torch.zeros(3, 8), t, None, None, None,
                            torch.zeros(3, 8, dtype=torch.bfloat16), True, None)
+    for bad in (t.long(), torch.zeros(2, dtype=torch.int32)):  # read as int32, one per row
+        with pytest.raises(ValueError):
+            L.ls_head_loss_fwd(torch.zeros(1, 8), torch.zeros(3, 8), bad, None, None, None, None)
+        with pytest.raises(ValueError):
+            L.ls_head_loss_bwd(torch.zeros(1, 8), torch.zeros(3, 8), bad, None, None, None, None, False, None)
 
 
 def test_workspace_follows_the_piece():

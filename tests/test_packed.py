@@ -6,9 +6,11 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 import packed_ref as R
 from paper_2510_02483_amd import lib as L
+from paper_2510_02483_amd.configs import PackedConfig
 
 NULL, SHAPE, UNSUPPORTED, ALIGN, ALIAS, WORKSPACE = 1, 2, 3, 4, 5, 6
 BASE = 1 << 20  # addresses are compared, never followed, by a call that refuses
@@ -75,6 +77,15 @@ def test_null_alignment_alias_and_sizes():
     assert bwd(c, dout=None) == NULL and bwd(c, ws=None) == NULL and bwd(c, dqkv=BASE * 64) == ALIAS
     assert bwd(c, ws_bytes=L.lib().ls_packed_attn_bwd_workspace(ctypes.byref(c)) - 1) == WORKSPACE
     assert bwd(c, dqkv=BASE * 320 + 8) == ALIGN
+
+
+def test_lengths_of_another_type_or_number():
+    """The library reads n_seqs + 1 int32; what torch makes of a cumulative sum is int64."""
+    c = PackedConfig(300, 3, 4, 2, 64)
+    buf = torch.zeros(1 << 16, dtype=torch.uint8)
+    for bad in (torch.zeros(4, dtype=torch.int64), torch.zeros(3, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            L.ls_packed_plan(c, bad, buf)
 
 
 def test_plan_has_room_for_every_batch_of_its_total():
