@@ -317,7 +317,9 @@ int ls_attn_core_bwd_noalloc(const ls_block_cfg* cfg, const ls_bf16* qkv, const 
  * 2*n_kv_heads)*head_dim], o [total, n_q_heads*head_dim], lse [n_q_heads, total].
  * As there, NaN or infinities in a sequence's k and v may reach all rows of that
  * sequence (a masked probability is 0, and 0 x NaN is NaN); they reach no other.
- * They may exceed 2 GiB.  head_dim is 64 or 128; total and n_seqs < 2^28, total x
+ * They may exceed 2 GiB.  head_dim is 64 or a multiple of 8 from 72 to 128 (heads
+ * between 64 and 128 are stored as they are and cost what heads of 128 do in the
+ * attention); total and n_seqs < 2^28, total x
  * n_q_heads < 2^31 and a row of qkv holds less than 2^20 features. */
 typedef struct {
   int64_t total;

@@ -1081,8 +1081,9 @@ static int check_packed_cfg(const ls_packed_cfg* c, ls::PackedShape& p) {
     return fail(LS_ERR_SHAPE, "all sizes must be positive");
   if (c->n_q_heads % c->n_kv_heads != 0)
     return fail(LS_ERR_SHAPE, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", c->n_q_heads, c->n_kv_heads);
-  if (c->head_dim != 64 && c->head_dim != 128)
-    return fail(LS_ERR_UNSUPPORTED, "packed sequences take head_dim 64 or 128 (got %d)", c->head_dim);
+  if (c->head_dim != 64 && !(c->head_dim > 64 && c->head_dim <= 128 && c->head_dim % 8 == 0))
+    return fail(LS_ERR_UNSUPPORTED, "head_dim %d is not supported (64, or a multiple of 8 from 72 to 128)",
+                c->head_dim);
   // rows and positions are 32-bit, a row's byte offset inside a 64-row tile too, and
   // there is a workgroup per tile and head
   if (c->total >= (int64_t)1 << 28) return fail(LS_ERR_SHAPE, "total (%lld) reaches 2^28", (long long)c->total);

@@ -84,18 +84,18 @@ LS_DEV int tile_swz(int r) {
 // byte offsets of the wave's share are computed once, for every tile of a
 // loop; a tile only moves the scalar resource, whose base is the tile's first
 // element and whose end is row `rows` (the tile's columns lie within a row:
-// col0 + D <= ld).
+// col0 + width <= ld).  Columns at or past `width`, a multiple of 8, read as zero.
 template <int D, int ROWS>
 struct TileLoader {
   static constexpr int CPR = D / 8, RPI = 64 / CPR, PER = ROWS / RPI / 4;
   static_assert(PER == 2 || PER == 4, "loads split evenly over 4 waves in groups of 2 or 4");
   uint32_t off[PER];
-  LS_DEV TileLoader(int64_t ld, int wave, int lane) {
+  LS_DEV TileLoader(int64_t ld, int wave, int lane, int width = D) {
 #pragma unroll
     for (int jj = 0; jj < PER; ++jj) {
       const int rr = (wave * PER + jj) * RPI + lane / CPR;
       const int c = (lane % CPR) ^ tile_swz<D>(rr);
-      off[jj] = ((uint32_t)rr * (uint32_t)ld + (uint32_t)(8 * c)) * 2u;
+      off[jj] = 8 * c < width ? ((uint32_t)rr * (uint32_t)ld + (uint32_t)(8 * c)) * 2u : LS_OOB;
     }
   }
   LS_DEV void operator()(const bf16_t* m, int64_t ld, int row0, int rows, int col0, bf16_t* t, int wave) const {
@@ -226,10 +226,18 @@ LS_DEV void put_rows(bf16_t* t, const u32x4 (&f)[D / 16], int lr, int lh) {
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) *(u32x4*)(t + lr * D + 8 * ((2 * s + lh) ^ tile_swz<D>(lr))) = f[s];
 }
+// A sequence's rows as a buffer (rows past the sequence read as zero), and the
+// operands of 32 of them: `off` is the byte offset of the lane's row and first
+// feature; features at or past `width` read as zero.  Without branches, so that the
+// loads of all operands are in flight together.
+LS_DEV __amdgpu_buffer_rsrc_t seq_rows(const bf16_t* m, const PackedTile& t, int64_t ld) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(m + t.start * ld), 0, (int)(t.len * ld * 2), 0x00020000);
+}
 template <int D>
-LS_DEV void get_rows(u32x4 (&f)[D / 16], const bf16_t* row, bool ok, int lh) {
+LS_DEV void get_rows(u32x4 (&f)[D / 16], __amdgpu_buffer_rsrc_t r, uint32_t off, int lh, int width) {
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) f[s] = ok ? load16(row + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
+  for (int s = 0; s < D / 16; ++s)
+    f[s] = __builtin_amdgcn_raw_buffer_load_b128(r, 16 * s + 8 * lh < width ? off + 32 * s + 16 * lh : LS_OOB, 0, 0);
 }
 // Orders a wave's own LDS writes before its later reads (the LDS serves a wave's accesses in order).
 LS_DEV void wave_lds_order() {
@@ -246,23 +254,24 @@ LS_DEV void wave_lds_order() {
 template <int D, int NB>
 LS_DEV void short_fwd(const AttnShape& sh, const PackedTile& t, int h, const bf16_t* __restrict__ qkv,
                       bf16_t* __restrict__ o, float* __restrict__ lse, float sl2, bf16_t* vt) {
-  const int nq = sh.nq, nkv = sh.nkv, kvh = h / (nq / nkv);
+  const int nq = sh.nq, nkv = sh.nkv, kvh = h / (nq / nkv), hd = sh.d;
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
-  const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
-  auto row = [&](int b) { return qkv + (t.start + (int64_t)min(32 * b + lr, t.len - 1)) * ld; };
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * hd;
+  const __amdgpu_buffer_rsrc_t rows = seq_rows(qkv, t, ld);
+  auto at = [&](int b, int head) { return (uint32_t)((32 * b + lr) * (int)ld + head * hd) * 2u; };
   u32x4 qf[D / 16], kf[NB][D / 16];
-  get_rows<D>(qf, row(0) + h * D, lr < t.len, lh);
+  get_rows<D>(qf, rows, at(0, h), lh, hd);
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     u32x4 vf[D / 16];
-    get_rows<D>(kf[b], row(b) + (nq + kvh) * D, 32 * b + lr < t.len, lh);
-    get_rows<D>(vf, row(b) + (nq + nkv + kvh) * D, 32 * b + lr < t.len, lh);
+    get_rows<D>(kf[b], rows, at(b, nq + kvh), lh, hd);
+    get_rows<D>(vf, rows, at(b, nq + nkv + kvh), lh, hd);
     put_rows<D>(vt + 32 * b * D, vf, lr, lh);
   }
   wave_lds_order();
 #pragma unroll
   for (int qb = 0; qb < NB; ++qb) {
-    if (qb > 0) get_rows<D>(qf, row(qb) + h * D, 32 * qb + lr < t.len, lh);
+    if (qb > 0) get_rows<D>(qf, rows, at(qb, h), lh, hd);
     f32x16 s[NB];
     float mx = -INFINITY;
     // lane holds query 32qb + lr, keys 32b + 8(r/4) + 4lh + r%4
@@ -299,19 +308,20 @@ LS_DEV void short_fwd(const AttnShape& sh, const PackedTile& t, int h, const bf1
     const float l = halves_sum(sum);
     if (32 * qb + lr >= t.len) continue;
     const float inv = 1.0f / l;
-    bf16_t* orow = o + (t.start + (int64_t)(32 * qb + lr)) * nq * D + h * D;
+    bf16_t* orow = o + (t.start + (int64_t)(32 * qb + lr)) * nq * hd + h * hd;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int rq = 0; rq < 4; ++rq)
-        *(u32x2*)(orow + 32 * i + 8 * rq + 4 * lh) = u32x2{pack_bf2(oacc[i][4 * rq] * inv, oacc[i][4 * rq + 1] * inv),
-                                                           pack_bf2(oacc[i][4 * rq + 2] * inv, oacc[i][4 * rq + 3] * inv)};
+        if (32 * i + 8 * rq + 4 * lh < hd)
+          *(u32x2*)(orow + 32 * i + 8 * rq + 4 * lh) = u32x2{pack_bf2(oacc[i][4 * rq] * inv, oacc[i][4 * rq + 1] * inv),
+                                                             pack_bf2(oacc[i][4 * rq + 2] * inv, oacc[i][4 * rq + 3] * inv)};
     if (lh == 0) lse[(int64_t)h * sh.seq + t.start + 32 * qb + lr] = (m + log2f(l)) * LN2;
   }
 }
 
 template <int D, bool PACKED>
-__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, PackedView pk, const bf16_t* __restrict__ qkv,
+__global__ __launch_bounds__(256, PACKED && D == 64 ? 4 : 2) void attn_fwd_kernel(AttnShape sh, PackedView pk, const bf16_t* __restrict__ qkv,
                                                            bf16_t* __restrict__ o, float* __restrict__ lse,
                                                            float sl2) {
   __shared__ __attribute__((aligned(1024))) bf16_t Ks[2][BKV * D];
@@ -339,19 +349,19 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, PackedVi
   } else {
     qtile = q_tile(sh);
   }
-  const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv);
-  const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
+  const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv), hd = PACKED ? sh.d : D;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * hd;
   const bf16_t* base = qkv + qtile.row0 * ld;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 31, lh = lane >> 5;
   const int q0 = qtile.qt * BQ;
   const int qrow = q0 + 32 * wave + lr;
   const int wave_qmin = q0 + 32 * wave, wave_qmax = wave_qmin + 31;
-  const int kcol = (nq + kvh) * D, vcol = (nq + nkv + kvh) * D;
+  const int kcol = (nq + kvh) * hd, vcol = (nq + nkv + kvh) * hd;
 
   const int kv_end = min(S, q0 + BQ);
   const int nkt = (kv_end + BKV - 1) / BKV;
 
-  const TileLoader<D, BKV> tl(ld, wave, lane);
+  const TileLoader<D, BKV> tl(ld, wave, lane, hd);
   auto load_kv = [&](int kv0, bf16_t* kt, bf16_t* vt) {
     tl(base, ld, kv0, S, kcol, kt, wave);
     tl(base, ld, kv0, S, vcol, vt, wave);
@@ -361,7 +371,8 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, PackedVi
   u32x4 qf[D / 16];
 #pragma unroll
   for (int s = 0; s < D / 16; ++s)
-    qf[s] = qrow < S ? load16(base + (int64_t)qrow * ld + h * D + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
+    qf[s] = qrow < S && 16 * s + 8 * lh < hd ? load16(base + (int64_t)qrow * ld + h * hd + 16 * s + 8 * lh)
+                                             : u32x4{0u, 0u, 0u, 0u};
 
   f32x16 oacc[D / 32];
 #pragma unroll
@@ -442,12 +453,13 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, PackedVi
 
   if (qrow < S) {
     const float inv = 1.0f / l;
-    bf16_t* orow = o + (qtile.row0 + qrow) * nq * D + h * D;
+    bf16_t* orow = o + (qtile.row0 + qrow) * nq * hd + h * hd;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int rq = 0; rq < 4; ++rq) {
         const int d = 32 * i + 8 * rq + 4 * lh;
+        if (PACKED && d >= hd) continue;
         *(u32x2*)(orow + d) = u32x2{pack_bf2(oacc[i][4 * rq] * inv, oacc[i][4 * rq + 1] * inv),
                                     pack_bf2(oacc[i][4 * rq + 2] * inv, oacc[i][4 * rq + 3] * inv)};
       }
@@ -455,9 +467,32 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnShape sh, PackedVi
   }
 }
 
+// attn_bwd_pre_kernel for one row of packed sequences and heads of any width: D / 8 lanes a head.
+template <int D>
+LS_DEV void bwd_pre_row(const AttnShape& sh, const bf16_t* __restrict__ orow, const bf16_t* __restrict__ drow,
+                        const float* __restrict__ lse, float* __restrict__ Dv, float* __restrict__ lse2, int64_t t) {
+  constexpr int CPH = D / 8;
+  const int lane = threadIdx.x & 63, c = lane % CPH;
+  for (int h = lane / CPH; h - lane / CPH < sh.nq; h += 64 / CPH) {
+    float acc = 0.f;
+    if (h < sh.nq && 8 * c < sh.d) {
+      const u32x4 a = load16(orow + h * sh.d + 8 * c), g = load16(drow + h * sh.d + 8 * c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc += bf_lo(a[e]) * bf_lo(g[e]) + bf_hi(a[e]) * bf_hi(g[e]);
+    }
+#pragma unroll
+    for (int off = CPH / 2; off >= 1; off >>= 1) acc += __shfl_xor(acc, off);
+    if (c == 0 && h < sh.nq) {
+      const int64_t i = (int64_t)h * sh.seq + t;
+      Dv[i] = acc;
+      lse2[i] = lse[i] * LOG2E;
+    }
+  }
+}
+
 // D[b,h,s] = <dO, O> over the head's d columns (fp32), and the log-sum-exp in
 // base 2 (lse * log2(e)), the form the backward kernels subtract.
-template <int D>
+template <int D, bool PACKED>
 __global__ __launch_bounds__(256) void attn_bwd_pre_kernel(AttnShape sh, const bf16_t* __restrict__ o,
                                                            const bf16_t* __restrict__ dout,
                                                            const float* __restrict__ lse, float* __restrict__ Dv,
@@ -466,6 +501,10 @@ __global__ __launch_bounds__(256) void attn_bwd_pre_kernel(AttnShape sh, const b
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= (int64_t)sh.batch * sh.seq) return;
+  if constexpr (PACKED) {
+    bwd_pre_row<D>(sh, o + t * sh.nq * sh.d, dout + t * sh.nq * sh.d, lse, Dv, lse2, t);
+    return;
+  }
   const int b = (int)(t / sh.seq), s = (int)(t % sh.seq);
   const int chunks = sh.nq * CPH;
   const bf16_t* orow = o + t * sh.nq * D;
@@ -491,19 +530,25 @@ __global__ __launch_bounds__(256) void attn_bwd_pre_kernel(AttnShape sh, const b
 // Inverse rotation of a gradient held in MFMA layout: lane holds columns
 // 32i + 8(r/4) + 4lh + r%4 of one row at position `pos`; the pair partner of
 // column d < D/2 is d + D/2, in register block i + D/64 of the same lane.
+// Without rotation (rope_cs null) only columns below `width` are stored.
 template <int D>
 LS_DEV void unrotate_store(const f32x16 (&acc)[D / 32], float scale, const float* rope_cs, int seq, int pos, int lh,
-                           bf16_t* row) {
+                           bf16_t* row, int width = D) {
   constexpr int HALF = D / 2, IP = HALF / 32;
   if (rope_cs == nullptr) {
+    auto store = [&](bool whole) {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+      for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-      for (int rq = 0; rq < 4; ++rq) {
-        const int d = 32 * i + 8 * rq + 4 * lh;
-        *(u32x2*)(row + d) = u32x2{pack_bf2(acc[i][4 * rq] * scale, acc[i][4 * rq + 1] * scale),
-                                   pack_bf2(acc[i][4 * rq + 2] * scale, acc[i][4 * rq + 3] * scale)};
-      }
+        for (int rq = 0; rq < 4; ++rq) {
+          const int d = 32 * i + 8 * rq + 4 * lh;
+          if (!whole && d >= width) continue;
+          *(u32x2*)(row + d) = u32x2{pack_bf2(acc[i][4 * rq] * scale, acc[i][4 * rq + 1] * scale),
+                                     pack_bf2(acc[i][4 * rq + 2] * scale, acc[i][4 * rq + 3] * scale)};
+        }
+    };
+    if (width == D) store(true);
+    else store(false);
     return;
   }
   // cos and sin of the lane's angle indices (4 consecutive ones per 8-column
@@ -555,22 +600,24 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const b
                       const bf16_t* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ Dv,
                       bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds) {
   constexpr int NSD = D / 16, NI = D / 32;
-  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv);
+  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv), hd = sh.d;
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
-  const int64_t ld = (int64_t)(nq + 2 * nkv) * D, ldo = (int64_t)nq * D;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * hd, ldo = (int64_t)nq * hd;
   const bool ok = lr < t.len;
   const int64_t r0 = t.start + (int64_t)(ok ? lr : 0);
   bf16_t *kt = (bf16_t*)lds, *qt = kt + PACKED_SHORT * D, *ot = qt + PACKED_SHORT * D;
   float *lv = (float*)(ot + PACKED_SHORT * D), *dvv = lv + PACKED_SHORT;
   u32x4 kf[NSD], vf[NSD], qf[NSD], of[NSD];
-  get_rows<D>(kf, qkv + r0 * ld + (nq + kvh) * D, ok, lh);
-  get_rows<D>(vf, qkv + r0 * ld + (nq + nkv + kvh) * D, ok, lh);
+  const __amdgpu_buffer_rsrc_t rows = seq_rows(qkv, t, ld), drows = seq_rows(dout, t, ldo);
+  auto at = [&](int r, int64_t ldr, int head) { return (uint32_t)(r * (int)ldr + head * hd) * 2u; };
+  get_rows<D>(kf, rows, at(lr, ld, nq + kvh), lh, hd);
+  get_rows<D>(vf, rows, at(lr, ld, nq + nkv + kvh), lh, hd);
   f32x16 dk[NI], dv[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) dk[i] = dv[i] = f32x16{};
   for (int h = hq0; h < hq0 + nq / nkv; ++h) {
-    get_rows<D>(qf, qkv + r0 * ld + h * D, ok, lh);
-    get_rows<D>(of, dout + r0 * ldo + h * D, ok, lh);
+    get_rows<D>(qf, rows, at(lr, ld, h), lh, hd);
+    get_rows<D>(of, drows, at(lr, ldo, h), lh, hd);
     const int64_t v0 = (int64_t)h * sh.seq + t.start;
     const float L = ok ? lse2[v0 + lr] : 0.f, Dr = ok ? Dv[v0 + lr] : 0.f;
     if (h == hq0) put_rows<D>(kt, kf, lr, lh);
@@ -630,13 +677,13 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const b
 #pragma unroll
         for (int i = 0; i < NI; ++i) dq[i] = mfma32(colt_frag<D>(kt, 32 * i, c, lane), sf, dq[i]);
       }
-      if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * D);
+      if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * hd, hd);
     }
     wave_lds_order();
   }
   if (!ok) return;
-  unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * D);
-  unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * D);
+  unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * hd, hd);
+  unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * hd, hd);
 }
 
 // The same for a middle sequence, of up to 64 rows, by a pair of waves: wave j of the
@@ -653,23 +700,25 @@ LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf1
                     const bf16_t* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ Dv,
                     bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds) {
   constexpr int NSD = D / 16, NI = D / 32;
-  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv);
+  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv), hd = sh.d;
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
   const int j = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) & 1, row = 32 * j + lr;
-  const int64_t ld = (int64_t)(nq + 2 * nkv) * D, ldo = (int64_t)nq * D;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * hd, ldo = (int64_t)nq * hd;
   const bool ok = row < t.len;
   const int64_t r0 = t.start + (int64_t)(ok ? row : 0);
   bf16_t *kt = (bf16_t*)lds, *qt = kt + PACKED_MID * D, *ot = qt + PACKED_MID * D;
   float *lv = (float*)(ot + PACKED_MID * D), *dvv = lv + PACKED_MID;
   u32x4 kf[NSD], vf[NSD], qf[NSD], of[NSD];
-  get_rows<D>(kf, qkv + r0 * ld + (nq + kvh) * D, ok, lh);
-  get_rows<D>(vf, qkv + r0 * ld + (nq + nkv + kvh) * D, ok, lh);
+  const __amdgpu_buffer_rsrc_t rows = seq_rows(qkv, t, ld), drows = seq_rows(dout, t, ldo);
+  auto at = [&](int r, int64_t ldr, int head) { return (uint32_t)(r * (int)ldr + head * hd) * 2u; };
+  get_rows<D>(kf, rows, at(row, ld, nq + kvh), lh, hd);
+  get_rows<D>(vf, rows, at(row, ld, nq + nkv + kvh), lh, hd);
   f32x16 dk[NI], dv[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) dk[i] = dv[i] = f32x16{};
   for (int h = hq0; h < hq0 + nq / nkv; ++h) {
-    get_rows<D>(qf, qkv + r0 * ld + h * D, ok, lh);
-    get_rows<D>(of, dout + r0 * ldo + h * D, ok, lh);
+    get_rows<D>(qf, rows, at(row, ld, h), lh, hd);
+    get_rows<D>(of, drows, at(row, ldo, h), lh, hd);
     const int64_t v = (int64_t)h * sh.seq + t.start;
     const float L = ok ? lse2[v + row] : 0.f, Dr = ok ? Dv[v + row] : 0.f;
     if (h > hq0) sync_lds();  // the tiles of the head before are read
@@ -723,7 +772,7 @@ LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf1
         for (int c = 0; c < NSD; ++c) p = mfma32(vf[c], of[c], p);
       } else {  // (a middle sequence has all of its first 32 rows)
         u32x4 v0[NSD];
-        get_rows<D>(v0, qkv + (t.start + (int64_t)lr) * ld + (nq + nkv + kvh) * D, lr < t.len, lh);
+        get_rows<D>(v0, rows, at(lr, ld, nq + nkv + kvh), lh, hd);
 #pragma unroll
         for (int c = 0; c < NSD; ++c) p = mfma32(v0[c], of[c], p);
       }
@@ -742,11 +791,11 @@ LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf1
         for (int i = 0; i < NI; ++i) dq[i] = mfma32(colt_frag<D>(kt + 32 * b * D, 32 * i, c, lane), sf, dq[i]);
       }
     }
-    if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * D);
+    if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * hd, hd);
   }
   if (!ok) return;
-  unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * D);
-  unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * D);
+  unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * hd, hd);
+  unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * hd, hd);
 }
 
 // dK and dV for 128 keys of one kv head (4 waves x 32 keys), summed over the
@@ -827,8 +876,9 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_
     S = t.len;
     row0 = vec0 = t.start;
   }
-  const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
-  const int64_t ldo = (int64_t)nq * D;
+  const int hd = PACKED ? sh.d : D;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * hd;
+  const int64_t ldo = (int64_t)nq * hd;
   const bf16_t* base = qkv + row0 * ld;
   const bf16_t* dbase = dout + row0 * ldo;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -847,11 +897,11 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_
       if (tbegin == ntiles) --tbegin;  // (no part is empty: a plan has at most a part per PACKED_STEPS tiles)
     }
   }
-  const TileLoader<D, BWD_BQ> tlq(ld, wave, lane), tlo(ldo, wave, lane);
+  const TileLoader<D, BWD_BQ> tlq(ld, wave, lane, hd), tlo(ldo, wave, lane, hd);
   auto issue = [&](int t, int st) {
     const int h = kvh * G + hs * Gs + t / nqt, q0 = q_begin + (t % nqt) * BWD_BQ;
-    tlq(base, ld, q0, S, h * D, stg[st].q, wave);
-    tlo(dbase, ldo, q0, S, h * D, stg[st].o, wave);
+    tlq(base, ld, q0, S, h * hd, stg[st].q, wave);
+    tlo(dbase, ldo, q0, S, h * hd, stg[st].o, wave);
     const int64_t v0 = vec0 + (int64_t)h * sh.seq;
     if (wave == 0) load_vec64(rsrc(lse2 + v0, (uint32_t)S * 4), q0, S, stg[st].l, lane);
     if (wave == 1) load_vec64(rsrc(Dv + v0, (uint32_t)S * 4), q0, S, stg[st].d, lane);
@@ -862,9 +912,9 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_
   u32x4 kf[NSD], vf[NSD];
 #pragma unroll
   for (int s = 0; s < NSD; ++s) {
-    const bool ok = kvrow < S;
-    kf[s] = ok ? load16(base + (int64_t)kvrow * ld + (nq + kvh) * D + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
-    vf[s] = ok ? load16(base + (int64_t)kvrow * ld + (nq + nkv + kvh) * D + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
+    const bool ok = kvrow < S && 16 * s + 8 * lh < hd;
+    kf[s] = ok ? load16(base + (int64_t)kvrow * ld + (nq + kvh) * hd + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
+    vf[s] = ok ? load16(base + (int64_t)kvrow * ld + (nq + nkv + kvh) * hd + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
   }
 
   f32x16 dk[NI], dv[NI];
@@ -988,8 +1038,8 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_
         *(f32x4*)(row + D + c) = f32x4{dv[i][4 * rq], dv[i][4 * rq + 1], dv[i][4 * rq + 2], dv[i][4 * rq + 3]};
       }
   } else {
-    unrotate_store<D>(dk, scale, rope_cs, S, kvrow, lh, dqkv + (row0 + kvrow) * ld + (nq + kvh) * D);
-    unrotate_store<D>(dv, 1.0f, nullptr, S, kvrow, lh, dqkv + (row0 + kvrow) * ld + (nq + nkv + kvh) * D);
+    unrotate_store<D>(dk, scale, rope_cs, S, kvrow, lh, dqkv + (row0 + kvrow) * ld + (nq + kvh) * hd, hd);
+    unrotate_store<D>(dv, 1.0f, nullptr, S, kvrow, lh, dqkv + (row0 + kvrow) * ld + (nq + nkv + kvh) * hd, hd);
   }
 }
 
@@ -1009,11 +1059,13 @@ LS_DEV void join_parts(const AttnShape& sh, const PackedView& pk, int tile, int 
   const int kv0 = ((t.len - 1) / BWD_BKV - t.rank) * BWD_BKV;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = E * lane;
   typedef float fE __attribute__((ext_vector_type(E)));
-  const int64_t ld = (int64_t)(sh.nq + 2 * nkv) * D, step = (int64_t)nkv * (PACKED_ROWS * 2 * D);
+  const int hd = sh.d;
+  const int64_t ld = (int64_t)(sh.nq + 2 * nkv) * hd, step = (int64_t)nkv * (PACKED_ROWS * 2 * D);
   const bool is_k = c0 < D;
+  const int col = is_k ? c0 : c0 - D;
   const float c = is_k ? scale : 1.0f;
   const float* src = part + ((int64_t)slot * nkv + kvh) * (PACKED_ROWS * 2 * D) + c0;
-  bf16_t* dst = dqkv + (t.start + (int64_t)kv0) * ld + (int64_t)(sh.nq + (is_k ? 0 : nkv) + kvh) * D + (is_k ? c0 : c0 - D);
+  bf16_t* dst = dqkv + (t.start + (int64_t)kv0) * ld + (int64_t)(sh.nq + (is_k ? 0 : nkv) + kvh) * hd + col;
   for (int r0 = ROWS * wave; r0 < BWD_BKV && kv0 + r0 < t.len; r0 += 4 * ROWS) {
     fE v[ROWS];
 #pragma unroll
@@ -1024,7 +1076,7 @@ LS_DEV void join_parts(const AttnShape& sh, const PackedView& pk, int tile, int 
       for (int k = 0; k < ROWS; ++k) v[k] += *(const fE*)(src + p * step + (r0 + k) * (2 * D));
 #pragma unroll
     for (int k = 0; k < ROWS; ++k) {
-      if (kv0 + r0 + k >= t.len) break;
+      if (kv0 + r0 + k >= t.len || col >= hd) break;
       bf16_t* y = dst + (r0 + k) * ld;
       if constexpr (E == 4) *(u32x2*)y = u32x2{pack_bf2(v[k][0] * c, v[k][1] * c), pack_bf2(v[k][2] * c, v[k][3] * c)};
       else *(uint32_t*)y = pack_bf2(v[k][0] * c, v[k][1] * c);
@@ -1135,28 +1187,29 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, Packe
   } else {
     qtile = q_tile(sh);
   }
-  const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv);
-  const int64_t ld = (int64_t)(nq + 2 * nkv) * D;
-  const int64_t ldo = (int64_t)nq * D;
+  const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv), hd = PACKED ? sh.d : D;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * hd;
+  const int64_t ldo = (int64_t)nq * hd;
   const bf16_t* base = qkv + qtile.row0 * ld;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
   const int q0 = qtile.qt * BQ;
   const int qrow = q0 + 32 * wave + lr;
   const bool qok = qrow < S;
-  const int kcol = (nq + kvh) * D, vcol = (nq + nkv + kvh) * D;
+  const int kcol = (nq + kvh) * hd, vcol = (nq + nkv + kvh) * hd;
 
   const int kv_end = min(S, q0 + BQ);
   const int nkt = (kv_end + BKV - 1) / BKV;
-  const TileLoader<D, BKV> tl(ld, wave, lane);
+  const TileLoader<D, BKV> tl(ld, wave, lane, hd);
   tl(base, ld, 0, S, kcol, Ks[0], wave);
   tl(base, ld, 0, S, vcol, Vs[0], wave);
 
   u32x4 qf[NSD], df[NSD];
 #pragma unroll
   for (int s = 0; s < NSD; ++s) {
-    qf[s] = qok ? load16(base + (int64_t)qrow * ld + h * D + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
-    df[s] = qok ? load16(dout + (qtile.row0 + qrow) * ldo + h * D + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
+    const bool ok = qok && 16 * s + 8 * lh < hd;
+    qf[s] = ok ? load16(base + (int64_t)qrow * ld + h * hd + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
+    df[s] = ok ? load16(dout + (qtile.row0 + qrow) * ldo + h * hd + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
   }
   const float L2 = qok ? lse2[qtile.vec0 + qrow] : 0.f;
   const float Dq = qok ? Dv[qtile.vec0 + qrow] : 0.f;
@@ -1245,7 +1298,7 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, Packe
     if (kt + 1 < nkt) step(std::integral_constant<int, 1>{}, kt + 1);
   }
   if (!qok) return;
-  unrotate_store<D>(dq, scale, rope_cs, S, qrow, lh, dqkv + (qtile.row0 + qrow) * ld + h * D);
+  unrotate_store<D>(dq, scale, rope_cs, S, qrow, lh, dqkv + (qtile.row0 + qrow) * ld + h * hd, hd);
 }
 
 template <int D, bool PACKED>
@@ -1253,7 +1306,7 @@ hipError_t attn_fwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* q
                       hipStream_t s) {
   const unsigned grid = PACKED ? (unsigned)pk.max_units * sh.nq
                                : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
-  const float sl2 = LOG2E / sqrtf((float)(sh.d_scale > 0 ? sh.d_scale : D));
+  const float sl2 = LOG2E / sqrtf((float)(PACKED ? sh.d : sh.d_scale > 0 ? sh.d_scale : D));
   hipLaunchKernelGGL((attn_fwd_kernel<D, PACKED>), dim3(grid), dim3(256), 0, s, sh, pk, qkv, o, lse, sl2);
   return hipGetLastError();
 }
@@ -1280,7 +1333,7 @@ hipError_t attn_bwd_t(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, c
   const int64_t T = (int64_t)sh.batch * sh.seq;
   float* Dv = (float*)ws;
   float* lse2 = Dv + T * sh.nq;
-  hipLaunchKernelGGL((attn_bwd_pre_kernel<D>), dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, sh, o, dout, lse, Dv,
+  hipLaunchKernelGGL((attn_bwd_pre_kernel<D, false>), dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, sh, o, dout, lse, Dv,
                      lse2);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -1317,11 +1370,11 @@ hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf
   float* Dv = (float*)ws;
   float* lse2 = Dv + T * sh.nq;
   float* part = (float*)((char*)ws + bwd_ws_head(sh));
-  hipLaunchKernelGGL((attn_bwd_pre_kernel<D>), dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, sh, o, dout, lse, Dv,
+  hipLaunchKernelGGL((attn_bwd_pre_kernel<D, true>), dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, sh, o, dout, lse, Dv,
                      lse2);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const float scale = 1.0f / sqrtf((float)D);
+  const float scale = 1.0f / sqrtf((float)sh.d);
   const unsigned gkv = (unsigned)(pk.max_units + pk.max_items - pk.max_tiles) * sh.nkv;
   hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, true>), dim3(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
                      (const float*)lse2, (const float*)Dv, dqkv, (const float*)nullptr, scale, scale * LOG2E, 1, part);
@@ -1361,22 +1414,21 @@ hipError_t attn_bwd(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, con
 hipError_t packed_attn_fwd(const PackedShape& p, const void* plan, const bf16_t* qkv, bf16_t* o, float* lse,
                            hipStream_t s) {
   const AttnShape sh = packed_shape(p);
-  if (p.d == 128) return attn_fwd_t<128, true>(sh, packed_view(p, plan), qkv, o, lse, s);
   if (p.d == 64) return attn_fwd_t<64, true>(sh, packed_view(p, plan), qkv, o, lse, s);
-  return hipErrorInvalidValue;
+  return attn_fwd_t<128, true>(sh, packed_view(p, plan), qkv, o, lse, s);
 }
 
 size_t packed_attn_bwd_workspace(const PackedShape& p) {
   // D and the base-2 log-sum-exp of every row and head, then the slots of partial dK | dV
-  return (size_t)(bwd_ws_head(packed_shape(p)) + packed_layout(p).max_slots * p.nkv * PACKED_ROWS * 2 * p.d * 4);
+  return (size_t)(bwd_ws_head(packed_shape(p)) + packed_layout(p).max_slots * p.nkv * PACKED_ROWS * 2 *
+                                                   (p.d == 64 ? 64 : 128) * 4);
 }
 
 hipError_t packed_attn_bwd(const PackedShape& p, const void* plan, const bf16_t* qkv, const bf16_t* o, const float* lse,
                            const bf16_t* dout, bf16_t* dqkv, void* ws, hipStream_t s) {
   const AttnShape sh = packed_shape(p);
-  if (p.d == 128) return packed_attn_bwd_t<128>(sh, packed_view(p, plan), qkv, o, lse, dout, dqkv, ws, s);
   if (p.d == 64) return packed_attn_bwd_t<64>(sh, packed_view(p, plan), qkv, o, lse, dout, dqkv, ws, s);
-  return hipErrorInvalidValue;
+  return packed_attn_bwd_t<128>(sh, packed_view(p, plan), qkv, o, lse, dout, dqkv, ws, s);
 }
 
 }  // namespace ls

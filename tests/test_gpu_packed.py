@@ -78,7 +78,7 @@ LENGTHS = {
 }
 
 
-@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (2, 2, 128), (6, 1, 64), (3, 1, 128)])
+@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (2, 2, 128), (6, 1, 64), (3, 1, 128), (4, 2, 104), (1, 1, 72)])
 @pytest.mark.parametrize("lens", LENGTHS, ids=list(LENGTHS))
 def test_attention_matches_the_reference(lens, nq, nkv, d):
     need_gpu()
@@ -136,7 +136,7 @@ def test_neighbours_do_not_matter():
 
 
 @pytest.mark.parametrize("inverse", [False, True])
-@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (24, 8, 128), (3, 3, 128)])
+@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (24, 8, 128), (3, 3, 128), (7, 7, 104), (5, 1, 72), (2, 1, 80)])
 def test_rope(nq, nkv, d, inverse):
     need_gpu()
     b = Batch([50, 0, 1, 333], nq, nkv, d, first=2, tail=5, seed=11)
@@ -176,7 +176,7 @@ def test_rope_far_positions():
         assert np.all(np.abs(got[:, 64 * h:64 * h + 32] - ref) <= R.U * np.abs(ref) * 1.01 + 2.0 ** -21 * (abs(lo) + abs(hi)))
 
 
-@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (2, 2, 128), (8, 1, 128)])
+@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (2, 2, 128), (8, 1, 128), (5, 1, 120)])
 def test_one_long_sequence_among_others(nq, nkv, d):
     """The dK/dV work of the long sequence's first keys is cut into parts."""
     need_gpu()

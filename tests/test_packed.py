@@ -48,7 +48,7 @@ CALLS = (plan, rope, fwd, bwd)
 @pytest.mark.parametrize("call", CALLS)
 @pytest.mark.parametrize("bad,status", [
     (dict(total=0), SHAPE), (dict(total=-5), SHAPE), (dict(n_seqs=0), SHAPE), (dict(nq=0), SHAPE), (dict(nkv=0), SHAPE),
-    (dict(nq=3, nkv=2), SHAPE), (dict(d=104), UNSUPPORTED), (dict(d=32), UNSUPPORTED), (dict(d=0), SHAPE),
+    (dict(nq=3, nkv=2), SHAPE), (dict(d=100), UNSUPPORTED), (dict(d=32), UNSUPPORTED), (dict(d=136), UNSUPPORTED), (dict(d=0), SHAPE),
     (dict(total=1 << 28), SHAPE), (dict(n_seqs=1 << 28), SHAPE), (dict(total=(1 << 28) - 1, nq=16, nkv=8), SHAPE), (dict(nq=1 << 14, nkv=1), SHAPE),
 ])
 def test_shapes_refused(call, bad, status):
@@ -100,7 +100,7 @@ def test_plan_has_room_for_every_batch_of_its_total():
         tiles = int(((lens + 127) // 128).sum())
         c = cfg(total=total, n_seqs=n)
         assert L.lib().ls_packed_plan_bytes(ctypes.byref(c)) >= 16 * tiles + 4 * total
-    assert L.lib().ls_packed_plan_bytes(ctypes.byref(cfg(d=72))) == 0
+    assert L.lib().ls_packed_plan_bytes(ctypes.byref(cfg(d=56))) == 0
     assert L.lib().ls_packed_attn_bwd_workspace(ctypes.byref(cfg(total=0))) == 0
 
 
