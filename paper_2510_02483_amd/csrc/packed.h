@@ -1,7 +1,7 @@
 // The plan of a batch of packed sequences, as the kernels read it:
-//   PackedHead, how many tiles and short sequences there are;
-//   PackedTile of every PACKED_ROWS rows of every sequence that is not short, in
-//     order of falling work, packed_max_tiles() of them at most;
+//   PackedHead, how many of the following there are;
+//   PackedTile of every PACKED_ROWS rows of every sequence of more than PACKED_MID
+//     rows, in order of falling work;
 //   PackedTile (rank 0) of every middle sequence, of more than PACKED_SHORT and up to
 //     PACKED_MID rows, and of every short one, of up to PACKED_SHORT;
 //   PackedItem of every piece of work of the dK/dV kernel on tiles: a key tile, or
@@ -9,8 +9,8 @@
 //   one int32 per row: its position in its sequence, or -1.
 // The lengths are known on the device only, so the attention's launches cover as
 // much work as there can be: unit u is tile u, or, past the tiles, middle and short
-// sequences: four, one per wave, of the forward kernel; of the dK/dV kernel two middle ones,
-// two waves each, or four short ones.
+// sequences (four of them, one per wave, in the forward kernel; two middle ones,
+// two waves each, or four short ones in the dK/dV kernel).
 #pragma once
 #include <algorithm>
 
@@ -101,8 +101,7 @@ inline const int32_t* packed_pos(const PackedShape& p, const void* plan) {
   return (const int32_t*)((const char*)plan + packed_layout(p).pos);
 }
 
-// Whatever a plan holds (lengths that were not in order, memory that was never
-// filled), the counts and entries returned lie inside the plan and the `total`
+// Whatever a plan holds (memory that was never filled, another shape's plan), the counts and entries returned lie inside the plan and the `total`
 // rows, so that nothing outside a buffer is touched.  All uniform over a wave.
 LS_DEV int packed_count(int n, int most) { return max(0, min(most, __builtin_amdgcn_readfirstlane(n))); }
 LS_DEV PackedTile packed_checked(PackedTile t, int total) {

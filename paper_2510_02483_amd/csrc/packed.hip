@@ -50,20 +50,28 @@ LS_DEV int seq_len(const int32_t* cu, int s, int total, int& start) {
   return a >= 0 && b > a && b <= total ? b - a : 0;
 }
 
-// Sum over the workgroup (every thread gets it).
-LS_DEV long long block_sum(long long v, long long* part) {
+// Sums of two values over the workgroup (every thread gets them).
+LS_DEV void block_sums(long long (&v)[2], long long (*part)[PLAN_WAVES]) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  for (int o = 32; o >= 1; o >>= 1) {
+    v[0] += __shfl_xor(v[0], o);
+    v[1] += __shfl_xor(v[1], o);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    part[0][threadIdx.x >> 6] = v[0];
+    part[1][threadIdx.x >> 6] = v[1];
+  }
   __syncthreads();
-  long long s = 0;
+  v[0] = v[1] = 0;
 #pragma unroll
-  for (int w = 0; w < PLAN_WAVES; ++w) s += part[w];
-  return s;
+  for (int w = 0; w < PLAN_WAVES; ++w) {
+    v[0] += part[0][w];
+    v[1] += part[1][w];
+  }
 }
 
-// Workgroup 0 lists the tiles, the middle and short sequences and the pieces of dK/dV work, the
-// others find the rows' positions.
+// Workgroup 0 lists the tiles, the middle and short sequences and the pieces of
+// dK/dV work, the others find the rows' positions.
 //
 // The list of tiles is a counting sort by rank (a tile's work), the highest first:
 // ranks are counted with one range update per sequence in a difference array,
@@ -73,7 +81,12 @@ LS_DEV long long block_sum(long long v, long long* part) {
 // class are cut into the same number of parts, so that a tile's place among the
 // pieces and its slots follow from its place in its class.
 //
-// Bound by latency: one pass over cu_seqlens, two scans and a sum, one more pass.
+// Lengths that are out of order and add up to more than the total make a plan
+// without sequences: the lists have no room for them, and entering them could take
+// as many steps as there are sequences times tiles.
+//
+// Bound by latency, 5 to 7 us: one pass over cu_seqlens, two scans and a sum, one
+// more pass.
 __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, int n, int nkv, int group,
                                                                    const int32_t* __restrict__ cu, char* plan,
                                                                    PackedLayout lay) {
@@ -99,7 +112,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   // per class: counts of ranks, then tiles entered so far; first tile; first piece; first slot
   __shared__ int level[LEVELS + 1], first[LEVELS], piece[LEVELS], slot[LEVELS];
   __shared__ int part[1][PLAN_WAVES], part3[3][PLAN_WAVES];
-  __shared__ long long part64[PLAN_WAVES];
+  __shared__ long long part64[2][PLAN_WAVES];
   __shared__ int nmid, nshort, nsplit;
   const int max_rank = (total - 1) / PACKED_ROWS;
   int shift = 0;
@@ -108,9 +121,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   if (tid == 0) nmid = nshort = nsplit = 0;
   __syncthreads();
   const int per = 1 << shift;
+  long long rows = 0;
   for (int s = tid; s < n; s += PLAN_THREADS) {
     int start;
     const int len = seq_len(cu, s, total, start);
+    rows += len;
     if (len <= PACKED_MID) continue;
     // classes 0 .. top-1 get `per` ranks each, class `top` the rest
     const int m = (len - 1) / PACKED_ROWS + 1, top = (m - 1) >> shift, rest = m - (top << shift);
@@ -131,13 +146,18 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   const int before = sum[0] - mine;
   // work of a class's last rank, and of a part at most
   auto units = [&](int l) { return (unsigned)(l + 1) << shift; };
-  long long work = 0;
+  long long sums[2] = {0, rows};
 #pragma unroll
   for (int k = 0; k < PT; ++k) {
     c[k] += before;
-    work += (long long)c[k] * units(PT * tid + k);
+    sums[0] += (long long)c[k] * units(PT * tid + k);
   }
-  work = (block_sum(work, part64) * nkv + 2 * PACKED_CUS - 1) / (2 * PACKED_CUS);
+  block_sums(sums, part64);
+  if (sums[1] > total) {
+    if (tid == 0) *(PackedHead*)plan = PackedHead{0, 0, 0, 0, 0};
+    return;
+  }
+  const long long work = (sums[0] * nkv + 2 * PACKED_CUS - 1) / (2 * PACKED_CUS);
   const unsigned least = (PACKED_PART + group - 1) / group, most = 1u << 30;
   const unsigned target = work < least ? least : work > most ? most : (unsigned)work;
   auto parts_of = [&](int l) { return (int)min((units(l) + target - 1) / target, 1023u); };
@@ -170,8 +190,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   auto enter = [&](int start, int len, int rank) {
     const int l = rank >> shift, p = parts_of(l);
     const int i = atomicAdd(&level[l], 1), at = first[l] + i, q = piece[l] + i * p;
-    // (lengths that are out of order may give more tiles than the lists have room for)
-    if (at < 0 || at >= lay.max_tiles || q < 0 || q + p > lay.max_items) return;
+    if (at < 0 || at >= lay.max_tiles || q < 0 || q + p > lay.max_items) return;  // (never)
     PackedTile t{start, len, rank, 1, 0};
     t.parts = (unsigned)p;
     t.slot = p > 1 ? (unsigned)(slot[l] + i * p) : 0u;

@@ -274,6 +274,40 @@ def test_nothing_written_outside_the_outputs():
     within("dh", x.dh, r["dh"], r["tol_dh"])
 
 
+def test_head_weights_beyond_2_gib():
+    """V x H x 2 = 2.4 GB: the forward takes the vocabulary in pieces too, and offsets pass 31 bits."""
+    need_gpu()
+    T, H, V = 24, 4096, 290_001
+    g = torch.Generator(device="cuda")
+    g.manual_seed(37)
+    e = torch.empty(V, H, dtype=torch.bfloat16, device="cuda")
+    for a in range(0, V, 50_000):
+        e[a:a + 50_000] = torch.randn(min(50_000, V - a), H, generator=g, device="cuda") * H ** -0.5
+    x = Head(T, H, 64, seed=37)
+    x.V, x.e = V, e
+    x.t = torch.tensor([0, V - 1, 261_990, 262_144, 131_072, -1] * 4, dtype=torch.int32, device="cuda")
+    x.low = torch.full((V, H), 7.0, dtype=torch.bfloat16, device="cuda")
+    x.fwd()
+    h = x.h.double()
+    z = torch.cat([h @ e[a:a + 20_000].double().T for a in range(0, V, 20_000)], 1)
+    lse = torch.logsumexp(z, 1)
+    has, at = x.t >= 0, x.t.long().clamp(min=0)
+    rows = torch.where(has, lse - z.gather(1, at[:, None])[:, 0], 0.0)
+    ez = H * W * (x.h.abs().double().sum(1) * float(e.abs().max()))
+    tol = ez + 2.0 ** -17 + 2.0 ** -21 * lse.abs()
+    within("lse", x.lse, lse, tol)
+    within("row_loss", x.rows, rows, tol + ez)
+    x.bwd(x.low)
+    n = int(has.sum())
+    dz = torch.exp(z - lse[:, None])
+    dz[torch.arange(T, device="cuda"), at] -= 1.0
+    dz *= has[:, None] * (0.375 / n)
+    for v in (0, 1, 131_072, 261_990, 262_143, 262_144, V - 2, V - 1):
+        ref = dz[:, v] @ h
+        lim = (1.01 * U * dz[:, v].abs() + 2 * (tol * 0.375 / n) * torch.exp(z[:, v] - lse)) @ h.abs()
+        within(f"d_embed[{v}]", x.low[v], ref, lim * (1 + U) + U * ref.abs() + T * W * (dz[:, v].abs() @ h.abs()))
+
+
 def test_agrees_with_the_cross_entropy_of_kept_logits():
     """ls_gemm_nt and ls_cross_entropy round the logits to bf16: U/2 of the largest logit apart at most."""
     need_gpu()

@@ -228,17 +228,26 @@ def test_offsets_past_32_bits():
 
 
 def test_lengths_out_of_order_stay_inside_the_buffers():
-    """Entries that fall, that are negative or lie beyond the total: whatever comes out, nothing outside the
-    outputs is written, and a good plan afterwards works."""
+    """Entries that fall, that are negative or lie beyond the total, a plan that was never made or one of another
+    shape: whatever comes out, nothing outside the outputs is written, and a good plan afterwards works."""
     need_gpu()
     b = Batch([100, 100, 100], 2, 1, 64, seed=19)
+    b.plan = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
     pad = 4096
-    for cu in ([0, 200, 100, 300], [-50, 100, 1000, 300], [300, 200, 100, 0], [0, 300, 0, 300], [2 ** 31 - 1, -2 ** 31, 5, 90]):
+    for cu in ([0, 200, 100, 300], [-50, 100, 1000, 300], [300, 200, 100, 0], [0, 300, 0, 300], [2 ** 31 - 1, -2 ** 31, 5, 90],
+               [0, 300, 300, 100], [10, 20, 15, 300], None, 0, 255, 1, PackedConfig(5000, 3, 2, 1, 64)):
         say(cu)
         flat = torch.full((b.dqkv.numel() + 2 * pad,), MARK, dtype=torch.bfloat16, device="cuda")
         of = torch.full((b.o.numel() + 2 * pad,), MARK, dtype=torch.bfloat16, device="cuda")
         dqkv, o = flat[pad:-pad].view_as(b.dqkv), of[pad:-pad].view_as(b.o)
-        L.ls_packed_plan(b.c, torch.tensor(cu, dtype=torch.int32, device="cuda"), b.plan)
+        if cu is None:
+            b.plan.random_(0, 256)
+        elif isinstance(cu, int):
+            b.plan.fill_(cu)
+        elif isinstance(cu, PackedConfig):
+            L.ls_packed_plan(cu, torch.tensor([0, 70, 200, 5000], dtype=torch.int32, device="cuda"), b.plan)
+        else:
+            L.ls_packed_plan(b.c, torch.tensor(cu, dtype=torch.int32, device="cuda"), b.plan)
         L.ls_packed_rope(b.c, b.plan, 1e4, b.qkv, dqkv)
         L.ls_packed_attn_fwd(b.c, b.plan, b.qkv, o, b.lse)
         L.ls_packed_attn_bwd(b.c, b.plan, b.qkv, o, b.lse, b.dout, dqkv, b.ws)
@@ -295,6 +304,24 @@ def test_another_stream():
     b.run(stream=s)
     s.synchronize()
     assert torch.equal(a.o, b.o) and torch.equal(a.dqkv, b.dqkv)
+
+
+def test_two_streams_share_a_plan():
+    """Layers on two streams at once: one plan, workspaces and outputs of their own."""
+    need_gpu()
+    lens = [700, 3, 60, 0, 400]
+    a, b = Batch(lens, 8, 2, 64, seed=31), Batch(lens, 8, 2, 64, seed=33)
+    want = [Batch(lens, 8, 2, 64, seed=s).run() for s in (31, 33)]
+    L.ls_packed_plan(a.c, a.cu, a.plan)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for x, s in zip((a, b), streams):
+            L.ls_packed_attn_fwd(x.c, a.plan, x.qkv, x.o, x.lse, stream=s)
+            L.ls_packed_attn_bwd(x.c, a.plan, x.qkv, x.o, x.lse, x.dout, x.dqkv, x.ws, stream=s)
+    torch.cuda.synchronize()
+    for x, w in zip((a, b), want):
+        assert torch.equal(x.o, w.o) and torch.equal(x.dqkv, w.dqkv)
 
 
 def test_gradient_against_differences():
