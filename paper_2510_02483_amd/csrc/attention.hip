@@ -64,6 +64,7 @@ constexpr int BQ = 128;       // queries per workgroup (forward, dQ)
 constexpr int BKV = 64;       // keys per tile (forward, dQ)
 constexpr int BWD_BKV = 128;  // keys per workgroup (dK/dV)
 constexpr int BWD_BQ = 64;    // queries per tile (dK/dV)
+constexpr int DKDV_STAGES = 3;  // their stages in LDS
 static_assert(BQ == PACKED_ROWS && BWD_BKV == PACKED_ROWS, "one plan of packed sequences for all kernels");
 
 LS_DEV u32x4 load16(const bf16_t* p) { return *(const u32x4*)p; }
@@ -833,15 +834,20 @@ LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf1
 // Packed sequences: a workgroup takes a piece of the plan's work on tiles (a key tile and kv
 // head, or a part of its 64-query steps of all heads of the group, whose partial
 // sums go to a slot of `part`), or past those four short sequences and a kv head.
+// One stage: Q tile, dO tile, log-sum-exp (base 2) and D of its queries
+// (every operand of a stage within the reach of an LDS instruction's offset).
+template <int D>
+struct DkdvStage {
+  bf16_t q[BWD_BQ * D];
+  bf16_t o[BWD_BQ * D];
+  float l[256];
+  float d[256];
+};
 template <int D, bool SPLIT, bool PACKED>
-__global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_kernel(AttnShape sh, PackedView pk,
-                                                                const bf16_t* __restrict__ qkv,
-                                                                const bf16_t* __restrict__ dout,
-                                                                const float* __restrict__ lse2,
-                                                                const float* __restrict__ Dv, bf16_t* __restrict__ dqkv,
-                                                                const float* __restrict__ rope_cs, float scale,
-                                                                float sl2, int hsplit_arg, float* __restrict__ part) {
-  constexpr int NST = 3;                    // LDS stages
+LS_DEV void dkdv_tile(const AttnShape& sh, const PackedView& pk, const int x, DkdvStage<D> (&stg)[DKDV_STAGES],
+                      const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
+                      const float* __restrict__ Dv, bf16_t* __restrict__ dqkv, const float* __restrict__ rope_cs,
+                      float scale, float sl2, int hsplit_arg, float* __restrict__ part) {
   constexpr int NSD = D / 16, NI = D / 32;  // 16-wide d steps; 32-row d blocks
   constexpr int P1 = NSD, P2 = NSD, P3 = 2 * NI, P4 = 2 * NI;  // slots per phase
   constexpr int NB = P1 + P2 + P3 + P4;     // slots of a 32-query block
@@ -850,19 +856,9 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_
   static_assert(NSLOT % RING == 0, "ring positions repeat every tile");
   static_assert(P1 >= 4 && P2 >= 4 && 16 % P2 == 0 && 16 % P3 == 0, "phase sizes");
   constexpr int BAR = NSLOT - RA;           // slot of the barrier
-  // one stage: Q tile, dO tile, log-sum-exp (base 2) and D of its queries
-  // (every operand of a stage within the reach of an LDS instruction's offset)
-  struct Stage {
-    bf16_t q[BWD_BQ * D];
-    bf16_t o[BWD_BQ * D];
-    float l[256];
-    float d[256];
-  };
-  __shared__ __attribute__((aligned(1024))) Stage stg[NST];
-
   const int hsplit = SPLIT ? hsplit_arg : 1;  // the unsplit instance folds every split term away
   const int nq = sh.nq, nkv = sh.nkv, G = nq / nkv, Gs = SPLIT ? G / hsplit : G;
-  const int per = nkv * sh.batch * hsplit, x = (int)blockIdx.x;
+  const int per = nkv * sh.batch * hsplit;
   const int hs = (x % per) % hsplit, kvh = ((x % per) / hsplit) % nkv, b = ((x % per) / hsplit) / nkv;
   int kvt = x / per, S = sh.seq;
   int64_t row0 = (int64_t)b * S, vec0 = (int64_t)b * nq * S;  // this sequence's first row; its entry of head 0's vectors
@@ -1057,14 +1053,28 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_
   }
 }
 
-// dK and dV of packed key tile `tile`, if its work was cut into parts, and kv head
-// kvh: the parts' sums added in their order, scaled and rounded.  A wave takes 8
-// rows at a time, their loads in flight together, a lane 2D / 64 columns of [dK | dV].
+template <int D, bool SPLIT, bool PACKED>
+__global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_kernel(AttnShape sh, PackedView pk,
+                                                                const bf16_t* __restrict__ qkv,
+                                                                const bf16_t* __restrict__ dout,
+                                                                const float* __restrict__ lse2,
+                                                                const float* __restrict__ Dv, bf16_t* __restrict__ dqkv,
+                                                                const float* __restrict__ rope_cs, float scale,
+                                                                float sl2, int hsplit, float* __restrict__ part) {
+  __shared__ __attribute__((aligned(1024))) DkdvStage<D> stg[DKDV_STAGES];
+  dkdv_tile<D, SPLIT, PACKED>(sh, pk, (int)blockIdx.x, stg, qkv, dout, lse2, Dv, dqkv, rope_cs, scale, sl2, hsplit, part);
+}
+
+// dK and dV of 32 rows of a packed key tile, if its work was cut into parts, and one kv
+// head: the parts' sums added in their order, scaled and rounded.  Workgroup x of
+// packed_joins takes quarter x % 4 of tile x / 4 / nkv, a wave 8 rows of it, a
+// lane 2D / 64 columns of [dK | dV]; the loads of four parts are in flight together.
+__host__ __device__ inline int packed_joins(const PackedView& pk, int nkv) { return packed_max_split(pk) * nkv * 4; }
 template <int D>
-LS_DEV void join_parts(const AttnShape& sh, const PackedView& pk, int tile, int kvh, const float* __restrict__ part,
+LS_DEV void join_parts(const AttnShape& sh, const PackedView& pk, int x, const float* __restrict__ part,
                        bf16_t* __restrict__ dqkv, float scale) {
-  constexpr int E = 2 * D / 64, ROWS = 8;
-  const int nkv = sh.nkv;
+  constexpr int E = 2 * D / 64, ROWS = 8, AHEAD = 4;
+  const int nkv = sh.nkv, kvh = (x >> 2) % nkv, tile = (x >> 2) / nkv;
   const PackedHead head = *pk.head;
   const PackedTile t = packed_checked(pk.tiles[tile], sh.seq);  // (one of max_tiles)
   if (tile >= min(packed_count(head.tiles, pk.max_tiles), packed_count(head.split, pk.max_tiles))) return;
@@ -1080,21 +1090,31 @@ LS_DEV void join_parts(const AttnShape& sh, const PackedView& pk, int tile, int 
   const float c = is_k ? scale : 1.0f;
   const float* src = part + ((int64_t)slot * nkv + kvh) * (PACKED_ROWS * 2 * D) + c0;
   bf16_t* dst = dqkv + (t.start + (int64_t)kv0) * ld + (int64_t)(sh.nq + (is_k ? 0 : nkv) + kvh) * hd + col;
-  for (int r0 = ROWS * wave; r0 < BWD_BKV && kv0 + r0 < t.len; r0 += 4 * ROWS) {
-    fE v[ROWS];
+  const int r0 = 32 * (x & 3) + ROWS * wave;
+  if (kv0 + r0 >= t.len) return;
+  fE v[ROWS], u[AHEAD][ROWS];
 #pragma unroll
-    for (int k = 0; k < ROWS; ++k) v[k] = fE{};
-    // (rows past the end of the sequence are in the slot, unwritten, and go nowhere)
-    for (int p = 0; p < parts; ++p)
+  for (int k = 0; k < ROWS; ++k) v[k] = fE{};
+  // (rows past the end of the sequence are in the slot, unwritten, and go nowhere)
+  for (int p = 0; p < parts; p += AHEAD) {
 #pragma unroll
-      for (int k = 0; k < ROWS; ++k) v[k] += *(const fE*)(src + p * step + (r0 + k) * (2 * D));
+    for (int a = 0; a < AHEAD; ++a)
 #pragma unroll
-    for (int k = 0; k < ROWS; ++k) {
-      if (kv0 + r0 + k >= t.len || col >= hd) break;
-      bf16_t* y = dst + (r0 + k) * ld;
-      if constexpr (E == 4) *(u32x2*)y = u32x2{pack_bf2(v[k][0] * c, v[k][1] * c), pack_bf2(v[k][2] * c, v[k][3] * c)};
-      else *(uint32_t*)y = pack_bf2(v[k][0] * c, v[k][1] * c);
-    }
+      for (int k = 0; k < ROWS; ++k) u[a][k] = *(const fE*)(src + min(p + a, parts - 1) * step + (r0 + k) * (2 * D));
+    __builtin_amdgcn_sched_barrier(0);  // all of them before the first is waited for
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a)
+      if (p + a < parts) {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) v[k] += u[a][k];
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) {
+    if (kv0 + r0 + k >= t.len || col >= hd) break;
+    bf16_t* y = dst + (r0 + k) * ld;
+    if constexpr (E == 4) *(u32x2*)y = u32x2{pack_bf2(v[k][0] * c, v[k][1] * c), pack_bf2(v[k][2] * c, v[k][3] * c)};
+    else *(uint32_t*)y = pack_bf2(v[k][0] * c, v[k][1] * c);
   }
 }
 
@@ -1170,37 +1190,17 @@ __global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, int hs
 // of registers within the tile; two workgroups per compute unit keep the
 // matrix cores busy across tile boundaries and while one wave waits.
 template <int D, bool PACKED>
-__global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, PackedView pk,
-                                                              const bf16_t* __restrict__ qkv,
-                                                              const bf16_t* __restrict__ dout,
-                                                              const float* __restrict__ lse2,
-                                                              const float* __restrict__ Dv, bf16_t* __restrict__ dqkv,
-                                                              const float* __restrict__ rope_cs, float scale,
-                                                              float sl2, const float* __restrict__ part) {
+LS_DEV void dq_tile(const AttnShape& sh, const QTile& qtile, bf16_t (&Ks)[2][BKV * D], bf16_t (&Vs)[2][BKV * D],
+                    const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
+                    const float* __restrict__ Dv, bf16_t* __restrict__ dqkv, const float* __restrict__ rope_cs,
+                    float scale, float sl2) {
   constexpr int NSD = D / 16, NI = D / 32;
   constexpr int PS = 2 * NSD;                // slots of one block's S^T and dP^T (interleaved)
   constexpr int PQ = 2 * NI;                 // slots of one block's dQ^T
   constexpr int NSLOT = 2 * PS + 2 * PQ;
   constexpr int RING = 2, RA = RING - 1;
   static_assert(NSLOT % RING == 0 && 16 % PS == 0 && 16 % PQ == 0, "slot counts");
-  __shared__ __attribute__((aligned(1024))) bf16_t Ks[2][BKV * D];
-  __shared__ __attribute__((aligned(1024))) bf16_t Vs[2][BKV * D];
-
   const int nq = sh.nq, nkv = sh.nkv;
-  QTile qtile;
-  if constexpr (PACKED) {
-    // the first workgroups finish dK and dV; short sequences have their dQ already
-    const int joins = packed_max_split(pk) * nkv, x = (int)blockIdx.x;
-    if (x < joins) {
-      join_parts<D>(sh, pk, x / nkv, x % nkv, part, dqkv, scale);
-      return;
-    }
-    PackedTile t;
-    if (!packed_unit(pk, (x - joins) / nq, sh.seq, t) || t.len == 0) return;
-    qtile = q_tile(sh, t, packed_head((x - joins) % nq, nq, nkv));
-  } else {
-    qtile = q_tile(sh);
-  }
   const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv), hd = PACKED ? sh.d : D;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * hd;
   const int64_t ldo = (int64_t)nq * hd;
@@ -1316,6 +1316,71 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, Packe
 }
 
 template <int D, bool PACKED>
+__global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, PackedView pk,
+                                                              const bf16_t* __restrict__ qkv,
+                                                              const bf16_t* __restrict__ dout,
+                                                              const float* __restrict__ lse2,
+                                                              const float* __restrict__ Dv, bf16_t* __restrict__ dqkv,
+                                                              const float* __restrict__ rope_cs, float scale,
+                                                              float sl2, const float* __restrict__ part) {
+  __shared__ __attribute__((aligned(1024))) bf16_t Ks[2][BKV * D];
+  __shared__ __attribute__((aligned(1024))) bf16_t Vs[2][BKV * D];
+  QTile qtile;
+  if constexpr (PACKED) {
+    // the last workgroups finish dK and dV; short sequences have their dQ already
+    const int x = (int)blockIdx.x, joins = x - pk.max_tiles * sh.nq;
+    if (joins >= 0) {
+      join_parts<D>(sh, pk, joins, part, dqkv, scale);
+      return;
+    }
+    PackedTile t;
+    if (!packed_unit(pk, x / sh.nq, sh.seq, t) || t.len == 0) return;
+    qtile = q_tile(sh, t, packed_head(x % sh.nq, sh.nq, sh.nkv));
+  } else {
+    qtile = q_tile(sh);
+  }
+  dq_tile<D, PACKED>(sh, qtile, Ks, Vs, qkv, dout, lse2, Dv, dqkv, rope_cs, scale, sl2);
+}
+
+// dK/dV and dQ of packed sequences in one launch, for batches whose launches one after
+// the other would each leave compute units idle behind their longest tiles
+// (packed_one_launch).  The pieces of dK/dV come first, then the query tiles,
+// both in order of falling work; the other way round was slower (6 documents on 3000
+// rows, 12/4 heads of 64: backward 41 us, this way 39, two launches 47).
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_bwd_kernel(AttnShape sh, PackedView pk,
+                                                             const bf16_t* __restrict__ qkv,
+                                                             const bf16_t* __restrict__ dout,
+                                                             const float* __restrict__ lse2,
+                                                             const float* __restrict__ Dv, bf16_t* __restrict__ dqkv,
+                                                             float scale, float sl2, float* __restrict__ part,
+                                                             int pieces) {
+  union Lds {
+    DkdvStage<D> stg[DKDV_STAGES];
+    struct {
+      bf16_t k[2][BKV * D], v[2][BKV * D];
+    } dq;
+  };
+  __shared__ __attribute__((aligned(1024))) char lds[sizeof(Lds)];
+  Lds& m = *(Lds*)lds;
+  const int x = (int)blockIdx.x;
+  if (x < pieces) {
+    dkdv_tile<D, false, true>(sh, pk, x, m.stg, qkv, dout, lse2, Dv, dqkv, nullptr, scale, sl2, 1, part);
+    return;
+  }
+  PackedTile t;
+  if (!packed_unit(pk, (x - pieces) / sh.nq, sh.seq, t) || t.len == 0) return;
+  dq_tile<D, true>(sh, q_tile(sh, t, packed_head((x - pieces) % sh.nq, sh.nq, sh.nkv)), m.dq.k, m.dq.v, qkv, dout, lse2,
+                   Dv, dqkv, nullptr, scale, sl2);
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void packed_join_kernel(AttnShape sh, PackedView pk, bf16_t* __restrict__ dqkv,
+                                                          float scale, const float* __restrict__ part) {
+  join_parts<D>(sh, pk, (int)blockIdx.x, part, dqkv, scale);
+}
+
+template <int D, bool PACKED>
 hipError_t attn_fwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, bf16_t* o, float* lse,
                       hipStream_t s) {
   const unsigned grid = PACKED ? (unsigned)pk.max_units * sh.nq
@@ -1377,6 +1442,13 @@ hipError_t attn_bwd_t(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, c
   return hipGetLastError();
 }
 
+// Whether dK/dV and dQ go into one launch (and the joining of parts into one behind it): up to
+// four query tiles to a compute unit.  Backward, one launch against two, at query
+// tiles times heads of (heads of 64) 348: 39 / 47 us, 704: 45 / 53, 1280: 91 / 93,
+// short documents of 3040: 62 / 58; (of 128, where one launch leaves dQ one
+// workgroup to a compute unit instead of two) 320: 71 / 82, 600: 209 / 227, 1824: 261 / 251.
+bool packed_one_launch(const AttnShape& sh, const PackedView& pk) { return (int64_t)pk.max_tiles * sh.nq <= 4 * PACKED_CUS; }
+
 template <int D>
 hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, const bf16_t* o,
                              const float* lse, const bf16_t* dout, bf16_t* dqkv, void* ws, hipStream_t s) {
@@ -1390,11 +1462,20 @@ hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf
   if (e != hipSuccess) return e;
   const float scale = 1.0f / sqrtf((float)sh.d);
   const unsigned gkv = (unsigned)(pk.max_units + pk.max_items - pk.max_tiles) * sh.nkv;
+  if (packed_one_launch(sh, pk)) {
+    hipLaunchKernelGGL((packed_bwd_kernel<D>), dim3(gkv + (unsigned)pk.max_tiles * sh.nq), dim3(256), 0, s, sh, pk, qkv,
+                       dout, (const float*)lse2, (const float*)Dv, dqkv, scale, scale * LOG2E, part, (int)gkv);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((packed_join_kernel<D>), dim3((unsigned)packed_joins(pk, sh.nkv)), dim3(256), 0, s, sh, pk,
+                       dqkv, scale, (const float*)part);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, true>), dim3(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
                      (const float*)lse2, (const float*)Dv, dqkv, (const float*)nullptr, scale, scale * LOG2E, 1, part);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const unsigned gq = (unsigned)packed_max_split(pk) * sh.nkv + (unsigned)pk.max_tiles * sh.nq;
+  const unsigned gq = (unsigned)packed_joins(pk, sh.nkv) + (unsigned)pk.max_tiles * sh.nq;
   hipLaunchKernelGGL((attn_bwd_dq_kernel<D, true>), dim3(gq), dim3(256), 0, s, sh, pk, qkv, dout, (const float*)lse2,
                      (const float*)Dv, dqkv, (const float*)nullptr, scale, scale * LOG2E, (const float*)part);
   return hipGetLastError();

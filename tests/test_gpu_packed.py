@@ -183,6 +183,23 @@ def test_one_long_sequence_among_others(nq, nkv, d):
     check(Batch([40, 2500, 3, 100], nq, nkv, d, tail=2, seed=27).run())
 
 
+@pytest.mark.parametrize("nq,nkv,d", [(6, 2, 64), (6, 3, 128), (6, 2, 88)])
+def test_backward_in_one_launch_or_two(nq, nkv, d):
+    """Rows behind the last sequence let the batch have more than 1024 query tiles times heads, the most whose dK/dV and
+    dQ share a launch: the same bits."""
+    need_gpu()
+    lens = [40, 500, 3, 100, 230, 64, 31]
+    few = Batch(lens, nq, nkv, d, tail=1, seed=31).run()
+    many = Batch(lens, nq, nkv, d, tail=22_000, seed=31)
+    rows = sum(lens)
+    many.qkv[:rows], many.dout[:rows] = few.qkv[:rows], few.dout[:rows]
+    many.run()
+    for a, b in ((few.o, many.o), (few.dqkv, many.dqkv)):
+        assert torch.equal(a[:rows], b[:rows])
+        assert (b[rows:] == MARK).all()
+    check(few)
+
+
 def test_many_sequences_and_every_row_once():
     """More sequences than the plan's workgroup has threads; the outputs do not depend on the order of its list."""
     need_gpu()
