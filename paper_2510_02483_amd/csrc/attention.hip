@@ -65,7 +65,7 @@ constexpr int BKV = 64;       // keys per tile (forward, dQ)
 constexpr int BWD_BKV = 128;  // keys per workgroup (dK/dV)
 constexpr int BWD_BQ = 64;    // queries per tile (dK/dV)
 constexpr int DKDV_STAGES = 3;  // their stages in LDS
-static_assert(BQ == PACKED_ROWS && BWD_BKV == PACKED_ROWS, "one plan of packed sequences for all kernels");
+static_assert(BQ == PACKED_ROWS && BWD_BKV == PACKED_ROWS && BWD_BQ == PACKED_STEP, "one plan of packed sequences for all kernels");
 
 LS_DEV u32x4 load16(const bf16_t* p) { return *(const u32x4*)p; }
 LS_DEV u32x4 pack_frag(const f32x16& v, int r0) {
@@ -901,7 +901,7 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const PackedView& pk, const int x, Dk
   int tbegin = 0, ntiles = Gs * nqt;  // (packed: this part's)
   if constexpr (PACKED) {
     if (parts > 1) {
-      // (a plan has fewer parts than steps; whatever it holds, a part has a step, within the sequence)
+      // (a plan has no more parts than steps; whatever it holds, a part has a step, within the sequence)
       const int all = ntiles;
       tbegin = min((int)((int64_t)all * part_no / parts), all - 1);
       ntiles = max((int)((int64_t)all * (part_no + 1) / parts), tbegin + 1);
@@ -1079,7 +1079,7 @@ LS_DEV void join_parts(const AttnShape& sh, const PackedView& pk, int x, const f
   const PackedTile t = packed_checked(pk.tiles[tile], sh.seq);  // (one of max_tiles)
   if (tile >= min(packed_count(head.tiles, pk.max_tiles), packed_count(head.split, pk.max_tiles))) return;
   const int parts = __builtin_amdgcn_readfirstlane((int)t.parts), slot = __builtin_amdgcn_readfirstlane((int)t.slot);
-  if (t.len == 0 || slot + parts > pk.max_slots) return;
+  if (t.len == 0 || parts < 2 || slot + parts > pk.max_slots) return;
   const int kv0 = ((t.len - 1) / BWD_BKV - t.rank) * BWD_BKV;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = E * lane;
   typedef float fE __attribute__((ext_vector_type(E)));

@@ -52,6 +52,7 @@ struct PackedLayout {
 // So there are at most 2 PACKED_CUS / nkv parts more than tiles, and as many tiles
 // that are cut.
 constexpr int PACKED_CUS = 256, PACKED_PART = 2;
+constexpr int PACKED_STEP = 64;  // queries of one head in a step of the dK/dV kernel
 inline PackedLayout packed_layout(const PackedShape& p) {
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   PackedLayout l;

@@ -191,11 +191,14 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
     const int l = rank >> shift, p = parts_of(l);
     const int i = atomicAdd(&level[l], 1), at = first[l] + i, q = piece[l] + i * p;
     if (at < 0 || at >= lay.max_tiles || q < 0 || q + p > lay.max_items) return;  // (never)
+    // a class of many ranks may cut its lowest into more parts than they have steps: their last pieces are empty
+    const int first_key = ((len - 1) / PACKED_ROWS - rank) * PACKED_ROWS;
+    const int mine = (int)min((long long)p, (long long)group * ((len - first_key + PACKED_STEP - 1) / PACKED_STEP));
     PackedTile t{start, len, rank, 1, 0};
-    t.parts = (unsigned)p;
+    t.parts = (unsigned)mine;
     t.slot = p > 1 ? (unsigned)(slot[l] + i * p) : 0u;
     tiles[at] = t;
-    for (int j = 0; j < p; ++j) items[q + j] = PackedItem{t, j, {0, 0, 0}};
+    for (int j = 0; j < p; ++j) items[q + j] = j < mine ? PackedItem{t, j, {0, 0, 0}} : PackedItem{};
   };
   // a wave takes 64 sequences at a time and enters 64 of their tiles at a time
   for (int s0 = 0; s0 < n; s0 += PLAN_THREADS) {

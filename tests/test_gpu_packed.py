@@ -200,6 +200,31 @@ def test_backward_in_one_launch_or_two(nq, nkv, d):
     check(few)
 
 
+@pytest.mark.parametrize("nq,nkv", [(1, 1), (2, 1)])
+@pytest.mark.parametrize("total", [300_000, 3_000_000])
+def test_short_sequences_in_a_long_row(total, nq, nkv):
+    """A row so long that the plan keeps many ranks to a class: a tile's work is not cut into more parts than it has
+    steps."""
+    need_gpu()
+    lens, d = [130, 65, 300, 1], 64
+    small = Batch(lens, nq, nkv, d, seed=33).run()
+    check(small)
+    big = PackedConfig(total, len(lens), nq, nkv, d)
+    plan = torch.empty(L.ls_packed_plan_bytes(big), dtype=torch.uint8, device="cuda")
+    L.ls_packed_plan(big, small.cu, plan)
+    rows = sum(lens)
+    qkv, dout = (torch.zeros(total, x.shape[1], dtype=x.dtype, device="cuda") for x in (small.qkv, small.dout))
+    qkv[:rows], dout[:rows] = small.qkv, small.dout
+    o, dqkv, lse = torch.zeros_like(dout), torch.zeros_like(qkv), torch.zeros(nq, total, device="cuda")
+    ws = torch.empty(L.ls_packed_attn_bwd_workspace(big), dtype=torch.uint8, device="cuda")
+    L.ls_packed_attn_fwd(big, plan, qkv, o, lse)
+    L.ls_packed_attn_bwd(big, plan, qkv, o, lse, dout, dqkv, ws)
+    assert torch.equal(o[:rows], small.o) and torch.equal(dqkv[:rows, :nq * d], small.dqkv[:, :nq * d])
+    small.dqkv = dqkv[:rows]
+    check(small)
+    assert not dqkv[rows:].any()
+
+
 def test_many_sequences_and_every_row_once():
     """More sequences than the plan's workgroup has threads; the outputs do not depend on the order of its list."""
     need_gpu()
