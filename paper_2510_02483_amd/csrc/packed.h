@@ -1,7 +1,7 @@
 // The plan of a batch of packed sequences, as the kernels read it:
 //   PackedHead, how many of the following there are;
 //   PackedTile of every PACKED_ROWS rows of every sequence of more than PACKED_MID
-//     rows, in order of falling work;
+//     rows, in order of falling work (and of the others, where they are few);
 //   PackedTile (rank 0) of every middle sequence, of more than PACKED_SHORT and up to
 //     PACKED_MID rows, and of every short one, of up to PACKED_SHORT;
 //   PackedItem of every piece of work of the dK/dV kernel on tiles: a key tile, or
@@ -46,12 +46,14 @@ struct PackedLayout {
   int64_t max_tiles, max_mids, max_shorts, max_items, max_slots, max_units;
   size_t tiles, mids, shorts, items, pos, total;
 };
-// A key tile of rank r is r + 1 units of dK/dV work per kv head (128 queries of every
-// head of the group each).  A tile with more than half of a compute unit's share
-// of all work is cut into parts of at most that, of two heads' units or more.
+// A key tile of rank r is r + 1 units of dK/dV work (128 queries) for every head of a kv
+// head's group.  A tile with more than half of a compute unit's share of the tiles' work
+// (in whole units of the group; less in small batches) is cut into parts of at most that.
 // So there are at most 2 PACKED_CUS / nkv parts more than tiles, and as many tiles
 // that are cut.
 constexpr int PACKED_CUS = 256, PACKED_PART = 2;
+// Middle and short sequences up to this many are listed as tiles where the heads of a group are many.
+__host__ __device__ inline int packed_few(int nkv) { return PACKED_CUS / 4 / nkv; }
 constexpr int PACKED_STEP = 64;  // queries of one head in a step of the dK/dV kernel
 inline PackedLayout packed_layout(const PackedShape& p) {
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
@@ -60,6 +62,7 @@ inline PackedLayout packed_layout(const PackedShape& p) {
   // At most `big` sequences are long enough for tiles, and one of n rows has at most 1 + n / PACKED_ROWS.
   const int64_t big = std::min(l.max_shorts, p.total / (PACKED_MID + 1));
   l.max_tiles = std::max<int64_t>(big + p.total / PACKED_ROWS, 1);
+  if (p.nq / p.nkv > 1) l.max_tiles += std::min<int64_t>(l.max_shorts, packed_few(p.nkv));
   // The work that all sequences can make, in units: a sequence of tiles takes its tiles, a middle one half a unit and
   // more than half as many rows as the shortest of tiles, a short one a quarter.  So most units come from as many
   // sequences of tiles as the rows allow, and short ones for the rest.  (A workgroup without work costs about a

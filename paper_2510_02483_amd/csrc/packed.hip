@@ -81,6 +81,12 @@ LS_DEV void block_sums(long long (&v)[2], long long (*part)[PLAN_WAVES]) {
 // class are cut into the same number of parts, so that a tile's place among the
 // pieces and its slots follow from its place in its class.
 //
+// Middle and short sequences are computed by a wave or two for all heads of a group, which
+// takes long where the group is large; a few of them, too few to fill the card, are
+// listed as tiles instead, whose heads can be shared out (the backward's main kernel on
+// one sequence of 64 rows, heads of 128: 4/2 heads 17 us by a pair of waves, 11 as a
+// tile; 8/2: 29, 12; 32/2: 103, 12; with one head to a group 11 and 14).
+//
 // Lengths that are out of order and add up to more than the total make a plan
 // without sequences: the lists have no room for them, and entering them could take
 // as many steps as there are sequences times tiles.
@@ -113,6 +119,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   __shared__ int level[LEVELS + 1], first[LEVELS], piece[LEVELS], slot[LEVELS];
   __shared__ int part[1][PLAN_WAVES], part3[3][PLAN_WAVES];
   __shared__ long long part64[2][PLAN_WAVES];
+  __shared__ int counts[3][PLAN_WAVES];  // of a wave: tiles, middle and short sequences
   __shared__ int nmid, nshort, nsplit;
   const int max_rank = (total - 1) / PACKED_ROWS;
   int shift = 0;
@@ -122,16 +129,28 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   __syncthreads();
   const int per = 1 << shift;
   long long rows = 0;
+  // (the latter two of the whole wave, in its first lane, which is in every turn)
+  int tiles_here = 0, mids_here = 0, shorts_here = 0;
   for (int s = tid; s < n; s += PLAN_THREADS) {
     int start;
     const int len = seq_len(cu, s, total, start);
     rows += len;
+    mids_here += __popcll(__ballot(len > PACKED_SHORT && len <= PACKED_MID));
+    shorts_here += __popcll(__ballot(len > 0 && len <= PACKED_SHORT));
     if (len <= PACKED_MID) continue;
     // classes 0 .. top-1 get `per` ranks each, class `top` the rest
     const int m = (len - 1) / PACKED_ROWS + 1, top = (m - 1) >> shift, rest = m - (top << shift);
+    tiles_here += m;
     atomicAdd(&level[0], per);
     atomicAdd(&level[top], rest - per);
     atomicAdd(&level[top + 1], -rest);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) tiles_here += __shfl_xor(tiles_here, o);
+  if ((tid & 63) == 0) {
+    counts[0][tid >> 6] = tiles_here;
+    counts[1][tid >> 6] = mids_here;
+    counts[2][tid >> 6] = shorts_here;
   }
   __syncthreads();
   constexpr int PT = LEVELS / PLAN_THREADS;  // classes per thread
@@ -144,23 +163,42 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   const int mine = sum[0];
   block_scan(sum, unused, part);
   const int before = sum[0] - mine;
-  // work of a class's last rank, and of a part at most
-  auto units = [&](int l) { return (unsigned)(l + 1) << shift; };
+  // work of a class's last rank, in units of 128 queries of one head
+  auto units = [&](int l) { return ((long long)(l + 1) << shift) * group; };
   long long sums[2] = {0, rows};
 #pragma unroll
   for (int k = 0; k < PT; ++k) {
     c[k] += before;
-    sums[0] += (long long)c[k] * units(PT * tid + k);
+    sums[0] += c[k] * units(PT * tid + k);
   }
   block_sums(sums, part64);
   if (sums[1] > total) {
     if (tid == 0) *(PackedHead*)plan = PackedHead{0, 0, 0, 0, 0};
     return;
   }
-  const long long work = (sums[0] * nkv + 2 * PACKED_CUS - 1) / (2 * PACKED_CUS);
-  const unsigned least = (PACKED_PART + group - 1) / group, most = 1u << 30;
-  const unsigned target = work < least ? least : work > most ? most : (unsigned)work;
-  auto parts_of = [&](int l) { return (int)min((units(l) + target - 1) / target, 1023u); };
+  int tiles_all = 0, mids_all = 0, shorts_all = 0;
+#pragma unroll
+  for (int w = 0; w < PLAN_WAVES; ++w) {
+    tiles_all += counts[0][w];
+    mids_all += counts[1][w];
+    shorts_all += counts[2][w];
+  }
+  const int few = mids_all + shorts_all;
+  const bool as_tiles = (mids_all > 0 ? 2 : 1) * group >= 4 && few <= packed_few(nkv) && tiles_all + few <= lay.max_tiles;
+  if (as_tiles) {
+    if (tid == 0) c[0] += few;
+    sums[0] += few * units(0);
+  }
+  // A part's work at most (PACKED_PART or more): half of a compute unit's share of the tiles' work in whole units of
+  // the group (parts of fractions were slower by up to a quarter where there are enough of whole ones), or, where
+  // there is little work for so many heads, a 64th of it and of the small sequences' (8/2 heads of 128, longest
+  // document 183 rows: backward 32 -> 24 us; without the small sequences in it, 60 short documents: 40 -> 43).
+  // In 32 bits, clamped: the plan's time is that of one thread's instructions.
+  auto clamped = [](long long v) { return (unsigned)min(v, 1ll << 30); };
+  auto share = [&](long long work, int n) { return max(clamped((work * nkv + n - 1) / n), (unsigned)PACKED_PART); };
+  const unsigned half = (share(sums[0], 2 * PACKED_CUS) + (unsigned)group - 1) / (unsigned)group * (unsigned)group;
+  const unsigned target = min(half, share(sums[0] + (as_tiles ? 0ll : (long long)few * group), 64));
+  auto parts_of = [&](int l) { return (int)min((clamped(units(l)) + target - 1) / target, 1023u); };
   // the first tile, piece and slot of each class, the highest class first
   int own[3] = {0, 0, 0}, all[3];  // tiles, pieces, slots
 #pragma unroll
@@ -214,9 +252,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
       at = __shfl(at, 0) + __popcll(few & ((1ull << lane) - 1));
       if (in && at < room) list[at] = PackedTile{start, len, 0, 1, 0};
     };
-    enter_small(len > PACKED_SHORT && len <= PACKED_MID, &nmid, mids, lay.max_mids);
-    enter_small(len > 0 && len <= PACKED_SHORT, &nshort, shorts, lay.max_shorts);
-    if (len <= PACKED_MID) len = 0;
+    if (!as_tiles) {
+      enter_small(len > PACKED_SHORT && len <= PACKED_MID, &nmid, mids, lay.max_mids);
+      enter_small(len > 0 && len <= PACKED_SHORT, &nshort, shorts, lay.max_shorts);
+      if (len <= PACKED_MID) len = 0;
+    }
     const int m = len > 0 ? (len - 1) / PACKED_ROWS + 1 : 0;
     int upto = m;
 #pragma unroll

@@ -86,6 +86,22 @@ def test_attention_matches_the_reference(lens, nq, nkv, d):
     check(Batch(nq=nq, nkv=nkv, d=d, seed=3, **LENGTHS[lens]).run())
 
 
+@pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (7, 1, 64), (8, 1, 128), (3, 1, 104)])
+def test_many_small_sequences_of_a_group(nq, nkv, d):
+    """More sequences of up to 64 rows than are listed as tiles (64 / nkv): waves and pairs of waves go through the
+    heads of the group."""
+    need_gpu()
+    lens = [1, 32, 33, 64, 0, 17, 50] * 12
+    check(Batch(lens + [65, 140], nq, nkv, d, tail=5, seed=35).run())
+
+
+@pytest.mark.parametrize("lens", [[1], [64], [33, 2], [20, 64, 0, 7]])
+@pytest.mark.parametrize("nq,nkv,d", [(32, 2, 64), (16, 1, 128)])
+def test_few_small_sequences_of_a_large_group(lens, nq, nkv, d):
+    need_gpu()
+    check(Batch(lens, nq, nkv, d, first=1, tail=2, seed=37).run())
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_peaked_scores(d):
     """Scores up to a hundred: the running maximum moves, probabilities underflow."""
