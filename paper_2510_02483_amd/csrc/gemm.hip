@@ -27,6 +27,21 @@ __global__ __launch_bounds__(256) void kpart_reduce_kernel(GemmArgs p) {
   }
 }
 
+// The same for the head's dh, whose rows and slices depend on the device's number of rows.
+__global__ __launch_bounds__(256) void dh_reduce_kernel(GemmArgs p, int bm, int bn) {
+  const int M = max(0, min(p.M, p.rows[0])), ks = dh_slices(p, M, bm, bn);
+  if (ks < 2) return;
+  const int64_t per = (int64_t)M * p.N, n4 = per / 4;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
+    const int64_t e = 4 * i;
+    const int m = (int)(e / p.N), n = (int)(e - (int64_t)m * p.N);
+    float* dst = p.F[0] + (int64_t)m * p.ldf + n;
+    f32x4 v = *(const f32x4*)dst;
+    for (int j = 0; j < ks - 1; ++j) v += *(const f32x4*)(p.kpart + j * per + e);
+    *(f32x4*)dst = v;
+  }
+}
+
 // Finishes a bf16-output product whose K was split: the slices' fp32 partial
 // sums ([slice][M][N]) are added in slice order and go through the product's
 // epilogue.  A thread takes 8 columns of a row (and their partner columns: the
@@ -251,7 +266,7 @@ GemmPlan make_plan(const GemmArgs& a, int64_t kpart_floats, int forced) {
   }
   // slices at least 8 k tiles deep, 8 at most; 32 for the head's dh, whose depth is a piece of the vocabulary
   // (509 x 768 x 32003: 45 -> 42 us)
-  const int most = a.epi == EPI_DH ? 32 : 8;
+  const int most = a.epi == EPI_DH ? MAX_DH_SLICES : 8;
   for (int ks = 1; ks <= most && (ks == 1 || ktiles >= 8 * ks); ++ks) {
     consider(128, 128, ks);
     consider(256, 128, ks);
@@ -277,6 +292,8 @@ int gemm_tile_override(int bm, int bn) {
 // call cannot make a launch need more than the call has checked.
 int64_t gemm_kpart_floats(const GemmArgs& a) {
   int64_t need = kpart_need(a, make_plan(a, INT64_MAX, 0).ks);
+  // for more slices where only some of the rows have a target, up to what a split may use at all
+  if (a.epi == EPI_DH) need = std::max(need, std::min<int64_t>((int64_t)(MAX_DH_SLICES - 1) * a.M * a.N, LLC_BYTES / 16));
   // the split a forced tile shape would use
   if (f32_out(a.epi)) need = std::max(need, kpart_need(a, ksplit_of(a.M, a.N, a.K)));
   return need;
@@ -304,16 +321,20 @@ hipError_t gemm(const GemmArgs& args, hipStream_t s, GemmPlan* used) {
                                  : p.bm == 256 ? (p.bn == 256 ? TILE_256 : TILE_256x192)
                                                : (p.bn == 256 ? TILE_192x256 : TILE_192);
   const int epi = a.epi;
+  if (epi == EPI_DH && a.kpart) {
+    const int64_t wgs = (int64_t)((a.M + p.bm - 1) / p.bm) * ((a.N + p.bn - 1) / p.bn) * p.ks;
+    a.fill = (int)std::min<int64_t>(wgs, t == TILE_128 ? 2 * compute_units() : compute_units());
+  }
   if (p.ks > 1 && t == TILE_256 && !f32_out(epi)) a.epi = EPI_PART;
   hipError_t e = epi >= EPI_LSE ? gemm_head(a, t, s)
                  : a.a_kcontig ? (a.b_kcontig ? gemm_nt(a, t, s) : gemm_nn(a, t, s)) : gemm_tn(a, t, s);
   a.epi = epi;
-  if (e != hipSuccess || p.ks == 1) return e;
+  if (e != hipSuccess || (p.ks == 1 && a.fill == 0)) return e;
   const int64_t items = f32_out(a.epi) ? (int64_t)a.M * a.N / 4 : (int64_t)a.M * a.N / 8;
   const dim3 grid((unsigned)std::min<int64_t>((items + 255) / 256, 256 * 8)), block(256);
   switch (a.epi) {
+    case EPI_DH: hipLaunchKernelGGL(dh_reduce_kernel, grid, block, 0, s, a, p.bm, p.bn); break;
     case EPI_F32:
-    case EPI_DH:
     case EPI_DE: hipLaunchKernelGGL(kpart_reduce_kernel, grid, block, 0, s, a); break;
     case EPI_BF16: hipLaunchKernelGGL((ksplit_finish_kernel<EPI_BF16>), grid, block, 0, s, a); break;
     case EPI_DE16: hipLaunchKernelGGL((ksplit_finish_kernel<EPI_DE16>), grid, block, 0, s, a); break;

@@ -95,6 +95,22 @@ __host__ __device__ inline void map_tile(int wg, int tiles_m, int tiles_n, int g
   tn = in_g / gm;
 }
 
+constexpr int MAX_DH_SLICES = 32;
+// Slices of K of the head's dh (EPI_DH): its tile rows are as many as the device's
+// number of rows needs, and where those leave workgroups of the launch without a
+// tile, they take more slices, as many as the partial sums' room holds (gradients of
+// 4096 rows of which a fifth have a target, 3072 x 128256: 3.52 -> 2.04 ms).
+__host__ __device__ inline int dh_slices(const GemmArgs& p, int M, int bm, int bn) {
+  if (p.fill == 0 || M <= 0) return p.ksplit;
+  const int tiles = ((M + bm - 1) / bm) * ((p.N + bn - 1) / bn);
+  const int64_t room = 1 + p.kpart_floats / ((int64_t)M * p.N);
+  int s = p.fill / tiles;
+  s = s < MAX_DH_SLICES ? s : MAX_DH_SLICES;
+  s = s < p.K / (8 * KT) ? s : p.K / (8 * KT);  // 8 k tiles at least
+  s = s < room ? s : (int)room;
+  return s > p.ksplit ? s : p.ksplit;
+}
+
 // LDS swizzles (XOR on the 16-byte chunk index).  The LDS serves 16 lanes of a
 // 16-byte read (32 lanes of an 8-byte read) per clock across 64 banks, so:
 //  - k-contiguous tiles (128-byte rows, 8 chunks): the 16 rows a 16-lane group
@@ -559,7 +575,8 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
   if constexpr (DEV_M) M = max(0, min(M, p.rows[0]));
   const int tiles_m = (M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN;
   // K may be split: workgroup x runs slice x / tiles of tile x % tiles
-  const int ks = p.ksplit;
+  int ks = p.ksplit;
+  if constexpr (EPI == EPI_DH) ks = dh_slices(p, M, BM, BN);
   if constexpr (DEV_M) {
     if ((int)blockIdx.x >= tiles_m * tiles_n * ks) return;
   }
@@ -881,7 +898,7 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
     // fp32 weight gradients straight from the registers: a lane's 4 columns are
     // 16 contiguous bytes (read-modify-write with accumulate).  Slices 1.. of a
     // split K store plain partial sums ([M][N] each) for kpart_reduce_kernel.
-    float* kp = slice > 0 ? p.kpart + (int64_t)(slice - 1) * p.M * p.N : nullptr;
+    float* kp = slice > 0 ? p.kpart + (int64_t)(slice - 1) * (EPI == EPI_DH ? M : p.M) * p.N : nullptr;
     float coef = 1.f;
     if constexpr (EPI == EPI_DE) coef = p.coef[0];
 #pragma unroll

@@ -73,6 +73,7 @@ struct GemmArgs {
   float* kpart = nullptr;
   int64_t kpart_floats = 0;
   int ksplit = 1;   // slices of K (set by gemm())
+  int fill = 0;     // EPI_DH: workgroups that its slices may fill when the rows are few (set by gemm())
   int group_m = 8;  // tile rows per group of the launch order (set by the launch)
 };
 

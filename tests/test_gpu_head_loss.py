@@ -113,6 +113,23 @@ def test_large_tiles(T, H, V):
     within("d_embed bf16", x.low, r["de"], r["tol_de"] * (1 + U) + U * r["de"].abs())
 
 
+@pytest.mark.parametrize("piece", [0, 4096])
+@pytest.mark.parametrize("T,H,V,masked", [(1500, 512, 9001, 0.8), (1500, 512, 9001, 0.97), (3000, 1024, 4500, 0.9),
+                                          (509, 256, 33000, 0.5), (509, 256, 33000, 0.998), (700, 64, 20000, 1.0)])
+def test_few_rows_with_a_target(T, H, V, masked, piece):
+    """dh of few rows is split over the vocabulary by the device; the rows left out hold NaN."""
+    need_gpu()
+    x = Head(T, H, V, masked=masked, seed=11).fwd()
+    r = x.reference()
+    x.h[x.t < 0] = float("nan")
+    x.bwd(x.de, piece=piece)
+    within("dh", x.dh, r["dh"], r["tol_dh"] + 1e-300)
+    within("d_embed", x.de, r["de"], r["tol_de"] + 1e-300)
+    again = x.dh.clone()
+    x.bwd(None, piece=piece)
+    assert torch.equal(x.dh, again)
+
+
 @pytest.mark.parametrize("piece", [1, 64, 200, 1024, 5000, 1 << 30])
 def test_pieces(piece):
     need_gpu()
