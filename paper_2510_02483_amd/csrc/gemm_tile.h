@@ -580,9 +580,16 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
   if constexpr (DEV_M) {
     if ((int)blockIdx.x >= tiles_m * tiles_n * ks) return;
   }
-  const int slice = ks > 1 ? (int)blockIdx.x / (tiles_m * tiles_n) : 0;
+  int slice = ks > 1 ? (int)blockIdx.x / (tiles_m * tiles_n) : 0;
   int tm, tn;
-  map_tile((int)blockIdx.x - slice * tiles_m * tiles_n, tiles_m, tiles_n, p.group_m, tm, tn);
+  if (EPI == EPI_DH && ks > 1) {
+    // the tiles of a slice, which read the same depth of both operands, on the same XCD
+    map_tile((int)blockIdx.x, tiles_m * tiles_n, ks, tiles_m * tiles_n, tm, slice);
+    tn = tm / tiles_m;
+    tm -= tn * tiles_m;
+  } else {
+    map_tile((int)blockIdx.x - slice * tiles_m * tiles_n, tiles_m, tiles_n, p.group_m, tm, tn);
+  }
   const int m0 = tm * BM, n0 = tn * BN;
   int K = p.K;
   if constexpr (DEV_K) K = max(0, min(K, p.rows[0]));
