@@ -91,7 +91,7 @@ LS_DEV void block_sums(long long (&v)[2], long long (*part)[PLAN_WAVES]) {
 // without sequences: the lists have no room for them, and entering them could take
 // as many steps as there are sequences times tiles.
 //
-// Bound by latency, 5 to 7 us: one pass over cu_seqlens, two scans and a sum, one
+// Bound by latency, 5 to 8 us: one pass over cu_seqlens, two scans and a sum, one
 // more pass.
 __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, int n, int nkv, int group,
                                                                    const int32_t* __restrict__ cu, char* plan,
