@@ -611,7 +611,7 @@ constexpr int short_lds_bytes() {
 }
 template <int D>
 LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf16_t* __restrict__ qkv,
-                      const bf16_t* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ Dv,
+                      const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
                       bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds) {
   constexpr int NSD = D / 16, NI = D / 32;
   const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv), hd = sh.d;
@@ -633,13 +633,39 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const b
     get_rows<D>(qf, rows, at(lr, ld, h), lh, hd);
     get_rows<D>(of, drows, at(lr, ldo, h), lh, hd);
     const int64_t v0 = (int64_t)h * sh.seq + t.start;
-    const float L = ok ? lse2[v0 + lr] : 0.f, Dr = ok ? Dv[v0 + lr] : 0.f;
+    const float L = ok ? lse2[v0 + lr] : 0.f;
     if (h == hq0) put_rows<D>(kt, kf, lr, lh);
     put_rows<D>(qt, qf, lr, lh);
     put_rows<D>(ot, of, lr, lh);
-    if (lh == 0) {
-      lv[lr] = L;
-      dvv[lr] = Dr;
+    if (lh == 0) lv[lr] = L;
+    wave_lds_order();
+    {  // lanes own queries: element r is key 8(r/4) + 4lh + r%4
+      f32x16 s{}, p{}, dq[NI];
+      float Dr = 0.f;
+#pragma unroll
+      for (int c = 0; c < NSD; ++c) {
+        s = mfma32(kf[c], qf[c], s);
+        p = mfma32(vf[c], of[c], p);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = ex2(fmaf(s[r], sl2, -L));
+        if (8 * (r >> 2) + 4 * lh + (r & 3) > lr) s[r] = p[r] = 0.f;
+        Dr = fmaf(s[r], p[r], Dr);
+      }
+      Dr = halves_sum(Dr);
+      if (lh == 0) dvv[lr] = Dr;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = s[r] * (p[r] - Dr);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) dq[i] = f32x16{};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const u32x4 sf = pack_frag(p, 8 * c);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) dq[i] = mfma32(colt_frag<D>(kt, 32 * i, c, lane), sf, dq[i]);
+      }
+      if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * hd, hd);
     }
     wave_lds_order();
     {  // lanes own keys: element r is query 8(r/4) + 4lh + r%4
@@ -670,29 +696,6 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const b
         }
       }
     }
-    {  // lanes own queries: element r is key 8(r/4) + 4lh + r%4
-      f32x16 s{}, p{}, dq[NI];
-#pragma unroll
-      for (int c = 0; c < NSD; ++c) {
-        s = mfma32(kf[c], qf[c], s);
-        p = mfma32(vf[c], of[c], p);
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float e = ex2(fmaf(s[r], sl2, -L));
-        if (8 * (r >> 2) + 4 * lh + (r & 3) > lr) e = 0.f;
-        p[r] = e * (p[r] - Dr);
-      }
-#pragma unroll
-      for (int i = 0; i < NI; ++i) dq[i] = f32x16{};
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const u32x4 sf = pack_frag(p, 8 * c);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) dq[i] = mfma32(colt_frag<D>(kt, 32 * i, c, lane), sf, dq[i]);
-      }
-      if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * hd, hd);
-    }
     wave_lds_order();
   }
   if (!ok) return;
@@ -711,7 +714,7 @@ constexpr int mid_lds_bytes() {
 }
 template <int D>
 LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf16_t* __restrict__ qkv,
-                    const bf16_t* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ Dv,
+                    const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
                     bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds) {
   constexpr int NSD = D / 16, NI = D / 32;
   const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv), hd = sh.d;
@@ -734,16 +737,58 @@ LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf1
     get_rows<D>(qf, rows, at(row, ld, h), lh, hd);
     get_rows<D>(of, drows, at(row, ldo, h), lh, hd);
     const int64_t v = (int64_t)h * sh.seq + t.start;
-    const float L = ok ? lse2[v + row] : 0.f, Dr = ok ? Dv[v + row] : 0.f;
+    const float L = ok ? lse2[v + row] : 0.f;
     if (h > hq0) sync_lds();  // the tiles of the head before are read
     if (h == hq0) put_rows<D>(kt + 32 * j * D, kf, lr, lh);
     put_rows<D>(qt + 32 * j * D, qf, lr, lh);
     put_rows<D>(ot + 32 * j * D, of, lr, lh);
-    if (lh == 0) {
-      lv[row] = L;
-      dvv[row] = Dr;
-    }
+    if (lh == 0) lv[row] = L;
     sync_lds();
+    // the wave's queries, keys of block b: element r is key 32b + 8(r/4) + 4lh + r%4
+    f32x16 dq[NI], s2[2], p2[2];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) dq[i] = f32x16{};
+    if (t.len > 0) {
+      float Dr = 0.f;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        s2[b] = p2[b] = f32x16{};
+        if (b > j) continue;
+        if (b == j) {
+#pragma unroll
+          for (int c = 0; c < NSD; ++c) p2[b] = mfma32(vf[c], row_frag<D>(ot, row, c, lh), p2[b]);
+        } else {  // (a middle sequence has all of its first 32 rows)
+          u32x4 v0[NSD];
+          get_rows<D>(v0, rows, at(lr, ld, nq + nkv + kvh), lh, hd);
+#pragma unroll
+          for (int c = 0; c < NSD; ++c) p2[b] = mfma32(v0[c], row_frag<D>(ot, row, c, lh), p2[b]);
+        }
+#pragma unroll
+        for (int c = 0; c < NSD; ++c)
+          s2[b] = mfma32(row_frag<D>(kt, 32 * b + lr, c, lh), row_frag<D>(qt, row, c, lh), s2[b]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s2[b][r] = ex2(fmaf(s2[b][r], sl2, -L));
+          if (32 * b + 8 * (r >> 2) + 4 * lh + (r & 3) > row) s2[b][r] = p2[b][r] = 0.f;
+          Dr = fmaf(s2[b][r], p2[b][r], Dr);
+        }
+      }
+      Dr = halves_sum(Dr);
+      if (lh == 0) dvv[row] = Dr;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if (b > j) continue;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p2[b][r] = s2[b][r] * (p2[b][r] - Dr);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const u32x4 sf = pack_frag(p2[b], 8 * c);
+#pragma unroll
+          for (int i = 0; i < NI; ++i) dq[i] = mfma32(colt_frag<D>(kt + 32 * b * D, 32 * i, c, lane), sf, dq[i]);
+        }
+      }
+    }
+    sync_lds();  // the other wave's D
     if (t.len == 0) continue;
     // the wave's keys, queries of block b: element r is query 32b + 8(r/4) + 4lh + r%4
     for (int b = j; b < 2; ++b) {
@@ -773,36 +818,6 @@ LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf1
           dv[i] = mfma32(colt_frag<D>(ot + 32 * b * D, 32 * i, c, lane), pf, dv[i]);
           dk[i] = mfma32(colt_frag<D>(qt + 32 * b * D, 32 * i, c, lane), sf, dk[i]);
         }
-      }
-    }
-    // the wave's queries, keys of block b: element r is key 32b + 8(r/4) + 4lh + r%4
-    f32x16 dq[NI];
-#pragma unroll
-    for (int i = 0; i < NI; ++i) dq[i] = f32x16{};
-    for (int b = 0; b <= j; ++b) {
-      f32x16 s{}, p{};
-      if (b == j) {
-#pragma unroll
-        for (int c = 0; c < NSD; ++c) p = mfma32(vf[c], of[c], p);
-      } else {  // (a middle sequence has all of its first 32 rows)
-        u32x4 v0[NSD];
-        get_rows<D>(v0, rows, at(lr, ld, nq + nkv + kvh), lh, hd);
-#pragma unroll
-        for (int c = 0; c < NSD; ++c) p = mfma32(v0[c], of[c], p);
-      }
-#pragma unroll
-      for (int c = 0; c < NSD; ++c) s = mfma32(row_frag<D>(kt, 32 * b + lr, c, lh), qf[c], s);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float e = ex2(fmaf(s[r], sl2, -L));
-        if (32 * b + 8 * (r >> 2) + 4 * lh + (r & 3) > row) e = 0.f;
-        p[r] = e * (p[r] - Dr);
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const u32x4 sf = pack_frag(p, 8 * c);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) dq[i] = mfma32(colt_frag<D>(kt + 32 * b * D, 32 * i, c, lane), sf, dq[i]);
       }
     }
     if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * hd, hd);
@@ -870,13 +885,13 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const PackedView& pk, const int x, Dk
     const PackedKind kind = packed_piece(pk, kvt, sh.seq, t, part_no);
     if (kind == PACKED_IS_MID) {
       const int pair = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 7);
-      mid_bwd<D>(sh, t, kvh, qkv, dout, lse2, Dv, dqkv, scale, sl2, (char*)&stg[0] + pair * mid_lds_bytes<D>());
+      mid_bwd<D>(sh, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + pair * mid_lds_bytes<D>());
       return;
     }
     if (t.len == 0) return;
     if (kind == PACKED_IS_SHORT) {
       const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-      short_bwd<D>(sh, t, kvh, qkv, dout, lse2, Dv, dqkv, scale, sl2, (char*)&stg[0] + w * short_lds_bytes<D>());
+      short_bwd<D>(sh, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + w * short_lds_bytes<D>());
       return;
     }
     parts = __builtin_amdgcn_readfirstlane((int)t.parts);
