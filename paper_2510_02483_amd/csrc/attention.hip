@@ -600,8 +600,24 @@ LS_DEV void unrotate_store(const f32x16 (&acc)[D / 32], float scale, const float
     }
 }
 
+// A lane's key row [dK | dV] of partial sums: columns 32i + 8(r/4) + 4lh + r%4.
+template <int D>
+LS_DEV void store_sums(float* row, const f32x16 (&dk)[D / 32], const f32x16 (&dv)[D / 32], int lh) {
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int rq = 0; rq < 4; ++rq) {
+      const int c = 32 * i + 8 * rq + 4 * lh;
+      *(f32x4*)(row + c) = f32x4{dk[i][4 * rq], dk[i][4 * rq + 1], dk[i][4 * rq + 2], dk[i][4 * rq + 3]};
+      *(f32x4*)(row + D + c) = f32x4{dv[i][4 * rq], dv[i][4 * rq + 1], dv[i][4 * rq + 2], dv[i][4 * rq + 3]};
+    }
+}
+
 // Backward of one kv head of a packed sequence of up to 32 rows by one wave: dQ of
-// its query heads, and dK and dV summed over them.
+// its query heads g0 .. g1 - 1 of the group, and dK and dV summed over them (to
+// `sums`, if given, as a part's fp32 sums).  D = sum P dP comes from the wave's own P and dP:
+// of few keys it is as large as dP, and from the rounded o it would cost dS more
+// than its own rounding does.
 // Scores and dP are formed both ways round, with the lanes owning keys for dK and
 // dV and owning queries for dQ: two more small products instead of transposing
 // dS.  K, Q and dO go through the wave's own LDS tiles for their transposes.
@@ -612,9 +628,9 @@ constexpr int short_lds_bytes() {
 template <int D>
 LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf16_t* __restrict__ qkv,
                       const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
-                      bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds) {
+                      bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds, int g0, int g1, float* sums) {
   constexpr int NSD = D / 16, NI = D / 32;
-  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv), hd = sh.d;
+  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv) + g0, hq1 = kvh * (nq / nkv) + g1, hd = sh.d;
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * hd, ldo = (int64_t)nq * hd;
   const bool ok = lr < t.len;
@@ -629,7 +645,7 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const b
   f32x16 dk[NI], dv[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) dk[i] = dv[i] = f32x16{};
-  for (int h = hq0; h < hq0 + nq / nkv; ++h) {
+  for (int h = hq0; h < hq1; ++h) {
     get_rows<D>(qf, rows, at(lr, ld, h), lh, hd);
     get_rows<D>(of, drows, at(lr, ldo, h), lh, hd);
     const int64_t v0 = (int64_t)h * sh.seq + t.start;
@@ -699,6 +715,10 @@ LS_DEV void short_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const b
     wave_lds_order();
   }
   if (!ok) return;
+  if (sums) {
+    store_sums<D>(sums + lr * (2 * D), dk, dv, lh);
+    return;
+  }
   unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * hd, hd);
   unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * hd, hd);
 }
@@ -715,9 +735,9 @@ constexpr int mid_lds_bytes() {
 template <int D>
 LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf16_t* __restrict__ qkv,
                     const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
-                    bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds) {
+                    bf16_t* __restrict__ dqkv, float scale, float sl2, char* lds, int g0, int g1, float* sums) {
   constexpr int NSD = D / 16, NI = D / 32;
-  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv), hd = sh.d;
+  const int nq = sh.nq, nkv = sh.nkv, hq0 = kvh * (nq / nkv) + g0, hq1 = kvh * (nq / nkv) + g1, hd = sh.d;
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
   const int j = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) & 1, row = 32 * j + lr;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * hd, ldo = (int64_t)nq * hd;
@@ -733,7 +753,7 @@ LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf1
   f32x16 dk[NI], dv[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) dk[i] = dv[i] = f32x16{};
-  for (int h = hq0; h < hq0 + nq / nkv; ++h) {
+  for (int h = hq0; h < hq1; ++h) {
     get_rows<D>(qf, rows, at(row, ld, h), lh, hd);
     get_rows<D>(of, drows, at(row, ldo, h), lh, hd);
     const int64_t v = (int64_t)h * sh.seq + t.start;
@@ -823,6 +843,10 @@ LS_DEV void mid_bwd(const AttnShape& sh, const PackedTile& t, int kvh, const bf1
     if (ok) unrotate_store<D>(dq, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + h * hd, hd);
   }
   if (!ok) return;
+  if (sums) {
+    store_sums<D>(sums + row * (2 * D), dk, dv, lh);
+    return;
+  }
   unrotate_store<D>(dk, scale, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + kvh) * hd, hd);
   unrotate_store<D>(dv, 1.0f, nullptr, 0, 0, lh, dqkv + r0 * ld + (nq + nkv + kvh) * hd, hd);
 }
@@ -885,17 +909,29 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const PackedView& pk, const int x, Dk
     const PackedKind kind = packed_piece(pk, kvt, sh.seq, t, part_no);
     if (kind == PACKED_IS_MID) {
       const int pair = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 7);
-      mid_bwd<D>(sh, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + pair * mid_lds_bytes<D>());
+      mid_bwd<D>(sh, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + pair * mid_lds_bytes<D>(), 0, G, nullptr);
       return;
     }
     if (t.len == 0) return;
     if (kind == PACKED_IS_SHORT) {
       const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-      short_bwd<D>(sh, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + w * short_lds_bytes<D>());
+      short_bwd<D>(sh, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + w * short_lds_bytes<D>(), 0, G, nullptr);
       return;
     }
     parts = __builtin_amdgcn_readfirstlane((int)t.parts);
     slot = __builtin_amdgcn_readfirstlane((int)t.slot);
+    if (t.len <= PACKED_MID) {  // few small sequences: the group's heads are what is cut
+      const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+      const int g0 = G * part_no / parts, g1 = G * (part_no + 1) / parts;
+      float* sums = parts > 1 ? part + (((int64_t)slot + part_no) * nkv + kvh) * (PACKED_ROWS * 2 * D) : nullptr;
+      if (t.len <= PACKED_SHORT) {
+        if (w == 0) short_bwd<D>(sh, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0], g0, g1, sums);
+      } else {
+        if (w >= 2) t.len = 0;  // (the first pair's)
+        mid_bwd<D>(sh, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + (w >> 1) * mid_lds_bytes<D>(), g0, g1, sums);
+      }
+      return;
+    }
     kvt = (t.len + BWD_BKV - 1) / BWD_BKV - 1 - t.rank;  // the most work: the first keys
     S = t.len;
     row0 = vec0 = t.start;
@@ -1054,14 +1090,7 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const PackedView& pk, const int x, Dk
     float* row = part;
     if constexpr (SPLIT) row += (((int64_t)hs * sh.batch * sh.seq + row0 + kvrow) * nkv + kvh) * (2 * D);
     else row += (((int64_t)slot + part_no) * nkv + kvh) * (PACKED_ROWS * 2 * D) + (32 * wave + lr) * (2 * D);
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-      for (int rq = 0; rq < 4; ++rq) {
-        const int c = 32 * i + 8 * rq + 4 * lh;
-        *(f32x4*)(row + c) = f32x4{dk[i][4 * rq], dk[i][4 * rq + 1], dk[i][4 * rq + 2], dk[i][4 * rq + 3]};
-        *(f32x4*)(row + D + c) = f32x4{dv[i][4 * rq], dv[i][4 * rq + 1], dv[i][4 * rq + 2], dv[i][4 * rq + 3]};
-      }
+    store_sums<D>(row, dk, dv, lh);
   } else {
     unrotate_store<D>(dk, scale, rope_cs, S, kvrow, lh, dqkv + (row0 + kvrow) * ld + (nq + kvh) * hd, hd);
     unrotate_store<D>(dv, 1.0f, nullptr, S, kvrow, lh, dqkv + (row0 + kvrow) * ld + (nq + nkv + kvh) * hd, hd);
@@ -1349,7 +1378,7 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(AttnShape sh, Packe
       return;
     }
     PackedTile t;
-    if (!packed_unit(pk, x / sh.nq, sh.seq, t) || t.len == 0) return;
+    if (!packed_unit(pk, x / sh.nq, sh.seq, t) || t.len <= PACKED_MID) return;
     qtile = q_tile(sh, t, packed_head(x % sh.nq, sh.nq, sh.nkv));
   } else {
     qtile = q_tile(sh);
@@ -1384,7 +1413,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void packed_bwd_kernel(AttnSh
     return;
   }
   PackedTile t;
-  if (!packed_unit(pk, (x - pieces) / sh.nq, sh.seq, t) || t.len == 0) return;
+  if (!packed_unit(pk, (x - pieces) / sh.nq, sh.seq, t) || t.len <= PACKED_MID) return;  // (small ones have their dQ)
   dq_tile<D, true>(sh, q_tile(sh, t, packed_head((x - pieces) % sh.nq, sh.nq, sh.nkv)), m.dq.k, m.dq.v, qkv, dout, lse2,
                    Dv, dqkv, nullptr, scale, sl2);
 }

@@ -62,7 +62,7 @@ inline PackedLayout packed_layout(const PackedShape& p) {
   // At most `big` sequences are long enough for tiles, and one of n rows has at most 1 + n / PACKED_ROWS.
   const int64_t big = std::min(l.max_shorts, p.total / (PACKED_MID + 1));
   l.max_tiles = std::max<int64_t>(big + p.total / PACKED_ROWS, 1);
-  if (p.nq / p.nkv > 1) l.max_tiles += std::min<int64_t>(l.max_shorts, packed_few(p.nkv));
+  if (p.nq / p.nkv > PACKED_PART) l.max_tiles += std::min<int64_t>(l.max_shorts, packed_few(p.nkv));
   // The work that all sequences can make, in units: a sequence of tiles takes its tiles, a middle one half a unit and
   // more than half as many rows as the shortest of tiles, a short one a quarter.  So most units come from as many
   // sequences of tiles as the rows allow, and short ones for the rest.  (A workgroup without work costs about a

@@ -83,9 +83,9 @@ LS_DEV void block_sums(long long (&v)[2], long long (*part)[PLAN_WAVES]) {
 //
 // Middle and short sequences are computed by a wave or two for all heads of a group, which
 // takes long where the group is large; a few of them, too few to fill the card, are
-// listed as tiles instead, whose heads can be shared out (the backward's main kernel on
-// one sequence of 64 rows, heads of 128: 4/2 heads 17 us by a pair of waves, 11 as a
-// tile; 8/2: 29, 12; 32/2: 103, 12; with one head to a group 11 and 14).
+// listed as tiles instead, whose heads are shared out by twos (the backward's main kernel
+// on one sequence of 64 rows, heads of 128: 8/2 heads 29 us by one pair of waves, 19
+// by two; 32/2: 103, 20; on one of 32 rows 15, 10 and 46, 11).
 //
 // Lengths that are out of order and add up to more than the total make a plan
 // without sequences: the lists have no room for them, and entering them could take
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   __shared__ int level[LEVELS + 1], first[LEVELS], piece[LEVELS], slot[LEVELS];
   __shared__ int part[1][PLAN_WAVES], part3[3][PLAN_WAVES];
   __shared__ long long part64[2][PLAN_WAVES];
-  __shared__ int counts[3][PLAN_WAVES];  // of a wave: tiles, middle and short sequences
+  __shared__ int counts[2][PLAN_WAVES];  // of a wave: tiles, middle and short sequences
   __shared__ int nmid, nshort, nsplit;
   const int max_rank = (total - 1) / PACKED_ROWS;
   int shift = 0;
@@ -129,14 +129,13 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   __syncthreads();
   const int per = 1 << shift;
   long long rows = 0;
-  // (the latter two of the whole wave, in its first lane, which is in every turn)
-  int tiles_here = 0, mids_here = 0, shorts_here = 0;
+  // (the latter of the whole wave, in its first lane, which is in every turn)
+  int tiles_here = 0, few_here = 0;
   for (int s = tid; s < n; s += PLAN_THREADS) {
     int start;
     const int len = seq_len(cu, s, total, start);
     rows += len;
-    mids_here += __popcll(__ballot(len > PACKED_SHORT && len <= PACKED_MID));
-    shorts_here += __popcll(__ballot(len > 0 && len <= PACKED_SHORT));
+    few_here += __popcll(__ballot(len > 0 && len <= PACKED_MID));
     if (len <= PACKED_MID) continue;
     // classes 0 .. top-1 get `per` ranks each, class `top` the rest
     const int m = (len - 1) / PACKED_ROWS + 1, top = (m - 1) >> shift, rest = m - (top << shift);
@@ -149,8 +148,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
   for (int o = 32; o >= 1; o >>= 1) tiles_here += __shfl_xor(tiles_here, o);
   if ((tid & 63) == 0) {
     counts[0][tid >> 6] = tiles_here;
-    counts[1][tid >> 6] = mids_here;
-    counts[2][tid >> 6] = shorts_here;
+    counts[1][tid >> 6] = few_here;
   }
   __syncthreads();
   constexpr int PT = LEVELS / PLAN_THREADS;  // classes per thread
@@ -176,15 +174,13 @@ __global__ __launch_bounds__(PLAN_THREADS) void packed_plan_kernel(int total, in
     if (tid == 0) *(PackedHead*)plan = PackedHead{0, 0, 0, 0, 0};
     return;
   }
-  int tiles_all = 0, mids_all = 0, shorts_all = 0;
+  int tiles_all = 0, few = 0;
 #pragma unroll
   for (int w = 0; w < PLAN_WAVES; ++w) {
     tiles_all += counts[0][w];
-    mids_all += counts[1][w];
-    shorts_all += counts[2][w];
+    few += counts[1][w];
   }
-  const int few = mids_all + shorts_all;
-  const bool as_tiles = (mids_all > 0 ? 2 : 1) * group >= 4 && few <= packed_few(nkv) && tiles_all + few <= lay.max_tiles;
+  const bool as_tiles = group > PACKED_PART && few <= packed_few(nkv) && tiles_all + few <= lay.max_tiles;
   if (as_tiles) {
     if (tid == 0) c[0] += few;
     sums[0] += few * units(0);
