@@ -349,7 +349,7 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 4 : 2) void attn_fwd_kerne
   if constexpr (PACKED) {
     static_assert(sizeof(Ks) >= 2 * PACKED_MID * D * sizeof(bf16_t), "a tile of V per wave");
     PackedTile t;
-    const int x = (int)blockIdx.x, head = packed_head(x % nq, nq, nkv);
+    const int x = packed_wg(), head = packed_head(x % nq, nq, nkv);
     const bool whole = packed_unit(pk, x / nq, sh.seq, t);
     if (t.len == 0) return;
     if (!whole) {
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(256) void attn_bwd_pre_kernel(AttnShape sh, const b
                                                            float* __restrict__ lse2) {
   constexpr int CPH = D / 8;  // 16-byte chunks per head
   const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t t = (int64_t)(PACKED ? packed_wg() : (int)blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (t >= (int64_t)sh.batch * sh.seq) return;
   if constexpr (PACKED) {
     bwd_pre_row<D>(sh, o + t * sh.nq * sh.d, dout + t * sh.nq * sh.d, lse, Dv, lse2, t);
@@ -1106,7 +1106,8 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_
                                                                 const float* __restrict__ rope_cs, float scale,
                                                                 float sl2, int hsplit, float* __restrict__ part) {
   __shared__ __attribute__((aligned(1024))) DkdvStage<D> stg[DKDV_STAGES];
-  dkdv_tile<D, SPLIT, PACKED>(sh, pk, (int)blockIdx.x, stg, qkv, dout, lse2, Dv, dqkv, rope_cs, scale, sl2, hsplit, part);
+  dkdv_tile<D, SPLIT, PACKED>(sh, pk, PACKED ? packed_wg() : (int)blockIdx.x, stg, qkv, dout, lse2, Dv, dqkv, rope_cs, scale, sl2,
+                              hsplit, part);
 }
 
 // dK and dV of 32 rows of a packed key tile, if its work was cut into parts, and one kv
@@ -1427,10 +1428,10 @@ __global__ __launch_bounds__(256) void packed_join_kernel(AttnShape sh, PackedVi
 template <int D, bool PACKED>
 hipError_t attn_fwd_t(const AttnShape& sh, const PackedView& pk, const bf16_t* qkv, bf16_t* o, float* lse,
                       hipStream_t s) {
-  const unsigned grid = PACKED ? (unsigned)pk.max_units * sh.nq
-                               : (unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch;
+  const dim3 grid = PACKED ? packed_grid((int64_t)pk.max_units * sh.nq)
+                           : dim3((unsigned)((sh.seq + BQ - 1) / BQ) * sh.nq * sh.batch);
   const float sl2 = LOG2E / sqrtf((float)(PACKED ? sh.d : sh.d_scale > 0 ? sh.d_scale : D));
-  hipLaunchKernelGGL((attn_fwd_kernel<D, PACKED>), dim3(grid), dim3(256), 0, s, sh, pk, qkv, o, lse, sl2);
+  hipLaunchKernelGGL((attn_fwd_kernel<D, PACKED>), grid, dim3(256), 0, s, sh, pk, qkv, o, lse, sl2);
   return hipGetLastError();
 }
 
@@ -1500,8 +1501,7 @@ hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf
   float* Dv = (float*)ws;
   float* lse2 = Dv + T * sh.nq;
   float* part = (float*)((char*)ws + bwd_ws_head(sh));
-  hipLaunchKernelGGL((attn_bwd_pre_kernel<D, true>), dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, sh, o, dout, lse, Dv,
-                     lse2);
+  hipLaunchKernelGGL((attn_bwd_pre_kernel<D, true>), packed_grid((T + 3) / 4), dim3(256), 0, s, sh, o, dout, lse, Dv, lse2);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const float scale = 1.0f / sqrtf((float)sh.d);
@@ -1515,10 +1515,11 @@ hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf
                        dqkv, scale, (const float*)part);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, true>), dim3(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
+  hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, true>), packed_grid(gkv), dim3(256), 0, s, sh, pk, qkv, dout,
                      (const float*)lse2, (const float*)Dv, dqkv, (const float*)nullptr, scale, scale * LOG2E, 1, part);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
+  // (one dimension's worth of tiles has more rows than the card's memory holds)
   const unsigned gq = (unsigned)packed_joins(pk, sh.nkv) + (unsigned)pk.max_tiles * sh.nq;
   hipLaunchKernelGGL((attn_bwd_dq_kernel<D, true>), dim3(gq), dim3(256), 0, s, sh, pk, qkv, dout, (const float*)lse2,
                      (const float*)Dv, dqkv, (const float*)nullptr, scale, scale * LOG2E, (const float*)part);

@@ -105,6 +105,15 @@ inline const int32_t* packed_pos(const PackedShape& p, const void* plan) {
   return (const int32_t*)((const char*)plan + packed_layout(p).pos);
 }
 
+// A dimension of a launch holds fewer than 2^32 threads, which is 2^24 workgroups of 256: more lie in rows of
+// PACKED_ROW_WGS, in the same order.  Those that the last row has too many find no work.
+constexpr int PACKED_ROW_WGS = 1 << 23;
+inline dim3 packed_grid(int64_t wgs) {
+  if (wgs <= PACKED_ROW_WGS) return dim3((unsigned)wgs);
+  return dim3(PACKED_ROW_WGS, (unsigned)((wgs + PACKED_ROW_WGS - 1) / PACKED_ROW_WGS));
+}
+LS_DEV int packed_wg() { return (int)(blockIdx.y * PACKED_ROW_WGS + blockIdx.x); }
+
 // Whatever a plan holds (memory that was never filled, another shape's plan), the counts and entries returned lie inside the plan and the `total`
 // rows, so that nothing outside a buffer is touched.  All uniform over a wave.
 LS_DEV int packed_count(int n, int most) { return max(0, min(most, __builtin_amdgcn_readfirstlane(n))); }
