@@ -1510,9 +1510,10 @@ hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf
     hipLaunchKernelGGL((packed_bwd_kernel<D>), dim3(gkv + (unsigned)pk.max_tiles * sh.nq), dim3(256), 0, s, sh, pk, qkv,
                        dout, (const float*)lse2, (const float*)Dv, dqkv, scale, scale * LOG2E, part, (int)gkv);
     e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((packed_join_kernel<D>), dim3((unsigned)packed_joins(pk, sh.nkv)), dim3(256), 0, s, sh, pk,
-                       dqkv, scale, (const float*)part);
+    const int joins = packed_joins(pk, sh.nkv);  // 0 with more than 2 PACKED_CUS kv heads, which cut no tile
+    if (e != hipSuccess || joins == 0) return e;
+    hipLaunchKernelGGL((packed_join_kernel<D>), dim3((unsigned)joins), dim3(256), 0, s, sh, pk, dqkv, scale,
+                       (const float*)part);
     return hipGetLastError();
   }
   hipLaunchKernelGGL((attn_bwd_dkdv_kernel<D, false, true>), packed_grid(gkv), dim3(256), 0, s, sh, pk, qkv, dout,

@@ -50,3 +50,9 @@ def test_packed_rows_beyond_one_dimension_of_a_launch():
     for t in (o, dqkv):
         for a in range(0, first, 1 << 23):
             assert bool((t[a:min(a + (1 << 23), first)] == MARK).all())
+
+@pytest.mark.parametrize("heads", [256, 300, 512, 513, 700])
+def test_more_kv_heads_than_parts(heads):
+    """Beyond 512 kv heads no tile is cut and no partial sums are joined."""
+    need_gpu()
+    check(Batch([60, 1, 0, 30], heads, heads, 64, first=1, tail=2, seed=43).run())
