@@ -1447,8 +1447,9 @@ int dkdv_split(const AttnShape& sh) {
 }
 
 // Bytes of the backward workspace before the partial sums: D, then the base-2 log-sum-exp.
+// In whole 256 bytes: the sums are stored and read as 16-byte vectors.
 int64_t bwd_ws_head(const AttnShape& sh) {
-  return 2 * (int64_t)sh.batch * sh.seq * sh.nq * (int64_t)sizeof(float);
+  return (2 * (int64_t)sh.batch * sh.seq * sh.nq * (int64_t)sizeof(float) + 255) & ~(int64_t)255;
 }
 
 template <int D>
