@@ -1563,7 +1563,8 @@ static HeadWs head_ws(int64_t T, int64_t H, int64_t V, int64_t piece) {
   // a piece's rows of E are one operand of a product, its dz another
   auto fit = [&](int64_t p) { return std::max<int64_t>(p & ~(int64_t)255, 256); };
   const int64_t most = fit((kMaxBytes - 1) / (2 * H));
-  w.fwd_piece = std::min(V, most);
+  // a product of all rows has 2^22 tiles of 256 x 256 (of 256 threads each) at most, a quarter of a launch's dimension
+  w.fwd_piece = std::min({V, most, fit(((int64_t)1 << 38) / T)});
   const int64_t by_dz = piece > 0 ? (piece + 63) / 64 * 64 : fit(kHeadDzBytes / (2 * T));
   w.bwd_piece = std::min({V, most, by_dz, std::max<int64_t>((kMaxBytes - 1) / (2 * T) / 64 * 64, 64)});
   w.ldz = (w.bwd_piece + 63) / 64 * 64;
