@@ -143,13 +143,13 @@ def _check(status: int, where: str):
         raise LsError(status, where, lib().ls_last_error().decode())
 
 
-def _p(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+def _p(t):  # (the prototypes make a pointer of it)
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream=None):
     s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    return s.cuda_stream
 
 
 def make_cfg(c: BlockConfig) -> LsBlockCfg:
@@ -242,12 +242,33 @@ def make_packed_cfg(c: PackedConfig) -> LsPackedCfg:
 
 
 def _bytes(t) -> int:
-    return t.numel() * t.element_size()
+    return 0 if t is None else t.numel() * t.element_size()
 
 
-def _need_int32(name, t, n):
-    if t.dtype != torch.int32 or t.numel() != n:
-        raise ValueError(f"{name} must hold {n} int32, not {t.numel()} {t.dtype}")
+def _need(*wanted):
+    """The library sees addresses: (name, tensor, type, number of elements) of every tensor of a call, or a ValueError.
+    Type and number None: any, the library checks the bytes.  A tensor that is None is the library's to refuse.
+    0.9 us for three tensors."""
+    on = None
+    for name, t, dtype, n in wanted:
+        if t is None:
+            continue
+        if dtype is not None and (t.dtype is not dtype or t.numel() != n):
+            raise ValueError(f"{name} must hold {n} {dtype}, not {t.numel()} {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        d = t.get_device()  # -1: not on a GPU
+        on = d if on is None or d == on else -1
+    if on is not None and (on < 0 or on != torch.cuda.current_device()):
+        raise ValueError("every tensor must be on the current GPU")
+
+
+def _packed_sizes(c):
+    """Elements of qkv and of o."""
+    return c.total * (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, c.total * c.n_q_heads * c.head_dim
+
+
+_BF16, _F32 = torch.bfloat16, torch.float32
 
 
 def ls_packed_plan_bytes(c) -> int:
@@ -257,7 +278,7 @@ def ls_packed_plan_bytes(c) -> int:
 
 def ls_packed_plan(c, cu_seqlens, plan, stream=None):
     """cu_seqlens: n_seqs + 1 int32 on the device; plan: a uint8 buffer of ls_packed_plan_bytes(c)."""
-    _need_int32("cu_seqlens", cu_seqlens, c.n_seqs + 1)
+    _need(("cu_seqlens", cu_seqlens, torch.int32, c.n_seqs + 1), ("plan", plan, None, None))
     cfg = make_packed_cfg(c)
     _check(lib().ls_packed_plan(ctypes.byref(cfg), _p(cu_seqlens), _p(plan), _bytes(plan), _stream(stream)),
            "ls_packed_plan")
@@ -265,12 +286,17 @@ def ls_packed_plan(c, cu_seqlens, plan, stream=None):
 
 def ls_packed_rope(c, plan, theta, src, dst, inverse=False, stream=None):
     """q and k of every row turned by its position; dst may be src."""
+    n, _ = _packed_sizes(c)
+    _need(("plan", plan, None, None), ("src", src, _BF16, n), ("dst", dst, _BF16, n))
     cfg = make_packed_cfg(c)
     _check(lib().ls_packed_rope(ctypes.byref(cfg), _p(plan), _bytes(plan), theta, int(inverse), _p(src), _p(dst),
                                 _stream(stream)), "ls_packed_rope")
 
 
 def ls_packed_attn_fwd(c, plan, qkv, o, lse, stream=None):
+    n, m = _packed_sizes(c)
+    _need(("plan", plan, None, None), ("qkv", qkv, _BF16, n), ("o", o, _BF16, m),
+          ("lse", lse, _F32, c.total * c.n_q_heads))
     cfg = make_packed_cfg(c)
     _check(lib().ls_packed_attn_fwd(ctypes.byref(cfg), _p(plan), _bytes(plan), _p(qkv), _p(o), _p(lse),
                                     _stream(stream)), "ls_packed_attn_fwd")
@@ -282,6 +308,10 @@ def ls_packed_attn_bwd_workspace(c) -> int:
 
 
 def ls_packed_attn_bwd(c, plan, qkv, o, lse, dout, dqkv, workspace, stream=None):
+    n, m = _packed_sizes(c)
+    _need(("plan", plan, None, None), ("qkv", qkv, _BF16, n), ("o", o, _BF16, m),
+          ("lse", lse, _F32, c.total * c.n_q_heads), ("dout", dout, _BF16, m), ("dqkv", dqkv, _BF16, n),
+          ("workspace", workspace, None, None))
     cfg = make_packed_cfg(c)
     _check(lib().ls_packed_attn_bwd(ctypes.byref(cfg), _p(plan), _bytes(plan), _p(qkv), _p(o), _p(lse), _p(dout),
                                     _p(dqkv), _p(workspace), _bytes(workspace), _stream(stream)), "ls_packed_attn_bwd")
@@ -367,7 +397,9 @@ def ls_head_loss_workspace(tokens: int, hidden: int, vocab: int, piece: int = 0)
 
 def ls_head_loss_fwd(h, embed, targets, loss, row_loss, lse, workspace, stream=None):
     T, H = h.shape
-    _need_int32("targets", targets, T)
+    _need(("h", h, _BF16, T * H), ("embed", embed, _BF16, embed.shape[0] * H), ("targets", targets, torch.int32, T),
+          ("loss", loss, _F32, 1), ("row_loss", row_loss, _F32, T), ("lse", lse, _F32, T),
+          ("workspace", workspace, None, None))
     _check(lib().ls_head_loss_fwd(T, H, embed.shape[0], _p(h), _p(embed), _p(targets), _p(loss), _p(row_loss), _p(lse),
                                   _p(workspace), _bytes(workspace), _stream(stream)), "ls_head_loss_fwd")
 
@@ -376,8 +408,10 @@ def ls_head_loss_bwd(h, embed, targets, lse, dloss, dh, d_embed, accumulate, wor
     """dloss: one fp32 or None (1); dh or d_embed may be None; d_embed: fp32, added to with
     ``accumulate``, or bf16, always overwritten."""
     T, H = h.shape
-    _need_int32("targets", targets, T)
     low = d_embed is not None and d_embed.dtype == torch.bfloat16
+    _need(("h", h, _BF16, T * H), ("embed", embed, _BF16, embed.shape[0] * H), ("targets", targets, torch.int32, T),
+          ("lse", lse, _F32, T), ("dloss", dloss, _F32, 1), ("dh", dh, _BF16, T * H),
+          ("d_embed", d_embed, _BF16 if low else _F32, embed.shape[0] * H), ("workspace", workspace, None, None))
     if low and accumulate:
         raise ValueError("a bf16 d_embed is overwritten, never added to")
     _check(lib().ls_head_loss_bwd(T, H, embed.shape[0], _p(h), _p(embed), _p(targets), _p(lse), _p(dloss), _p(dh),
