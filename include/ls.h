@@ -350,9 +350,11 @@ int ls_packed_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes
 /* Causal attention inside every sequence on q and k already rotated:
  * ls_attn_core_fwd / _bwd with the mask start of i's sequence <= j <= i.  What a
  * sequence gives does not depend on what its neighbours hold, bit for bit, nor on
- * where in the row it lies; the lengths of all sequences decide over how many
- * workgroups the sums of a long one's dk and dv are spread, and so the order in
- * which they are added.  The backward takes o and lse of the forward call; workspace:
+ * where in the row it lies.  Its o, lse and dq do not depend on the neighbours'
+ * lengths either.  Its dk and dv do, long or short: total and all lengths (for
+ * sequences of up to 64 rows, how many of those there are) decide over how many workgroups
+ * the sums of a sequence's dk and dv are spread, and so the order in which they are
+ * added.  The backward takes o and lse of the forward call; workspace:
  * at least ls_packed_attn_bwd_workspace(cfg) bytes. */
 int ls_packed_attn_fwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, const ls_bf16* qkv,
                        ls_bf16* o, float* lse, void* stream);
