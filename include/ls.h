@@ -308,7 +308,9 @@ int ls_attn_core_bwd_noalloc(const ls_block_cfg* cfg, const ls_bf16* qkv, const 
  * cu_seqlens[s+1] - 1.  Entries must not fall, start at 0 or more and end at
  * `total` or less; a sequence may be empty.  Rows before the first and behind
  * the last sequence belong to none: their inputs (whatever they hold, NaN
- * too) reach no other row, and every output of theirs is left as it was.
+ * too) reach no other row, and every output of theirs is left as it was: a buffer
+ * that served an earlier batch keeps that batch's values there, and whoever sums
+ * over all rows (the products of the weight gradients) clears o's and dqkv's first.
  * The library never reads cu_seqlens on the host.  Entries that break the rule
  * give unspecified values in the outputs, with nothing read or written outside
  * a buffer.
