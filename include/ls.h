@@ -433,7 +433,7 @@ int ls_cross_entropy(int64_t tokens, int32_t seq, int32_t vocab, ls_bf16* logits
  *   dh = c dz embed                     (bf16, summed in fp32; 0 in the rows left
  *                                        out; NULL: not wanted)
  *   d_embed (+)= c dz^T h               (fp32, added with `accumulate`; or
- *   d_embed_bf16 = c dz^T h              rounded once to bf16, without `accumulate`).
+ *   d_embed_bf16 = c dz^T h              rounded once to bf16; refused with `accumulate`).
  *
  * At most one of d_embed and d_embed_bf16; both NULL for a frozen head.  lse is the
  * forward call's, for the same h, embed and targets.

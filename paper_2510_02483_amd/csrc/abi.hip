@@ -1653,6 +1653,7 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
   if (int e = check_head(tokens, hidden, vocab, piece)) return e;
   if (!dh && !d_embed && !d_embed_bf16) return fail(LS_ERR_NULL, "dh, d_embed and d_embed_bf16 are all NULL");
   if (d_embed && d_embed_bf16) return fail(LS_ERR_UNSUPPORTED, "d_embed and d_embed_bf16 are both given");
+  if (d_embed_bf16 && accumulate) return fail(LS_ERR_UNSUPPORTED, "d_embed_bf16 is overwritten, never added to");
   const int64_t T = tokens, H = hidden, V = vocab;
   Range in[5] = {{h, (size_t)(T * H * 2), "h"},
                  {embed, (size_t)(V * H * 2), "embed"},
