@@ -247,13 +247,14 @@ def _bytes(t) -> int:
 
 def _need(*wanted):
     """The library sees addresses: (name, tensor, type, number of elements) of every tensor of a call, or a ValueError.
-    Type and number None: any, the library checks the bytes.  A tensor that is None is the library's to refuse.
+    Lengths and targets hold exactly so many, other buffers may be longer.  Type and number None: any, the library
+    checks the bytes.  A tensor that is None is the library's to refuse.
     0.9 us for three tensors."""
     on = None
     for name, t, dtype, n in wanted:
         if t is None:
             continue
-        if dtype is not None and (t.dtype is not dtype or t.numel() != n):
+        if dtype is not None and (t.dtype is not dtype or t.numel() < n or (dtype is torch.int32 and t.numel() > n)):
             raise ValueError(f"{name} must hold {n} {dtype}, not {t.numel()} {t.dtype}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")

@@ -5,7 +5,7 @@ import pytest
 
 from paper_2510_02483_amd import lib as L
 
-OK, UNSUPPORTED, WORKSPACE = 0, 3, 6
+UNSUPPORTED, WORKSPACE = 3, 6
 A = 1 << 30  # addresses are compared, never followed, by a call that refuses
 
 
