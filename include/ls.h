@@ -320,8 +320,8 @@ int ls_attn_core_bwd_noalloc(const ls_block_cfg* cfg, const ls_bf16* qkv, const 
  * As there, NaN or infinities in a sequence's k and v may reach all rows of that
  * sequence (a masked probability is 0, and 0 x NaN is NaN); they reach no other.
  * They may exceed 2 GiB.  head_dim is 64 or a multiple of 8 from 72 to 128 (heads
- * between 64 and 128 are stored as they are and cost what heads of 128 do in the
- * attention); total and n_seqs < 2^28, total x
+ * between 64 and 128 are stored as they are, and the attention runs the matrix products of
+ * heads of 128 for them); total and n_seqs < 2^28, total x
  * n_q_heads < 2^31 and a row of qkv holds less than 2^20 features. */
 typedef struct {
   int64_t total;

@@ -99,7 +99,7 @@ constexpr int MAX_DH_SLICES = 32;
 // Slices of K of the head's dh (EPI_DH): its tile rows are as many as the device's
 // number of rows needs, and where those leave workgroups of the launch without a
 // tile, they take more slices, as many as the partial sums' room holds (gradients of
-// 4096 rows of which a fifth have a target, 3072 x 128256: 3.52 -> 2.04 ms).
+// 4096 rows of which a fifth have a target, 3072 x 128256: 3.52 -> 2.03 ms).
 __host__ __device__ inline int dh_slices(const GemmArgs& p, int M, int bm, int bn) {
   if (p.fill == 0 || M <= 0) return p.ksplit;
   const int tiles = ((M + bm - 1) / bm) * ((p.N + bn - 1) / bn);
@@ -427,8 +427,9 @@ LS_DEV void lse_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw,
 // target is out of range.  One rounding, to bf16, as the operand of the
 // gradients' products; the loss's factor comes after them, in fp32: with it, the
 // target's entry, the largest, would be one number close to -dloss / N in every
-// row and carry the same rounding error in all, which no sum evens out (errors
-// of dh and dE 0.0039 of their norm against 0.0024 so).  exp2 flushes
+// row and carry the same rounding error in all, which no sum evens out (509 rows,
+// 768 x 32003: errors of dh and dE 0.0039 of their norm, 0.0017 so, which is the
+// outputs' own rounding).  exp2 flushes
 // probabilities below 2^-126.
 struct DzRow {
   float l2;
