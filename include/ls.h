@@ -262,6 +262,33 @@ int ls_adamw_step(int64_t n, int64_t n_decay, const ls_adamw_cfg* cfg, float* ma
                   ls_bf16* param, const float* grad, float* m, float* v, float* grad_norm,
                   void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- gradients of many tensors ------------------------------------------------------
+ *
+ * Clipping by the global norm where the gradients are separate tensors (ls_adamw_step
+ * clips one flat array):
+ *
+ *   norm = sqrt(sum over all tensors of g^2)                       (one fp32 on the device)
+ *   out[i] = grads[i] min(1, max_norm / (norm + 1e-6)).
+ *
+ * Two calls, so that a caller can add up the squares of several GPUs' norms between them.
+ * Lists are HOST arrays of n (1 .. 2^20) entries, read before the calls return; tensors
+ * are dense, 16-byte aligned, fp32 or bf16 mixed at will, and may be empty (data is not
+ * looked at then).  The norm is summed in fp64 in an order that depends on the sizes only.
+ * ls_grad_clip: out NULL clips in place; otherwise out[i] has grads[i]'s number of
+ * elements, is of either type (one rounding) and is grads[i] itself, in the same type, or overlaps
+ * none of grads and out.  max_norm > 0.  A norm of NaN makes every result NaN, an infinite one
+ * every finite gradient 0 and the others NaN. */
+typedef enum { LS_F32 = 0, LS_BF16 = 1 } ls_dtype;
+typedef struct {
+  void* data;
+  int64_t numel;
+  int32_t dtype; /* ls_dtype */
+} ls_tensor;
+size_t ls_grad_norm_workspace(void);
+int ls_grad_norm(int32_t n, const ls_tensor* grads, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+int ls_grad_clip(int32_t n, const ls_tensor* grads, const float* norm, float max_norm, const ls_tensor* out,
+                 void* stream);
+
 /* ---- single-kernel entry points (used for per-kernel parity) ---------------- */
 
 /* Causal attention core on a packed projection buffer.
@@ -349,6 +376,35 @@ int ls_packed_plan(const ls_packed_cfg* cfg, const int32_t* cu_seqlens, void* pl
 int ls_packed_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, float theta, int inverse,
                    const ls_bf16* src, ls_bf16* dst, void* stream);
 
+/* RMSNorm of every q and k head and the rotation behind it, in one pass: for a
+ * head x of head_dim features and the gain g of its kind (q_gain or k_gain,
+ * [head_dim] bf16, shared by the heads of a kind),
+ *
+ *   r = (mean x^2 + eps)^-1/2,  y = R_p (x r g),
+ *
+ * R_p the rotation of ls_packed_rope.  eps >= 0.  dst == src works in place and leaves v
+ * alone; otherwise the buffers must not overlap and v is copied.  Rows of no
+ * sequence are left as they were.
+ *
+ * Backward, for the gradient dy of y (and of v): dn = R_p^-1 dy, a = g dn,
+ *
+ *   dx = r a - x r^3 <a, x> / head_dim;  dq_gain, dk_gain (+)= sum over rows and heads of dn x r
+ *
+ * ([head_dim] fp32, NULL: not wanted; both NULL: the workspace is not used).
+ * src is the forward call's (so the forward pass of a training step works out of place), r is
+ * formed again from it.  dx == dy works in place; otherwise v's part is copied.
+ * Rows of no sequence add nothing to the gains' gradients, whatever they hold.
+ * Every output is deterministic.  workspace: at least
+ * ls_packed_qk_norm_rope_bwd_workspace(cfg) bytes. */
+int ls_packed_qk_norm_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, float theta, float eps,
+                           const ls_bf16* q_gain, const ls_bf16* k_gain, const ls_bf16* src, ls_bf16* dst,
+                           void* stream);
+size_t ls_packed_qk_norm_rope_bwd_workspace(const ls_packed_cfg* cfg);
+int ls_packed_qk_norm_rope_bwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, float theta, float eps,
+                               const ls_bf16* q_gain, const ls_bf16* k_gain, const ls_bf16* src, const ls_bf16* dy,
+                               ls_bf16* dx, float* dq_gain, float* dk_gain, int accumulate, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
 /* Causal attention inside every sequence on q and k already rotated:
  * ls_attn_core_fwd / _bwd with the mask start of i's sequence <= j <= i.  What a
  * sequence gives does not depend on what its neighbours hold, bit for bit, nor on
@@ -364,6 +420,27 @@ size_t ls_packed_attn_bwd_workspace(const ls_packed_cfg* cfg);
 int ls_packed_attn_bwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, const ls_bf16* qkv,
                        const ls_bf16* o, const float* lse, const ls_bf16* dout, ls_bf16* dqkv, void* workspace,
                        size_t workspace_bytes, void* stream);
+
+/* The same attention with other scores and a window: of query i and key j in one
+ * sequence,
+ *
+ *   s = scale q.k (cap 0) or cap tanh(scale q.k / cap),  softmax over i - window < j <= i.
+ *
+ * A capped score lies within -cap .. cap and carries an error of up to 2^-21 cap
+ * beside that of q.k.  All of *score 0 is ls_packed_attn_fwd / _bwd, bit for bit.  lse is that
+ * of these scores; plan, buffers, rows of no sequence, what neighbours change and the workspace
+ * (ls_packed_attn_bwd_workspace) are as there.  A window saves the work outside
+ * it (in whole tiles of 64 keys or queries); one plan serves calls with any. */
+typedef struct {
+  float scale;    /* 0: 1/sqrt(head_dim); positive */
+  float cap;      /* 0: none; 0.01 .. 1000, scale / cap at most 1e30 */
+  int32_t window; /* positions that a query sees, itself included; 0: all before it */
+} ls_score_cfg;
+int ls_packed_score_attn_fwd(const ls_packed_cfg* cfg, const ls_score_cfg* score, const void* plan, size_t plan_bytes,
+                             const ls_bf16* qkv, ls_bf16* o, float* lse, void* stream);
+int ls_packed_score_attn_bwd(const ls_packed_cfg* cfg, const ls_score_cfg* score, const void* plan, size_t plan_bytes,
+                             const ls_bf16* qkv, const ls_bf16* o, const float* lse, const ls_bf16* dout,
+                             ls_bf16* dqkv, void* workspace, size_t workspace_bytes, void* stream);
 
 /* RMSNorm over rows of length `hidden`: h = x * r * gamma, r = (mean x^2 + eps)^-1/2.
  * x, h: [rows, hidden] bf16; r: [rows] fp32. */
@@ -478,7 +555,8 @@ int ls_gemm_tile_override(int32_t bm, int32_t bn);
  * "output projection", "gate/up projection", "down projection", "dact",
  * "dWd", "dh2", "dWg/dWu", "rmsnorm bwd", "dO", "dWo", "attention bwd",
  * "dh1", "dWqkv", "packed plan", "packed rope", "packed attention fwd",
- * "packed attention bwd", "head loss logits", "head loss rows", "head loss gather",
+ * "packed attention bwd", "packed qk norm rope", "packed qk norm rope bwd", "packed score attention fwd",
+ * "packed score attention bwd", "gradient norm", "gradient clip", "head loss logits", "head loss rows", "head loss gather",
  * "head loss dz", "head loss dh", "head loss dE", "head loss scatter", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
  * "logits", "cross-entropy", "dh head", "dE head", "loss", "embedding bwd",
  * and "adamw" for ls_adamw_step),

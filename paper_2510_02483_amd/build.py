@@ -16,7 +16,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libls.so")
-SOURCES = ("abi.hip", "gemm.hip", "gemm_nt.hip", "gemm_nn.hip", "gemm_tn.hip", "gemm_head.hip", "attention.hip", "packed.hip", "norm.hip", "lmhead.hip", "headloss.hip", "optim.hip", "headpad.hip")
+SOURCES = ("abi.hip", "gemm.hip", "gemm_nt.hip", "gemm_nn.hip", "gemm_tn.hip", "gemm_head.hip", "attention.hip", "attention_score.hip", "packed.hip", "qknorm.hip", "norm.hip", "lmhead.hip", "headloss.hip", "optim.hip", "gradnorm.hip", "headpad.hip")
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -31,7 +31,7 @@ CFLAGS = [
 # The attention kernels keep their matrix-product accumulators in ordinary
 # vector registers (the softmax works on them), which leaves the accumulation
 # registers free for values that only the matrix cores read.
-EXTRA = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("attention.hip", "attention_score.hip")}
 
 
 def build(verbose: bool = False) -> str:

@@ -82,6 +82,14 @@ class PackedConfig:
 
 
 @dataclass(frozen=True)
+class ScoreConfig:
+    """The scores of ls_packed_score_attn_*: cap tanh(scale q.k / cap) over the last `window` positions."""
+    scale: float = 0.0   # 0: 1 / sqrt(head_dim)
+    cap: float = 0.0     # 0: none
+    window: int = 0      # positions that a query sees, itself included; 0: all before it
+
+
+@dataclass(frozen=True)
 class StackConfig:
     """A stack of identical blocks between a tied token embedding and a final
     RMSNorm + LM head, trained on next-token cross-entropy (Section 2.4)."""

@@ -1,5 +1,6 @@
 // C ABI of the decoder-block library: argument validation (all of it before
 // any HIP call) and the orchestration of the kernels for each sub-layer.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -1139,6 +1140,64 @@ int ls_packed_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes
   return LS_OK;
 }
 
+static int check_qk_norm(float theta, float eps) {
+  if (!(theta > 1.0f) || !(theta <= 3.4e38f)) return fail(LS_ERR_SHAPE, "theta must exceed 1 and be finite");
+  if (!(eps >= 0.0f) || !(eps <= 3.4e38f)) return fail(LS_ERR_SHAPE, "eps must be >= 0 and finite");
+  return LS_OK;
+}
+
+int ls_packed_qk_norm_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, float theta, float eps,
+                           const ls_bf16* q_gain, const ls_bf16* k_gain, const ls_bf16* src, ls_bf16* dst,
+                           void* stream) {
+  ls::PackedShape p;
+  if (int e = check_packed_cfg(cfg, p)) return e;
+  if (int e = check_qk_norm(theta, eps)) return e;
+  const size_t bytes = packed_qkv_bytes(p), gain = (size_t)p.d * 2;
+  const Range in[] = {{plan, plan_bytes, "plan"}, {q_gain, gain, "q_gain"}, {k_gain, gain, "k_gain"}, {src, bytes, "src"}};
+  const Range out[] = {{dst, bytes, "dst"}};
+  if (int e = check_ranges(in, src == dst ? 3 : 4, out, 1)) return e;
+  if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("packed qk norm rope", st,
+          ls::packed_qk_norm_rope(p, plan, (double)theta, eps, (const bf16_t*)q_gain, (const bf16_t*)k_gain,
+                                  (const bf16_t*)src, (bf16_t*)dst, st));
+  return LS_OK;
+}
+
+size_t ls_packed_qk_norm_rope_bwd_workspace(const ls_packed_cfg* cfg) {
+  ls::PackedShape p;
+  return check_packed_cfg(cfg, p) ? 0 : ls::packed_qk_norm_rope_bwd_workspace(p);
+}
+
+int ls_packed_qk_norm_rope_bwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, float theta, float eps,
+                               const ls_bf16* q_gain, const ls_bf16* k_gain, const ls_bf16* src, const ls_bf16* dy,
+                               ls_bf16* dx, float* dq_gain, float* dk_gain, int accumulate, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  ls::PackedShape p;
+  if (int e = check_packed_cfg(cfg, p)) return e;
+  if (int e = check_qk_norm(theta, eps)) return e;
+  const size_t bytes = packed_qkv_bytes(p), gain = (size_t)p.d * 2;
+  const Range in[] = {{plan, plan_bytes, "plan"},
+                      {q_gain, gain, "q_gain"},
+                      {k_gain, gain, "k_gain"},
+                      {src, bytes, "src"},
+                      {dy, bytes, "dy"}};
+  Range out[4] = {{dx, bytes, "dx"}, {workspace, workspace_bytes, "workspace"}};
+  size_t nout = 2;
+  if (dq_gain) out[nout++] = {dq_gain, 2 * gain, "dq_gain"};
+  if (dk_gain) out[nout++] = {dk_gain, 2 * gain, "dk_gain"};
+  if (int e = check_ranges(in, dy == dx ? 4 : 5, out, nout)) return e;
+  if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  const size_t need = ls::packed_qk_norm_rope_bwd_workspace(p);
+  if (workspace_bytes < need) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, need);
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("packed qk norm rope bwd", st,
+          ls::packed_qk_norm_rope_bwd(p, plan, (double)theta, eps, (const bf16_t*)q_gain, (const bf16_t*)k_gain,
+                                      (const bf16_t*)src, (const bf16_t*)dy, (bf16_t*)dx, dq_gain, dk_gain,
+                                      accumulate != 0, workspace, st));
+  return LS_OK;
+}
+
 int ls_packed_attn_fwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes, const ls_bf16* qkv, ls_bf16* o,
                        float* lse, void* stream) {
   ls::PackedShape p;
@@ -1176,6 +1235,66 @@ int ls_packed_attn_bwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_b
   LS_STEP("packed attention bwd", st,
           ls::packed_attn_bwd(p, plan, (const bf16_t*)qkv, (const bf16_t*)o, lse, (const bf16_t*)dout, (bf16_t*)dqkv,
                               workspace, st));
+  return LS_OK;
+}
+
+static int check_score_cfg(const ls_score_cfg* c, const ls::PackedShape& p, ls::ScoreShape& out, bool& plain) {
+  if (!c) return fail(LS_ERR_NULL, "score is NULL");
+  if (!(c->scale >= 0.0f) || !(c->scale <= 3.4e38f)) return fail(LS_ERR_SHAPE, "scale must be positive and finite, or 0");
+  if (!(c->cap >= 0.0f)) return fail(LS_ERR_SHAPE, "cap must be positive, or 0");
+  if (c->cap > 0.0f && (c->cap < 0.01f || c->cap > 1000.0f))
+    return fail(LS_ERR_UNSUPPORTED, "cap (%g) outside 0.01 .. 1000", (double)c->cap);
+  if (c->window < 0) return fail(LS_ERR_SHAPE, "window must be positive, or 0");
+  out.scale = c->scale > 0.0f ? c->scale : 1.0f / sqrtf((float)p.d);
+  out.cap = c->cap;
+  out.window = c->window > 0 ? (int)std::min<int64_t>(c->window, p.total) : (int)p.total;
+  if (c->cap > 0.0f && !(out.scale / out.cap <= 1e30f)) return fail(LS_ERR_SHAPE, "scale / cap must not exceed 1e30");
+  plain = c->scale == 0.0f && c->cap == 0.0f && out.window >= p.total;
+  return LS_OK;
+}
+
+int ls_packed_score_attn_fwd(const ls_packed_cfg* cfg, const ls_score_cfg* score, const void* plan, size_t plan_bytes,
+                             const ls_bf16* qkv, ls_bf16* o, float* lse, void* stream) {
+  ls::PackedShape p;
+  ls::ScoreShape c;
+  bool plain;
+  if (int e = check_packed_cfg(cfg, p)) return e;
+  if (int e = check_score_cfg(score, p, c, plain)) return e;
+  if (plain) return ls_packed_attn_fwd(cfg, plan, plan_bytes, qkv, o, lse, stream);
+  const Range in[] = {{plan, plan_bytes, "plan"}, {qkv, packed_qkv_bytes(p), "qkv"}};
+  const Range out[] = {{o, packed_o_bytes(p), "o"}, {lse, (size_t)p.nq * p.total * 4, "lse"}};
+  if (int e = check_ranges(in, 2, out, 2)) return e;
+  if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("packed score attention fwd", st,
+          ls::packed_score_attn_fwd(p, c, plan, (const bf16_t*)qkv, (bf16_t*)o, lse, st));
+  return LS_OK;
+}
+
+int ls_packed_score_attn_bwd(const ls_packed_cfg* cfg, const ls_score_cfg* score, const void* plan, size_t plan_bytes,
+                             const ls_bf16* qkv, const ls_bf16* o, const float* lse, const ls_bf16* dout,
+                             ls_bf16* dqkv, void* workspace, size_t workspace_bytes, void* stream) {
+  ls::PackedShape p;
+  ls::ScoreShape c;
+  bool plain;
+  if (int e = check_packed_cfg(cfg, p)) return e;
+  if (int e = check_score_cfg(score, p, c, plain)) return e;
+  if (plain)
+    return ls_packed_attn_bwd(cfg, plan, plan_bytes, qkv, o, lse, dout, dqkv, workspace, workspace_bytes, stream);
+  const Range in[] = {{plan, plan_bytes, "plan"},
+                      {qkv, packed_qkv_bytes(p), "qkv"},
+                      {o, packed_o_bytes(p), "o"},
+                      {lse, (size_t)p.nq * p.total * 4, "lse"},
+                      {dout, packed_o_bytes(p), "dout"}};
+  const Range out[] = {{dqkv, packed_qkv_bytes(p), "dqkv"}, {workspace, workspace_bytes, "workspace"}};
+  if (int e = check_ranges(in, 5, out, 2)) return e;
+  if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  const size_t need = ls::packed_attn_bwd_workspace(p);
+  if (workspace_bytes < need) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, need);
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("packed score attention bwd", st,
+          ls::packed_score_attn_bwd(p, c, plan, (const bf16_t*)qkv, (const bf16_t*)o, lse, (const bf16_t*)dout,
+                                    (bf16_t*)dqkv, workspace, st));
   return LS_OK;
 }
 
@@ -1773,6 +1892,94 @@ int ls_adamw_step(int64_t n, int64_t n_decay, const ls_adamw_cfg* cfg, float* ma
   ls::AdamwHyper h{cfg->lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->weight_decay, cfg->max_norm, cfg->step};
   const hipStream_t st = (hipStream_t)stream;
   LS_STEP("adamw", st, ls::adamw_step(n, n_decay, h, master, (bf16_t*)param, grad, m, v, grad_norm, workspace, st));
+  return LS_OK;
+}
+
+// ---- gradients of many tensors -----------------------------------------------------------
+
+size_t ls_grad_norm_workspace(void) { return ls::grad_norm_workspace(); }
+
+// The list as the kernels take it; room for `n` was checked.
+static int check_tensors(int32_t n, const ls_tensor* t, const char* name, std::vector<ls::GradTensor>& out) {
+  if (!t) return fail(LS_ERR_NULL, "%s is NULL", name);
+  for (int32_t i = 0; i < n; ++i) {
+    if (t[i].numel < 0 || t[i].numel >= (int64_t)1 << 40)
+      return fail(LS_ERR_SHAPE, "%s[%d]: numel (%lld) outside 0 .. 2^40 - 1", name, i, (long long)t[i].numel);
+    if (t[i].dtype != LS_F32 && t[i].dtype != LS_BF16)
+      return fail(LS_ERR_UNSUPPORTED, "%s[%d]: dtype %d is neither LS_F32 nor LS_BF16", name, i, t[i].dtype);
+    if (t[i].numel > 0 && !t[i].data) return fail(LS_ERR_NULL, "%s[%d] is NULL", name, i);
+    if (t[i].numel > 0 && misaligned(t[i].data)) return fail(LS_ERR_ALIGN, "%s[%d] is not 16-byte aligned", name, i);
+    out.push_back(ls::GradTensor{t[i].data, t[i].numel, t[i].dtype == LS_BF16});
+  }
+  return LS_OK;
+}
+static int check_tensor_count(int32_t n) {
+  if (n <= 0 || n > 1 << 20) return fail(LS_ERR_SHAPE, "n (%d) outside 1 .. 2^20", n);
+  return LS_OK;
+}
+
+int ls_grad_norm(int32_t n, const ls_tensor* grads, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int e = check_tensor_count(n)) return e;
+  std::vector<ls::GradTensor> g;
+  try {
+    g.reserve((size_t)n);
+  } catch (...) {
+    return fail(LS_ERR_WORKSPACE, "no host memory for %d tensors", n);
+  }
+  if (int e = check_tensors(n, grads, "grads", g)) return e;
+  const Range out[] = {{norm, 4, "norm"}, {workspace, workspace_bytes, "workspace"}};
+  if (int e = check_ranges(nullptr, 0, out, 2)) return e;
+  for (const ls::GradTensor& t : g)
+    for (const Range& r : out)
+      if (overlaps(r, Range{t.p, (size_t)t.n * (t.bf16 ? 2 : 4), ""})) return fail(LS_ERR_ALIAS, "%s overlaps a gradient", r.name);
+  if (workspace_bytes < ls::grad_norm_workspace())
+    return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, ls::grad_norm_workspace());
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("gradient norm", st, ls::grad_norm(n, g.data(), norm, workspace, st));
+  return LS_OK;
+}
+
+int ls_grad_clip(int32_t n, const ls_tensor* grads, const float* norm, float max_norm, const ls_tensor* out, void* stream) {
+  if (int e = check_tensor_count(n)) return e;
+  if (!(max_norm > 0.0f) || !(max_norm <= 3.4e38f)) return fail(LS_ERR_SHAPE, "max_norm must be positive and finite");
+  struct Span {
+    uintptr_t from, to;
+    bool written;
+  };
+  std::vector<ls::GradTensor> g, o;
+  std::vector<Span> spans;
+  try {
+    g.reserve((size_t)n);
+    o.reserve((size_t)n);
+    spans.reserve(2 * (size_t)n + 1);
+  } catch (...) {
+    return fail(LS_ERR_WORKSPACE, "no host memory for %d tensors", n);
+  }
+  if (int e = check_tensors(n, grads, "grads", g)) return e;
+  if (int e = check_tensors(n, out ? out : grads, out ? "out" : "grads", o)) return e;
+  const Range r[] = {{norm, 4, "norm"}};
+  if (int e = check_ranges(r, 1, nullptr, 0)) return e;
+  auto span = [](const ls::GradTensor& t, bool written) {
+    return Span{(uintptr_t)t.p, (uintptr_t)t.p + (size_t)t.n * (t.bf16 ? 2 : 4), written};
+  };
+  for (int32_t i = 0; i < n; ++i) {
+    if (g[i].n != o[i].n)
+      return fail(LS_ERR_SHAPE, "out[%d] has %lld elements, its gradient %lld", i, (long long)o[i].n, (long long)g[i].n);
+    if (g[i].n == 0) continue;
+    spans.push_back(span(o[i], true));
+    if (g[i].p != o[i].p || g[i].bf16 != o[i].bf16) spans.push_back(span(g[i], false));  // (else its own result)
+  }
+  spans.push_back(Span{(uintptr_t)norm, (uintptr_t)norm + 4, false});
+  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
+  uintptr_t read = 0, written = 0;  // ends of what lies before
+  for (const Span& s : spans) {
+    if (s.from < written || (s.written && s.from < read))
+      return fail(LS_ERR_ALIAS, "a result overlaps another, a gradient that is not its own, or norm");
+    uintptr_t& end = s.written ? written : read;
+    end = std::max(end, s.to);
+  }
+  const hipStream_t st = (hipStream_t)stream;
+  LS_STEP("gradient clip", st, ls::grad_clip(n, g.data(), norm, max_norm, o.data(), st));
   return LS_OK;
 }
 

@@ -145,11 +145,31 @@ hipError_t packed_plan(const PackedShape& p, const int32_t* cu, void* plan, hipS
 // dst = q and k of src turned (v copied unless dst == src); rows of no sequence are left alone.
 hipError_t packed_rope(const PackedShape& p, const void* plan, double theta, int inverse, const bf16_t* src,
                        bf16_t* dst, hipStream_t s);
+// dst = q and k of src normed per head (gains gq, gk of d features) and turned (v copied unless dst == src).
+hipError_t packed_qk_norm_rope(const PackedShape& p, const void* plan, double theta, float eps, const bf16_t* gq,
+                               const bf16_t* gk, const bf16_t* src, bf16_t* dst, hipStream_t s);
+// dx = its gradient for src, from dy (may be dx); dgq and dgk (either may be null) (+)= those of the gains.
+size_t packed_qk_norm_rope_bwd_workspace(const PackedShape& p);
+hipError_t packed_qk_norm_rope_bwd(const PackedShape& p, const void* plan, double theta, float eps, const bf16_t* gq,
+                                   const bf16_t* gk, const bf16_t* src, const bf16_t* dy, bf16_t* dx, float* dgq,
+                                   float* dgk, int accumulate, void* ws, hipStream_t s);
 hipError_t packed_attn_fwd(const PackedShape& p, const void* plan, const bf16_t* qkv, bf16_t* o, float* lse,
                            hipStream_t s);
 size_t packed_attn_bwd_workspace(const PackedShape& p);
 hipError_t packed_attn_bwd(const PackedShape& p, const void* plan, const bf16_t* qkv, const bf16_t* o, const float* lse,
                            const bf16_t* dout, bf16_t* dqkv, void* ws, hipStream_t s);
+
+// The same attention with scores cap tanh(scale q.k / cap) (cap 0: scale q.k) over the last `window` positions
+// (1 .. total); workspace: packed_attn_bwd_workspace.
+struct ScoreShape {
+  float scale, cap;
+  int window;
+};
+hipError_t packed_score_attn_fwd(const PackedShape& p, const ScoreShape& c, const void* plan, const bf16_t* qkv,
+                                 bf16_t* o, float* lse, hipStream_t s);
+hipError_t packed_score_attn_bwd(const PackedShape& p, const ScoreShape& c, const void* plan, const bf16_t* qkv,
+                                 const bf16_t* o, const float* lse, const bf16_t* dout, bf16_t* dqkv, void* ws,
+                                 hipStream_t s);
 
 // ---- padded head layout (64 < d < 128 held in 128-wide slots) -------------------
 // Feature s of a head sits at slot s (s < d/2) or dp/2 + s - d/2; other slots are zero.
@@ -189,6 +209,19 @@ hipError_t head_gather(int64_t T, int H, int V, const int32_t* targets, const fl
 // dh[t] = coef dhc[slot[t]] rounded to bf16, 0 for a row without a target.
 hipError_t head_scatter(int64_t T, int H, const int32_t* slot, const float* coef, const float* dhc, bf16_t* dh,
                         hipStream_t s);
+
+// ---- gradients of many tensors ------------------------------------------------------
+constexpr int GN_TENSORS = 96;  // tensors that one launch takes
+struct GradTensor {
+  void* p;
+  int64_t n;
+  bool bf16;
+};
+// norm = the L2 norm of all n tensors together; ws: grad_norm_workspace() bytes.
+size_t grad_norm_workspace();
+hipError_t grad_norm(int n, const GradTensor* g, float* norm, void* ws, hipStream_t s);
+// out[i] = g[i] min(1, max_norm / (norm + 1e-6)), out[i] of as many elements as g[i], or g[i] itself.
+hipError_t grad_clip(int n, const GradTensor* g, const float* norm, float max_norm, const GradTensor* out, hipStream_t s);
 
 // ---- optimizer ------------------------------------------------------------------
 struct AdamwHyper {

@@ -1,0 +1,288 @@
+// Queries and keys normed per head and turned by their position, in one pass over a
+// packed projection buffer, and its backward pass.
+//
+// For a head x of d features with gain g, at position p of its sequence:
+//   r = (mean x^2 + eps)^-1/2,  n = r g x,  y = R_p n
+// (R_p turns the pairs (i, i + d/2) by p theta^(-2i/d)).  Backward, for dy:
+//   dn = R_p^T dy,  a = g dn,  dx = r (a - x r <a, x r> / d),  dg = sum over rows and heads of r dn x.
+// r is formed again from x, which the backward pass reads anyhow: nothing is saved.
+//
+// A wave takes a row; G lanes (4, 8 or 16) take a head, lane c of them V pairs: features
+// V c .. and d/2 + V c .., so that loads and stores are V bf16 wide, sums over a head
+// stay in G neighbouring lanes (lane swaps of the vector unit) and 64 / G heads are
+// worked on at once.  V = 8 where a head's half is a multiple of 8, else 4; lanes past a
+// head's features, and past the last head, work on zeros.
+//
+// Bound by HBM bandwidth: every row is read and written once, all sums in fp32, one
+// rounding to bf16.
+#include <math.h>
+
+#include <algorithm>
+
+#include "packed.h"
+
+namespace ls {
+
+namespace {
+
+constexpr int QKN_WAVES = 4;
+constexpr int QKN_PARTS = 1024;  // most workgroups, and rows of partial gain gradients, of the backward pass
+constexpr int SUM_GROUPS = 16;   // threads that share a column of those
+
+template <int CTRL>
+LS_DEV float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// Sum over the G lanes of a head (all lanes active): within quads, across the halves of
+// eight lanes, of sixteen (mirrored: after the steps before, the lanes there agree).
+template <int G>
+LS_DEV float head_sum(float v) {
+  v += dpp<0xB1>(v);
+  v += dpp<0x4E>(v);
+  if constexpr (G >= 8) v += dpp<0x141>(v);
+  if constexpr (G >= 16) v += dpp<0x140>(v);
+  return v;
+}
+
+// V features of either half of a head, and the cos and sin of their angles.
+template <int V>
+struct Pairs {
+  float a[V], b[V];
+};
+template <int V>
+LS_DEV Pairs<V> load_pairs(const bf16_t* p, int half, bool ok) {
+  typedef uint32_t words __attribute__((ext_vector_type(V / 2)));
+  words u{}, w{};
+  if (ok) {
+    u = *(const words*)p;
+    w = *(const words*)(p + half);
+  }
+  Pairs<V> x;
+#pragma unroll
+  for (int e = 0; e < V / 2; ++e) {
+    x.a[2 * e] = bf_lo(u[e]);
+    x.a[2 * e + 1] = bf_hi(u[e]);
+    x.b[2 * e] = bf_lo(w[e]);
+    x.b[2 * e + 1] = bf_hi(w[e]);
+  }
+  return x;
+}
+template <int V>
+LS_DEV void store_pairs(bf16_t* p, int half, const Pairs<V>& x) {
+  typedef uint32_t words __attribute__((ext_vector_type(V / 2)));
+  words u, w;
+#pragma unroll
+  for (int e = 0; e < V / 2; ++e) {
+    u[e] = pack_bf2(x.a[2 * e], x.a[2 * e + 1]);
+    w[e] = pack_bf2(x.b[2 * e], x.b[2 * e + 1]);
+  }
+  *(words*)p = u;
+  *(words*)(p + half) = w;
+}
+// The row's angles, one per lane in fp64 as turns without their whole part (in fp32 the
+// fraction of a far position's angle would be lost), then handed to the lanes of the pairs.
+template <int V>
+LS_DEV Pairs<V> row_turns(double turns, int pos, int c) {
+  const double t = pos * turns;
+  float sn, cs;
+  sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
+  Pairs<V> out;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    out.a[e] = __shfl(cs, V * c + e);
+    out.b[e] = __shfl(sn, V * c + e);
+  }
+  return out;
+}
+LS_DEV double turns_of(int pair, int half, double log2_theta) {
+  return exp2(-(double)(pair % half) / half * log2_theta) * 0.15915494309189533577;
+}
+// v of one row goes along where the result lies elsewhere.
+LS_DEV void copy_v(const bf16_t* src, bf16_t* dst, int n, int lane) {
+  for (int i = lane; i < n / 8; i += 64) ((u32x4*)dst)[i] = ((const u32x4*)src)[i];
+}
+
+template <int V, int G>
+__global__ __launch_bounds__(64 * QKN_WAVES) void qk_norm_rope_kernel(int total, int nq, int nkv, int d, float eps,
+                                                                      double log2_theta,
+                                                                      const int32_t* __restrict__ pos,
+                                                                      const bf16_t* __restrict__ gq,
+                                                                      const bf16_t* __restrict__ gk, const bf16_t* src,
+                                                                      bf16_t* dst) {
+  constexpr int HPW = 64 / G;
+  const int lane = threadIdx.x & 63, half = d / 2, c = lane % G, h0 = lane / G;
+  const bool in = V * c < half;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * d;
+  const double turns = turns_of(lane, half, log2_theta);
+  const Pairs<V> gains[2] = {load_pairs<V>(gq + V * c, half, in), load_pairs<V>(gk + V * c, half, in)};
+  for (int64_t row = (int64_t)blockIdx.x * QKN_WAVES + (threadIdx.x >> 6); row < total;
+       row += (int64_t)gridDim.x * QKN_WAVES) {
+    const int p = pos[row];
+    if (p < 0 || p > row) continue;
+    const Pairs<V> cs = row_turns<V>(turns, p, c);
+    auto heads = [&](int first, int n, const Pairs<V>& g) {
+      for (int hb = 0; hb < n; hb += HPW) {
+        const bool ok = in && hb + h0 < n;
+        const int64_t at = row * ld + (int64_t)(first + hb + h0) * d + V * c;
+        Pairs<V> x = load_pairs<V>(src + at, half, ok);
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
+        const float r = 1.0f / sqrtf(head_sum<G>(ss) / (float)d + eps);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float a = x.a[e] * r * g.a[e], b = x.b[e] * r * g.b[e];
+          x.a[e] = a * cs.a[e] - b * cs.b[e];
+          x.b[e] = a * cs.b[e] + b * cs.a[e];
+        }
+        if (ok) store_pairs<V>(dst + at, half, x);
+      }
+    };
+    heads(0, nq, gains[0]);
+    heads(nq, nkv, gains[1]);
+    if (src != dst) copy_v(src + row * ld + (int64_t)(nq + nkv) * d, dst + row * ld + (int64_t)(nq + nkv) * d, nkv * d, lane);
+  }
+}
+
+// A workgroup's sums for the gains' gradients, of the rows that its waves take, go to
+// part[blockIdx.x][2d] (q's, then k's), which gain_sum_kernel adds.  Sums over a lane's rows
+// and heads, then over the lanes of the same features, then over the waves: a fixed
+// order.
+template <int V, int G>
+__global__ __launch_bounds__(64 * QKN_WAVES) void qk_norm_rope_bwd_kernel(
+    int total, int nq, int nkv, int d, float eps, double log2_theta, const int32_t* __restrict__ pos,
+    const bf16_t* __restrict__ gq, const bf16_t* __restrict__ gk, const bf16_t* __restrict__ src, const bf16_t* dy,
+    bf16_t* dx, float* __restrict__ part) {
+  constexpr int HPW = 64 / G;
+  __shared__ float red[QKN_WAVES][2][2 * V * G];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = d / 2, c = lane % G, h0 = lane / G;
+  const bool in = V * c < half;
+  const int64_t ld = (int64_t)(nq + 2 * nkv) * d;
+  const double turns = turns_of(lane, half, log2_theta);
+  const Pairs<V> gains[2] = {load_pairs<V>(gq + V * c, half, in), load_pairs<V>(gk + V * c, half, in)};
+  Pairs<V> sums[2] = {};
+  for (int64_t row = (int64_t)blockIdx.x * QKN_WAVES + wave; row < total; row += (int64_t)gridDim.x * QKN_WAVES) {
+    const int p = pos[row];
+    if (p < 0 || p > row) continue;
+    const Pairs<V> cs = row_turns<V>(turns, p, c);
+    auto heads = [&](int first, int n, const Pairs<V>& g, Pairs<V>& sum) {
+      for (int hb = 0; hb < n; hb += HPW) {
+        const bool ok = in && hb + h0 < n;
+        const int64_t at = row * ld + (int64_t)(first + hb + h0) * d + V * c;
+        const Pairs<V> x = load_pairs<V>(src + at, half, ok), t = load_pairs<V>(dy + at, half, ok);
+        Pairs<V> dn;
+        float ss = 0.f, dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          dn.a[e] = t.a[e] * cs.a[e] + t.b[e] * cs.b[e];
+          dn.b[e] = t.b[e] * cs.a[e] - t.a[e] * cs.b[e];
+          ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
+          dot += g.a[e] * dn.a[e] * x.a[e] + g.b[e] * dn.b[e] * x.b[e];
+        }
+        const float ms = head_sum<G>(ss) / (float)d + eps;
+        const float r = ok ? 1.0f / sqrtf(ms) : 0.f;  // (a lane without a head adds nothing to the gains' sums, eps 0 too)
+        // <a, x r> / d: with r inside, no power of it can leave the range
+        const float coef = r * head_sum<G>(dot) / (float)d;
+        Pairs<V> out;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float na = x.a[e] * r, nb = x.b[e] * r;
+          sum.a[e] += dn.a[e] * na;
+          sum.b[e] += dn.b[e] * nb;
+          out.a[e] = r * (g.a[e] * dn.a[e] - na * coef);
+          out.b[e] = r * (g.b[e] * dn.b[e] - nb * coef);
+        }
+        if (ok) store_pairs<V>(dx + at, half, out);
+      }
+    };
+    heads(0, nq, gains[0], sums[0]);
+    heads(nq, nkv, gains[1], sums[1]);
+    if (dy != dx) copy_v(dy + row * ld + (int64_t)(nq + nkv) * d, dx + row * ld + (int64_t)(nq + nkv) * d, nkv * d, lane);
+  }
+  if (!part) return;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int e = 0; e < 2 * V; ++e) {
+      float v = e < V ? sums[k].a[e % V] : sums[k].b[e % V];
+#pragma unroll
+      for (int o = G; o < 64; o <<= 1) v += __shfl_xor(v, o);
+      if (h0 == 0) red[wave][k][2 * V * c + e] = v;
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * d; i += 64 * QKN_WAVES) {
+    // feature f of a gain: lane (f mod d/2) / V of a head, value f mod V of its half
+    const int k = i / d, f = i % d, u = f % half, e = 2 * V * (u / V) + u % V + (f < half ? 0 : V);
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < QKN_WAVES; ++w) v += red[w][k][e];
+    part[(int64_t)blockIdx.x * 2 * d + i] = v;
+  }
+}
+
+// dg (+)= the sum of the parts, 64 columns to a workgroup, 16 threads to a column; in
+// fp64 and a fixed order.
+__global__ __launch_bounds__(64 * SUM_GROUPS) void gain_sum_kernel(int parts, int d, const float* __restrict__ part,
+                                                                   float* __restrict__ dgq, float* __restrict__ dgk,
+                                                                   int accumulate) {
+  __shared__ double red[SUM_GROUPS][64];
+  const int c = threadIdx.x & 63, g = threadIdx.x >> 6, i = blockIdx.x * 64 + c;
+  double v = 0.0;
+  if (i < 2 * d) {
+#pragma unroll 8
+    for (int p = g; p < parts; p += SUM_GROUPS) v += part[(int64_t)p * 2 * d + i];
+  }
+  red[g][c] = v;
+  __syncthreads();
+  if (g > 0 || i >= 2 * d) return;
+  for (int k = 1; k < SUM_GROUPS; ++k) v += red[k][c];
+  float* out = i < d ? dgq : dgk;
+  if (!out) return;
+  out += i % d;
+  *out = (float)(accumulate ? v + *out : v);
+}
+
+// f(V, G) for a head size.
+template <class F>
+void by_head(int d, F&& f) {
+  using std::integral_constant;
+  if (d == 64) f(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+  else if (d % 16 == 0) f(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+  else f(integral_constant<int, 4>{}, integral_constant<int, 16>{});
+}
+
+int qkn_parts(const PackedShape& p) { return (int)std::min<int64_t>((p.total + QKN_WAVES - 1) / QKN_WAVES, QKN_PARTS); }
+
+}  // namespace
+
+hipError_t packed_qk_norm_rope(const PackedShape& p, const void* plan, double theta, float eps, const bf16_t* gq,
+                               const bf16_t* gk, const bf16_t* src, bf16_t* dst, hipStream_t s) {
+  const int64_t need = (p.total + QKN_WAVES - 1) / QKN_WAVES;
+  const dim3 grid((unsigned)std::min<int64_t>(need, 8192)), block(64 * QKN_WAVES);
+  by_head(p.d, [&](auto v, auto g) {
+    hipLaunchKernelGGL((qk_norm_rope_kernel<decltype(v)::value, decltype(g)::value>), grid, block, 0, s, (int)p.total, p.nq,
+                       p.nkv, p.d, eps, log2(theta), packed_pos(p, plan), gq, gk, src, dst);
+  });
+  return hipGetLastError();
+}
+
+size_t packed_qk_norm_rope_bwd_workspace(const PackedShape& p) { return (size_t)qkn_parts(p) * 2 * p.d * 4; }
+
+hipError_t packed_qk_norm_rope_bwd(const PackedShape& p, const void* plan, double theta, float eps, const bf16_t* gq,
+                                   const bf16_t* gk, const bf16_t* src, const bf16_t* dy, bf16_t* dx, float* dgq,
+                                   float* dgk, int accumulate, void* ws, hipStream_t s) {
+  const int parts = qkn_parts(p);
+  float* part = dgq || dgk ? (float*)ws : nullptr;
+  by_head(p.d, [&](auto v, auto g) {
+    hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<decltype(v)::value, decltype(g)::value>), dim3((unsigned)parts),
+                       dim3(64 * QKN_WAVES), 0, s, (int)p.total, p.nq, p.nkv, p.d, eps, log2(theta), packed_pos(p, plan),
+                       gq, gk, src, dy, dx, part);
+  });
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !part) return e;
+  hipLaunchKernelGGL(gain_sum_kernel, dim3((unsigned)((2 * p.d + 63) / 64)), dim3(64 * SUM_GROUPS), 0, s, parts, p.d,
+                     (const float*)part, dgq, dgk, accumulate);
+  return hipGetLastError();
+}
+
+}  // namespace ls

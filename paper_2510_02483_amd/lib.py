@@ -11,7 +11,7 @@ import os
 
 import torch
 
-from .configs import BlockConfig, PackedConfig, StackConfig
+from .configs import BlockConfig, PackedConfig, ScoreConfig, StackConfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libls.so")
@@ -67,6 +67,14 @@ class LsPackedCfg(ctypes.Structure):
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
+class LsScoreCfg(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("window", ctypes.c_int32)]
+
+
+class LsTensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
 class LsAdamwCfg(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
                 ("weight_decay", ctypes.c_float), ("max_norm", ctypes.c_float), ("step", ctypes.c_int32)]
@@ -94,6 +102,17 @@ _PROTOS = {
     "ls_packed_attn_fwd": (ctypes.c_int, [_P, _P, ctypes.c_size_t, _P, _P, _P, _P]),
     "ls_packed_attn_bwd_workspace": (ctypes.c_size_t, [_P]),
     "ls_packed_attn_bwd": (ctypes.c_int, [_P, _P, ctypes.c_size_t, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "ls_packed_qk_norm_rope": (ctypes.c_int, [_P, _P, ctypes.c_size_t, ctypes.c_float, ctypes.c_float, _P, _P, _P, _P,
+                                              _P]),
+    "ls_packed_qk_norm_rope_bwd_workspace": (ctypes.c_size_t, [_P]),
+    "ls_packed_qk_norm_rope_bwd": (ctypes.c_int, [_P, _P, ctypes.c_size_t, ctypes.c_float, ctypes.c_float, _P, _P, _P,
+                                                  _P, _P, _P, _P, ctypes.c_int, _P, ctypes.c_size_t, _P]),
+    "ls_packed_score_attn_fwd": (ctypes.c_int, [_P, _P, _P, ctypes.c_size_t, _P, _P, _P, _P]),
+    "ls_packed_score_attn_bwd": (ctypes.c_int, [_P, _P, _P, ctypes.c_size_t, _P, _P, _P, _P, _P, _P, ctypes.c_size_t,
+                                                _P]),
+    "ls_grad_norm_workspace": (ctypes.c_size_t, []),
+    "ls_grad_norm": (ctypes.c_int, [ctypes.c_int32, _P, _P, _P, ctypes.c_size_t, _P]),
+    "ls_grad_clip": (ctypes.c_int, [ctypes.c_int32, _P, _P, ctypes.c_float, _P, _P]),
     "ls_rmsnorm_fwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_float, _P, _P, _P, _P, _P]),
     "ls_rmsnorm_bwd_workspace": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int32]),
     "ls_rmsnorm_bwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P, ctypes.c_int, _P,
@@ -318,6 +337,61 @@ def ls_packed_attn_bwd(c, plan, qkv, o, lse, dout, dqkv, workspace, stream=None)
                                     _p(dqkv), _p(workspace), _bytes(workspace), _stream(stream)), "ls_packed_attn_bwd")
 
 
+def ls_packed_qk_norm_rope(c, plan, theta, eps, q_gain, k_gain, src, dst, stream=None):
+    """q and k of every row normed per head (gains: head_dim bf16) and turned by its position; dst may be src."""
+    n, _ = _packed_sizes(c)
+    _need(("plan", plan, None, None), ("q_gain", q_gain, _BF16, c.head_dim), ("k_gain", k_gain, _BF16, c.head_dim),
+          ("src", src, _BF16, n), ("dst", dst, _BF16, n))
+    cfg = make_packed_cfg(c)
+    _check(lib().ls_packed_qk_norm_rope(ctypes.byref(cfg), _p(plan), _bytes(plan), theta, eps, _p(q_gain), _p(k_gain),
+                                        _p(src), _p(dst), _stream(stream)), "ls_packed_qk_norm_rope")
+
+
+def ls_packed_qk_norm_rope_bwd_workspace(c) -> int:
+    cfg = make_packed_cfg(c)
+    return lib().ls_packed_qk_norm_rope_bwd_workspace(ctypes.byref(cfg))
+
+
+def ls_packed_qk_norm_rope_bwd(c, plan, theta, eps, q_gain, k_gain, src, dy, dx, dq_gain, dk_gain, accumulate,
+                               workspace, stream=None):
+    """src: the forward call's, before the norm; dx may be dy; either gain's gradient (head_dim fp32) may be None."""
+    n, _ = _packed_sizes(c)
+    _need(("plan", plan, None, None), ("q_gain", q_gain, _BF16, c.head_dim), ("k_gain", k_gain, _BF16, c.head_dim),
+          ("src", src, _BF16, n), ("dy", dy, _BF16, n), ("dx", dx, _BF16, n), ("dq_gain", dq_gain, _F32, c.head_dim),
+          ("dk_gain", dk_gain, _F32, c.head_dim), ("workspace", workspace, None, None))
+    cfg = make_packed_cfg(c)
+    _check(lib().ls_packed_qk_norm_rope_bwd(ctypes.byref(cfg), _p(plan), _bytes(plan), theta, eps, _p(q_gain),
+                                            _p(k_gain), _p(src), _p(dy), _p(dx), _p(dq_gain), _p(dk_gain),
+                                            int(accumulate), _p(workspace), _bytes(workspace), _stream(stream)),
+           "ls_packed_qk_norm_rope_bwd")
+
+
+def make_score_cfg(s: ScoreConfig) -> LsScoreCfg:
+    return LsScoreCfg(s.scale, s.cap, s.window)
+
+
+def ls_packed_score_attn_fwd(c, score, plan, qkv, o, lse, stream=None):
+    """ls_packed_attn_fwd with the scores of ``score``."""
+    n, m = _packed_sizes(c)
+    _need(("plan", plan, None, None), ("qkv", qkv, _BF16, n), ("o", o, _BF16, m),
+          ("lse", lse, _F32, c.total * c.n_q_heads))
+    cfg, sc = make_packed_cfg(c), make_score_cfg(score)
+    _check(lib().ls_packed_score_attn_fwd(ctypes.byref(cfg), ctypes.byref(sc), _p(plan), _bytes(plan), _p(qkv), _p(o),
+                                          _p(lse), _stream(stream)), "ls_packed_score_attn_fwd")
+
+
+def ls_packed_score_attn_bwd(c, score, plan, qkv, o, lse, dout, dqkv, workspace, stream=None):
+    """workspace: ls_packed_attn_bwd_workspace(c) bytes."""
+    n, m = _packed_sizes(c)
+    _need(("plan", plan, None, None), ("qkv", qkv, _BF16, n), ("o", o, _BF16, m),
+          ("lse", lse, _F32, c.total * c.n_q_heads), ("dout", dout, _BF16, m), ("dqkv", dqkv, _BF16, n),
+          ("workspace", workspace, None, None))
+    cfg, sc = make_packed_cfg(c), make_score_cfg(score)
+    _check(lib().ls_packed_score_attn_bwd(ctypes.byref(cfg), ctypes.byref(sc), _p(plan), _bytes(plan), _p(qkv), _p(o),
+                                          _p(lse), _p(dout), _p(dqkv), _p(workspace), _bytes(workspace),
+                                          _stream(stream)), "ls_packed_score_attn_bwd")
+
+
 def ls_rmsnorm_fwd(rows, hidden, eps, x, gamma, h, r, stream=None):
     _check(lib().ls_rmsnorm_fwd(rows, hidden, eps, _p(x), _p(gamma), _p(h), _p(r), _stream(stream)), "ls_rmsnorm_fwd")
 
@@ -445,6 +519,44 @@ def ls_adamw_step(master, param, grad, m, v, *, step, lr, beta1=0.9, beta2=0.95,
     _check(lib().ls_adamw_step(n, nd, ctypes.byref(cfg), _p(master), _p(param), _p(grad), _p(m), _p(v),
                                _p(grad_norm), _p(workspace), workspace.numel() * workspace.element_size(),
                                _stream(stream)), "ls_adamw_step")
+
+
+def _tensors(name, ts):
+    """Dense fp32 or bf16 tensors of the current GPU as a list of the library's, or a ValueError."""
+    if not ts:
+        raise ValueError(f"{name} must hold a tensor at least")
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -2
+    out = (LsTensor * len(ts))()
+    for i, t in enumerate(ts):
+        if t.dtype is not _F32 and t.dtype is not _BF16:
+            raise ValueError(f"{name}[{i}] must be float32 or bfloat16, not {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name}[{i}] must be contiguous")
+        if t.get_device() != here:
+            raise ValueError(f"{name}[{i}] must be on the current GPU")
+        out[i] = (t.data_ptr(), t.numel(), int(t.dtype is _BF16))
+    return out
+
+
+def ls_grad_norm_workspace() -> int:
+    return lib().ls_grad_norm_workspace()
+
+
+def ls_grad_norm(grads, norm, workspace, stream=None):
+    """norm (one fp32): the L2 norm of all of ``grads`` (a list of fp32 or bf16 tensors) together."""
+    g = _tensors("grads", grads)
+    _need(("norm", norm, _F32, 1), ("workspace", workspace, None, None))
+    _check(lib().ls_grad_norm(len(g), g, _p(norm), _p(workspace), _bytes(workspace), _stream(stream)), "ls_grad_norm")
+
+
+def ls_grad_clip(grads, norm, max_norm, out=None, stream=None):
+    """grads x min(1, max_norm / (norm + 1e-6)), in place or into ``out``, tensors of the same sizes and either type."""
+    g = _tensors("grads", grads)
+    o = None if out is None else _tensors("out", out)
+    if o is not None and len(o) != len(g):
+        raise ValueError(f"out must hold {len(g)} tensors, not {len(o)}")
+    _need(("norm", norm, _F32, 1))
+    _check(lib().ls_grad_clip(len(g), g, _p(norm), float(max_norm), o, _stream(stream)), "ls_grad_clip")
 
 
 def ls_timing_begin(label: str, max_launches: int):
