@@ -1254,17 +1254,19 @@ static int check_score_cfg(const ls_score_cfg* c, const ls::PackedShape& p, ls::
 }
 
 int ls_packed_score_attn_fwd(const ls_packed_cfg* cfg, const ls_score_cfg* score, const void* plan, size_t plan_bytes,
-                             const ls_bf16* qkv, ls_bf16* o, float* lse, void* stream) {
+                             const ls_bf16* qkv, ls_bf16* o, float* lse, ls_bf16* o_rest, void* stream) {
   ls::PackedShape p;
   ls::ScoreShape c;
   bool plain;
   if (int e = check_packed_cfg(cfg, p)) return e;
   if (int e = check_score_cfg(score, p, c, plain)) return e;
-  if (plain) return ls_packed_attn_fwd(cfg, plan, plan_bytes, qkv, o, lse, stream);
+  if (plain && !o_rest) return ls_packed_attn_fwd(cfg, plan, plan_bytes, qkv, o, lse, stream);
   const Range in[] = {{plan, plan_bytes, "plan"}, {qkv, packed_qkv_bytes(p), "qkv"}};
-  const Range out[] = {{o, packed_o_bytes(p), "o"}, {lse, (size_t)p.nq * p.total * 4, "lse"}};
-  if (int e = check_ranges(in, 2, out, 2)) return e;
+  Range out[3] = {{o, packed_o_bytes(p), "o"}, {lse, (size_t)p.nq * p.total * 4, "lse"}};
+  if (o_rest) out[2] = {o_rest, packed_o_bytes(p), "o_rest"};
+  if (int e = check_ranges(in, 2, out, o_rest ? 3 : 2)) return e;
   if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  c.rest = (bf16_t*)o_rest;
   const hipStream_t st = (hipStream_t)stream;
   LS_STEP("packed score attention fwd", st,
           ls::packed_score_attn_fwd(p, c, plan, (const bf16_t*)qkv, (bf16_t*)o, lse, st));
@@ -1272,23 +1274,25 @@ int ls_packed_score_attn_fwd(const ls_packed_cfg* cfg, const ls_score_cfg* score
 }
 
 int ls_packed_score_attn_bwd(const ls_packed_cfg* cfg, const ls_score_cfg* score, const void* plan, size_t plan_bytes,
-                             const ls_bf16* qkv, const ls_bf16* o, const float* lse, const ls_bf16* dout,
-                             ls_bf16* dqkv, void* workspace, size_t workspace_bytes, void* stream) {
+                             const ls_bf16* qkv, const ls_bf16* o, const float* lse, const ls_bf16* o_rest,
+                             const ls_bf16* dout, ls_bf16* dqkv, void* workspace, size_t workspace_bytes, void* stream) {
   ls::PackedShape p;
   ls::ScoreShape c;
   bool plain;
   if (int e = check_packed_cfg(cfg, p)) return e;
   if (int e = check_score_cfg(score, p, c, plain)) return e;
-  if (plain)
+  if (plain && !o_rest)
     return ls_packed_attn_bwd(cfg, plan, plan_bytes, qkv, o, lse, dout, dqkv, workspace, workspace_bytes, stream);
-  const Range in[] = {{plan, plan_bytes, "plan"},
-                      {qkv, packed_qkv_bytes(p), "qkv"},
-                      {o, packed_o_bytes(p), "o"},
-                      {lse, (size_t)p.nq * p.total * 4, "lse"},
-                      {dout, packed_o_bytes(p), "dout"}};
+  Range in[6] = {{plan, plan_bytes, "plan"},
+                 {qkv, packed_qkv_bytes(p), "qkv"},
+                 {o, packed_o_bytes(p), "o"},
+                 {lse, (size_t)p.nq * p.total * 4, "lse"},
+                 {dout, packed_o_bytes(p), "dout"}};
+  if (o_rest) in[5] = {o_rest, packed_o_bytes(p), "o_rest"};
   const Range out[] = {{dqkv, packed_qkv_bytes(p), "dqkv"}, {workspace, workspace_bytes, "workspace"}};
-  if (int e = check_ranges(in, 5, out, 2)) return e;
+  if (int e = check_ranges(in, o_rest ? 6 : 5, out, 2)) return e;
   if (int e = check_plan_bytes(p, plan_bytes)) return e;
+  c.rest = (bf16_t*)o_rest;
   const size_t need = ls::packed_attn_bwd_workspace(p);
   if (workspace_bytes < need) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, need);
   const hipStream_t st = (hipStream_t)stream;

@@ -9,8 +9,8 @@ namespace {
 // f(a ModScore) for the cap (0: none) and the window (of at most `total` positions).
 template <class F>
 hipError_t with_score(const ScoreShape& c, F&& f) {
-  if (c.cap > 0.f) return f(ModScore<true>{c.window, 2.0f * LOG2E * c.scale / c.cap, c.cap * LOG2E});
-  return f(ModScore<false>{c.window, 0.f, 0.f});
+  if (c.cap > 0.f) return f(ModScore<true>{c.window, 2.0f * LOG2E * c.scale / c.cap, c.cap * LOG2E, c.rest});
+  return f(ModScore<false>{c.window, 0.f, 0.f, c.rest});
 }
 
 }  // namespace

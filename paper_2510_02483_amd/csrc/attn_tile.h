@@ -94,6 +94,7 @@ struct ModScore {
   int window;  // positions that a query sees, itself included
   float in;    // capped: 2 log2(e) scale / cap, what q.k is multiplied with
   float c2;    // capped: cap log2(e), the largest score in base 2
+  bf16_t* rest;  // null, or what the rounding of o left (written by the forward pass, read by the backward pass)
   // r of a raw score, and the base-2 score c2 tanh = c2 - 2 c2 r less `m`
   LS_DEV float half(float x) const { return __builtin_amdgcn_rcpf(1.0f + ex2(x * in)); }
   LS_DEV float less(float r, float m) const { return fmaf(r, -2.0f * c2, c2 - m); }
@@ -297,6 +298,28 @@ LS_DEV void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// What rounding a lane's row of o (columns 32i + 8(r/4) + 4lh + r%4, times inv) to bf16 leaves, in bf16: with it the
+// backward pass has <dO, O> to 2^-17 of its terms instead of 2^-8.  Where the softmax is peaked that error, which all
+// of a row's dS share, is larger than the rounding of dS itself (600 rows, scores of a standard deviation of 4: dqkv
+// 0.0032 of its norm off without, 0.0024 with it).
+template <int D, class SC>
+LS_DEV void store_rest(const SC& sc, int64_t at, const f32x16 (&oacc)[D / 32], float inv, int hd, int lh) {
+  if (!sc.rest) return;
+  bf16_t* row = sc.rest + at;
+  auto left = [](float x) { return x - bf2f(f2bf(x)); };
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int rq = 0; rq < 4; ++rq) {
+      const int d = 32 * i + 8 * rq + 4 * lh;
+      if (d >= hd) continue;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = left(oacc[i][4 * rq + e] * inv);
+      *(u32x2*)(row + d) = u32x2{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
+    }
+}
+
 // Forward of one head of a packed sequence of up to 32 NB rows by one wave: every
 // operand straight from global memory, V through the wave's own LDS tile `vt` for
 // its transpose.  A workgroup's four waves work on four sequences, without
@@ -363,7 +386,8 @@ LS_DEV void short_fwd(const AttnShape& sh, const SC& sc, const PackedTile& t, in
     const float l = halves_sum(sum);
     if (32 * qb + lr >= t.len) continue;
     const float inv = 1.0f / l;
-    bf16_t* orow = o + (t.start + (int64_t)(32 * qb + lr)) * nq * hd + h * hd;
+    const int64_t at_row = (t.start + (int64_t)(32 * qb + lr)) * nq * hd + h * hd;
+    bf16_t* orow = o + at_row;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -371,6 +395,7 @@ LS_DEV void short_fwd(const AttnShape& sh, const SC& sc, const PackedTile& t, in
         if (32 * i + 8 * rq + 4 * lh < hd)
           *(u32x2*)(orow + 32 * i + 8 * rq + 4 * lh) = u32x2{pack_bf2(oacc[i][4 * rq] * inv, oacc[i][4 * rq + 1] * inv),
                                                              pack_bf2(oacc[i][4 * rq + 2] * inv, oacc[i][4 * rq + 3] * inv)};
+    if constexpr (SC::ON) store_rest<D>(sc, at_row, oacc, inv, hd, lh);
     if (lh == 0) lse[(int64_t)h * sh.seq + t.start + 32 * qb + lr] = (m + log2f(l)) * LN2;
   }
 }
@@ -523,6 +548,7 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 4 : 2) void attn_fwd_kerne
   if (qrow < S) {
     const float inv = 1.0f / l;
     bf16_t* orow = o + (qtile.row0 + qrow) * nq * hd + h * hd;
+    if constexpr (SC::ON) store_rest<D>(sc, (qtile.row0 + qrow) * nq * hd + h * hd, oacc, inv, hd, lh);
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -537,9 +563,10 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 4 : 2) void attn_fwd_kerne
 }
 
 // attn_bwd_pre_kernel for one row of packed sequences and heads of any width: D / 8 lanes a head.
-template <int D>
+template <int D, bool REST>
 LS_DEV void bwd_pre_row(const AttnShape& sh, const bf16_t* __restrict__ orow, const bf16_t* __restrict__ drow,
-                        const float* __restrict__ lse, float* __restrict__ Dv, float* __restrict__ lse2, int64_t t) {
+                        const float* __restrict__ lse, float* __restrict__ Dv, float* __restrict__ lse2, int64_t t,
+                        const bf16_t* __restrict__ rrow) {
   constexpr int CPH = D / 8;
   const int lane = threadIdx.x & 63, c = lane % CPH;
   for (int h = lane / CPH; h - lane / CPH < sh.nq; h += 64 / CPH) {
@@ -548,6 +575,11 @@ LS_DEV void bwd_pre_row(const AttnShape& sh, const bf16_t* __restrict__ orow, co
       const u32x4 a = load16(orow + h * sh.d + 8 * c), g = load16(drow + h * sh.d + 8 * c);
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc += bf_lo(a[e]) * bf_lo(g[e]) + bf_hi(a[e]) * bf_hi(g[e]);
+      if constexpr (REST) {
+        const u32x4 r = load16(rrow + h * sh.d + 8 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc += bf_lo(r[e]) * bf_lo(g[e]) + bf_hi(r[e]) * bf_hi(g[e]);
+      }
     }
 #pragma unroll
     for (int off = CPH / 2; off >= 1; off >>= 1) acc += __shfl_xor(acc, off);
@@ -561,17 +593,18 @@ LS_DEV void bwd_pre_row(const AttnShape& sh, const bf16_t* __restrict__ orow, co
 
 // D[b,h,s] = <dO, O> over the head's d columns (fp32), and the log-sum-exp in
 // base 2 (lse * log2(e)), the form the backward kernels subtract.
-template <int D, bool PACKED>
+// REST: O is o and the rest that its rounding left.
+template <int D, bool PACKED, bool REST = false>
 __global__ __launch_bounds__(256) void attn_bwd_pre_kernel(AttnShape sh, const bf16_t* __restrict__ o,
                                                            const bf16_t* __restrict__ dout,
                                                            const float* __restrict__ lse, float* __restrict__ Dv,
-                                                           float* __restrict__ lse2) {
+                                                           float* __restrict__ lse2, const bf16_t* __restrict__ rest) {
   constexpr int CPH = D / 8;  // 16-byte chunks per head
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)(PACKED ? packed_wg() : (int)blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (t >= (int64_t)sh.batch * sh.seq) return;
   if constexpr (PACKED) {
-    bwd_pre_row<D>(sh, o + t * sh.nq * sh.d, dout + t * sh.nq * sh.d, lse, Dv, lse2, t);
+    bwd_pre_row<D, REST>(sh, o + t * sh.nq * sh.d, dout + t * sh.nq * sh.d, lse, Dv, lse2, t, rest + t * sh.nq * sh.d);
     return;
   }
   const int b = (int)(t / sh.seq), s = (int)(t % sh.seq);
@@ -1579,7 +1612,14 @@ hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf
   float* Dv = (float*)ws;
   float* lse2 = Dv + T * sh.nq;
   float* part = (float*)((char*)ws + bwd_ws_head(sh));
-  hipLaunchKernelGGL((attn_bwd_pre_kernel<D, true>), packed_grid((T + 3) / 4), dim3(256), 0, s, sh, o, dout, lse, Dv, lse2);
+  const bf16_t* rest = nullptr;
+  if constexpr (SC::ON) rest = sc.rest;
+  if (SC::ON && rest)
+    hipLaunchKernelGGL((attn_bwd_pre_kernel<D, true, SC::ON>), packed_grid((T + 3) / 4), dim3(256), 0, s, sh, o, dout, lse,
+                       Dv, lse2, rest);
+  else
+    hipLaunchKernelGGL((attn_bwd_pre_kernel<D, true>), packed_grid((T + 3) / 4), dim3(256), 0, s, sh, o, dout, lse, Dv,
+                       lse2, rest);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const float qk = SC::ON ? own_scale : 1.0f / sqrtf((float)sh.d), sl2 = qk * LOG2E;

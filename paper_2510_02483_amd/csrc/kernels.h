@@ -161,9 +161,11 @@ hipError_t packed_attn_bwd(const PackedShape& p, const void* plan, const bf16_t*
 
 // The same attention with scores cap tanh(scale q.k / cap) (cap 0: scale q.k) over the last `window` positions
 // (1 .. total); workspace: packed_attn_bwd_workspace.
+// rest: null, or what rounding o to bf16 left, in bf16 (an output of the forward call).
 struct ScoreShape {
   float scale, cap;
   int window;
+  bf16_t* rest = nullptr;
 };
 hipError_t packed_score_attn_fwd(const PackedShape& p, const ScoreShape& c, const void* plan, const bf16_t* qkv,
                                  bf16_t* o, float* lse, hipStream_t s);

@@ -107,9 +107,9 @@ _PROTOS = {
     "ls_packed_qk_norm_rope_bwd_workspace": (ctypes.c_size_t, [_P]),
     "ls_packed_qk_norm_rope_bwd": (ctypes.c_int, [_P, _P, ctypes.c_size_t, ctypes.c_float, ctypes.c_float, _P, _P, _P,
                                                   _P, _P, _P, _P, ctypes.c_int, _P, ctypes.c_size_t, _P]),
-    "ls_packed_score_attn_fwd": (ctypes.c_int, [_P, _P, _P, ctypes.c_size_t, _P, _P, _P, _P]),
-    "ls_packed_score_attn_bwd": (ctypes.c_int, [_P, _P, _P, ctypes.c_size_t, _P, _P, _P, _P, _P, _P, ctypes.c_size_t,
-                                                _P]),
+    "ls_packed_score_attn_fwd": (ctypes.c_int, [_P, _P, _P, ctypes.c_size_t, _P, _P, _P, _P, _P]),
+    "ls_packed_score_attn_bwd": (ctypes.c_int, [_P, _P, _P, ctypes.c_size_t, _P, _P, _P, _P, _P, _P, _P,
+                                                ctypes.c_size_t, _P]),
     "ls_grad_norm_workspace": (ctypes.c_size_t, []),
     "ls_grad_norm": (ctypes.c_int, [ctypes.c_int32, _P, _P, _P, ctypes.c_size_t, _P]),
     "ls_grad_clip": (ctypes.c_int, [ctypes.c_int32, _P, _P, ctypes.c_float, _P, _P]),
@@ -370,25 +370,25 @@ def make_score_cfg(s: ScoreConfig) -> LsScoreCfg:
     return LsScoreCfg(s.scale, s.cap, s.window)
 
 
-def ls_packed_score_attn_fwd(c, score, plan, qkv, o, lse, stream=None):
-    """ls_packed_attn_fwd with the scores of ``score``."""
+def ls_packed_score_attn_fwd(c, score, plan, qkv, o, lse, o_rest=None, stream=None):
+    """ls_packed_attn_fwd with the scores of ``score``; o_rest (as o, or None) takes what rounding o left."""
     n, m = _packed_sizes(c)
     _need(("plan", plan, None, None), ("qkv", qkv, _BF16, n), ("o", o, _BF16, m),
-          ("lse", lse, _F32, c.total * c.n_q_heads))
+          ("lse", lse, _F32, c.total * c.n_q_heads), ("o_rest", o_rest, _BF16, m))
     cfg, sc = make_packed_cfg(c), make_score_cfg(score)
     _check(lib().ls_packed_score_attn_fwd(ctypes.byref(cfg), ctypes.byref(sc), _p(plan), _bytes(plan), _p(qkv), _p(o),
-                                          _p(lse), _stream(stream)), "ls_packed_score_attn_fwd")
+                                          _p(lse), _p(o_rest), _stream(stream)), "ls_packed_score_attn_fwd")
 
 
-def ls_packed_score_attn_bwd(c, score, plan, qkv, o, lse, dout, dqkv, workspace, stream=None):
-    """workspace: ls_packed_attn_bwd_workspace(c) bytes."""
+def ls_packed_score_attn_bwd(c, score, plan, qkv, o, lse, dout, dqkv, workspace, o_rest=None, stream=None):
+    """workspace: ls_packed_attn_bwd_workspace(c) bytes; o_rest: the forward call's, or None."""
     n, m = _packed_sizes(c)
     _need(("plan", plan, None, None), ("qkv", qkv, _BF16, n), ("o", o, _BF16, m),
-          ("lse", lse, _F32, c.total * c.n_q_heads), ("dout", dout, _BF16, m), ("dqkv", dqkv, _BF16, n),
-          ("workspace", workspace, None, None))
+          ("lse", lse, _F32, c.total * c.n_q_heads), ("o_rest", o_rest, _BF16, m), ("dout", dout, _BF16, m),
+          ("dqkv", dqkv, _BF16, n), ("workspace", workspace, None, None))
     cfg, sc = make_packed_cfg(c), make_score_cfg(score)
     _check(lib().ls_packed_score_attn_bwd(ctypes.byref(cfg), ctypes.byref(sc), _p(plan), _bytes(plan), _p(qkv), _p(o),
-                                          _p(lse), _p(dout), _p(dqkv), _p(workspace), _bytes(workspace),
+                                          _p(lse), _p(o_rest), _p(dout), _p(dqkv), _p(workspace), _bytes(workspace),
                                           _stream(stream)), "ls_packed_score_attn_bwd")
 
 

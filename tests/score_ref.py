@@ -9,11 +9,12 @@ import packed_ref as R
 U, W = R.U, R.W
 
 
-def attention(qkv, lens, first, nq, nkv, d, dout=None, scale=0.0, cap=0.0, window=0):
+def attention(qkv, lens, first, nq, nkv, d, dout=None, scale=0.0, cap=0.0, window=0, rest=False):
     """packed_ref.attention with scores cap tanh(scale q.k / cap) over a window.
 
     Beside the errors counted there: a capped score is c2 - 2 c2 r with r good to 1.9 x 2^-23, so it is off by cap x
-    2^-21, and p relatively by twice that (its own and the log-sum-exp's); the slope 4 r (1 - r) is off by 2^-20."""
+    2^-21, and p relatively by twice that (its own and the log-sum-exp's); the slope 4 r (1 - r) is off by 2^-20.
+    rest: D comes from o and the rest of its rounding, which is o to 2^-17 but for the rounding of p."""
     total = qkv.shape[0]
     o, lse, grad = np.zeros((total, nq * d)), np.zeros((nq, total)), np.zeros_like(qkv)
     tol = {"o": np.zeros_like(o), "lse": np.zeros_like(lse), "dqkv": np.zeros_like(qkv)}
@@ -60,6 +61,8 @@ def attention(qkv, lens, first, nq, nkv, d, dout=None, scale=0.0, cap=0.0, windo
             grad[a:b, hv] += p.T @ do
             grad[a:b, hq] = ds @ k * sc
             grad[a:b, hk] += ds.T @ q * sc
+            if rest:
+                err_o = err_o - U * np.abs(o[a:b, hq]) * 1.01 + 2.0 ** -16 * np.abs(o[a:b, hq])
             err_D = (np.abs(do) * err_o).sum(1, keepdims=True)
             flat = d * W * (np.abs(do) @ np.abs(v).T + np.abs(D))
             err_ds = U * np.abs(ds) * 1.01 + slope * p * (err_D + flat) * (1 + U) + slack * np.abs(ds) + \

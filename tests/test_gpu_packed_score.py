@@ -14,18 +14,27 @@ from test_gpu_packed import LENGTHS, MARK, Batch
 pytestmark = pytest.mark.gpu
 
 
-def run(b, score, backward=True, stream=None):
+def run(b, score, backward=True, stream=None, rest=False):
+    b.rest = torch.full_like(b.o, MARK) if rest else None
     L.ls_packed_plan(b.c, b.cu, b.plan, stream=stream)
-    L.ls_packed_score_attn_fwd(b.c, score, b.plan, b.qkv, b.o, b.lse, stream=stream)
+    L.ls_packed_score_attn_fwd(b.c, score, b.plan, b.qkv, b.o, b.lse, o_rest=b.rest, stream=stream)
     if backward:
-        L.ls_packed_score_attn_bwd(b.c, score, b.plan, b.qkv, b.o, b.lse, b.dout, b.dqkv, b.ws, stream=stream)
+        L.ls_packed_score_attn_bwd(b.c, score, b.plan, b.qkv, b.o, b.lse, b.dout, b.dqkv, b.ws, o_rest=b.rest,
+                                   stream=stream)
     return b
 
 
 def check(b, score, backward=True):
     x, g = b.inputs64()
-    o, lse, grad, tol = S.attention(x, b.lens, b.first, b.nq, b.nkv, b.d, g, score.scale, score.cap, score.window)
+    rest = b.rest is not None
+    o, lse, grad, tol = S.attention(x, b.lens, b.first, b.nq, b.nkv, b.d, g, score.scale, score.cap, score.window, rest)
     out = b.outside.cpu().numpy()
+    if rest:
+        assert np.all(f64(b.rest)[out] == MARK)
+        # o and its rest: the rounding of p is left, and two of fp32
+        lim = tol["o"] - S.U * np.abs(o) * 1.01 + 2.0 ** -16 * np.abs(o) + 1e-30
+        assert np.all(np.abs(f64(b.o) + f64(b.rest) - o)[~out] <= lim[~out])
+        assert np.all(np.abs(f64(b.rest)[~out]) <= S.U * np.abs(f64(b.o)[~out]))
     pairs = [("o", f64(b.o), o, tol["o"]), ("lse", f64(b.lse).T, lse.T, tol["lse"].T)]
     if backward:
         pairs.append(("dqkv", f64(b.dqkv), grad, tol["dqkv"]))
@@ -56,8 +65,9 @@ SCORES = {
 def test_against_the_reference(lens, score, nq, nkv, d):
     need_gpu()
     say(lens, score, nq, nkv, d)
-    b = Batch(nq=nq, nkv=nkv, d=d, seed=3, std=2.0, **LENGTHS[lens])
-    check(run(b, SCORES[score]), SCORES[score])
+    for rest in (False, True):
+        b = Batch(nq=nq, nkv=nkv, d=d, seed=3, std=2.0, **LENGTHS[lens])
+        check(run(b, SCORES[score], rest=rest), SCORES[score])
 
 
 @pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (8, 1, 128), (5, 1, 120)])
@@ -84,6 +94,20 @@ def test_few_small_sequences_of_a_large_group(lens, nq, nkv, d):
     need_gpu()
     score = ScoreConfig(cap=8.0, window=21)
     check(run(Batch(lens, nq, nkv, d, first=1, tail=2, seed=37, std=2.0), score), score)
+
+
+def test_the_rest_of_o_alone():
+    """Plain scores with a rest: o and lse are those of the plain attention; the gradients nearer than without."""
+    need_gpu()
+    a, b = (Batch([600, 90, 20], 4, 2, 64, tail=3, seed=9, std=2.0) for _ in range(2))
+    a.run()
+    run(b, ScoreConfig(), rest=True)
+    assert torch.equal(a.o, b.o) and torch.equal(a.lse, b.lse)
+    check(b, ScoreConfig())
+    x, g = a.inputs64()
+    ref = S.attention(x, a.lens, 0, 4, 2, 64, g)[2]
+    off = [np.linalg.norm((f64(t.dqkv) - ref)[:710]) for t in (a, b)]
+    assert off[1] < off[0]
 
 
 @pytest.mark.parametrize("cap", [0.01, 1.0, 30.0, 50.0, 60.0, 1000.0])

@@ -63,16 +63,17 @@ def test_qk_norm_backward_refusals(bad, status):
     assert norm_bwd(**bad) == status
 
 
-def score_fwd(score, plan_bytes=None, qkv=A[1], o=A[2], lse=A[3]):
+def score_fwd(score, plan_bytes=None, qkv=A[1], o=A[2], lse=A[3], rest=None):
     cfg, n = packed()
-    return L.lib().ls_packed_score_attn_fwd(cfg, score, A[0], n if plan_bytes is None else plan_bytes, qkv, o, lse, None)
+    return L.lib().ls_packed_score_attn_fwd(cfg, score, A[0], n if plan_bytes is None else plan_bytes, qkv, o, lse, rest,
+                                            None)
 
 
-def score_bwd(score, plan_bytes=None, qkv=A[1], o=A[2], lse=A[3], dout=A[4], dqkv=A[5], ws=A[6], ws_bytes=None):
+def score_bwd(score, plan_bytes=None, qkv=A[1], o=A[2], lse=A[3], dout=A[4], dqkv=A[5], ws=A[6], ws_bytes=None, rest=None):
     cfg, n = packed()
     need = L.ls_packed_attn_bwd_workspace(C)
-    return L.lib().ls_packed_score_attn_bwd(cfg, score, A[0], n if plan_bytes is None else plan_bytes, qkv, o, lse, dout,
-                                            dqkv, ws, need if ws_bytes is None else ws_bytes, None)
+    return L.lib().ls_packed_score_attn_bwd(cfg, score, A[0], n if plan_bytes is None else plan_bytes, qkv, o, lse, rest,
+                                            dout, dqkv, ws, need if ws_bytes is None else ws_bytes, None)
 
 
 @pytest.mark.parametrize("call", [score_fwd, score_bwd])
@@ -94,6 +95,8 @@ def test_score_attention_refusals(score):
     assert score_fwd(sc, qkv=at(A[1], 2)) == 4
     assert score_bwd(sc, dqkv=A[1]) == 5 and score_bwd(sc, ws=None) == 1 and score_bwd(sc, ws_bytes=64) == 6
     assert score_bwd(sc, dout=None) == 1
+    assert score_fwd(sc, rest=A[2]) == 5 and score_fwd(sc, rest=A[1]) == 5 and score_fwd(sc, rest=at(A[7], 4)) == 4
+    assert score_bwd(sc, rest=A[5]) == 5 and score_bwd(sc, rest=at(A[7], 4)) == 4
 
 
 def tensors(*spec):
@@ -158,9 +161,9 @@ ENTRIES = {
     "norm_bwd": (lambda t: L.ls_packed_qk_norm_rope_bwd(C, theta=1e4, eps=1e-5, accumulate=False, **t),
                  dict(plan=PLAN, q_gain=GAIN, k_gain=GAIN, src=QKV, dy=QKV, dx=QKV, dq_gain=(F32, (64,)),
                       dk_gain=(F32, (64,)), workspace=WS)),
-    "score": (lambda t: L.ls_packed_score_attn_fwd(C, ScoreConfig(cap=5.0), **t), dict(plan=PLAN, qkv=QKV, o=O, lse=LSE)),
+    "score": (lambda t: L.ls_packed_score_attn_fwd(C, ScoreConfig(cap=5.0), **t), dict(plan=PLAN, qkv=QKV, o=O, lse=LSE, o_rest=O)),
     "score_bwd": (lambda t: L.ls_packed_score_attn_bwd(C, ScoreConfig(cap=5.0), **t),
-                  dict(plan=PLAN, qkv=QKV, o=O, lse=LSE, dout=O, dqkv=QKV, workspace=WS)),
+                  dict(plan=PLAN, qkv=QKV, o=O, lse=LSE, o_rest=O, dout=O, dqkv=QKV, workspace=WS)),
 }
 
 
