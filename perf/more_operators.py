@@ -222,7 +222,7 @@ def _buffers(s):
     s["score"] = ScoreConfig(cap=c["cap"], window=c["window"])
     s["o"], s["lse"] = zeros(c["rows"], c["nq"] * c["d"], dtype=BF16), zeros(c["nq"], c["rows"])
     if c["kind"] == "attn_train":
-        s["dqkv"] = torch.zeros_like(s["qkv"])
+        s["dqkv"], s["o_rest"] = torch.zeros_like(s["qkv"]), torch.zeros_like(s["o"])
         s["workspace"] = space(lib.ls_packed_attn_bwd_workspace(cfg))
 
 
@@ -257,11 +257,11 @@ def _run_own(s):
                                            s["dout"], s["dqkv"], s["dq_gain"], s["dk_gain"], False, s["workspace"])
             out.update(dqkv=s["dqkv"], dq_gain=s["dq_gain"], dk_gain=s["dk_gain"])
         return out
-    lib.ls_packed_score_attn_fwd(s["cfg"], s["score"], s["plan"], s["qkv"], s["o"], s["lse"])
+    lib.ls_packed_score_attn_fwd(s["cfg"], s["score"], s["plan"], s["qkv"], s["o"], s["lse"], o_rest=s.get("o_rest"))
     out = {"o": s["o"], "lse": s["lse"]}
     if c["kind"] == "attn_train":
         lib.ls_packed_score_attn_bwd(s["cfg"], s["score"], s["plan"], s["qkv"], s["o"], s["lse"], s["dout"], s["dqkv"],
-                                     s["workspace"])
+                                     s["workspace"], o_rest=s["o_rest"])
         out["dqkv"] = s["dqkv"]
     return out
 
