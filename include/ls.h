@@ -532,6 +532,43 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
                      int accumulate, ls_bf16* d_embed_bf16, int32_t piece, void* workspace,
                      size_t workspace_bytes, void* stream);
 
+/* ---- log probabilities of given tokens, entropies and top alternatives ---------------
+ *
+ * For hidden states h [tokens, hidden], head weights embed [vocab, hidden] and the scaled
+ * logits z = scale h embed^T (scale > 0: one over a temperature), formed tile by tile and
+ * not stored:
+ *
+ *   lse[t] = ln sum_v exp z[t,v];  logprob[t] = z[t, targets[t]] - lse[t];
+ *   entropy[t] = -sum_v p ln p, p = exp(z[t,v] - lse[t]);
+ *
+ * logprob and entropy are 0 in rows with targets[t] = -1, which are no part of a loss, and NaN where
+ * a target lies outside [-1, vocab).  With top (1 .. 64), the `top` largest logits of every row, with a
+ * target or without: top_ids and top_logprob [tokens, top], largest first, ties to the lower id;
+ * -1 and -inf past the vocabulary; NaN logits are never among them.  (Their logits are summed
+ * in another order than the target's, so that equal tokens may differ by an fp32 rounding.)  All in fp32.
+ *
+ * The backward call, for gradients dlogprob and dentropy [tokens] (fp32; NULL: 0, one of them at
+ * least), gives with g = dlogprob[t], e = dentropy[t] and c the largest finite |g|, |e| of a row that has a target
+ *
+ *   dz = (g (onehot - p) - e p (ln p + entropy)) / c   (rounded to bf16, the operand of the next
+ *        products; rows with targets[t] = -1 are left out: their h, g and e may hold anything)
+ *   dh = c scale dz embed,  d_embed (+)= c scale dz^T h,
+ *
+ * with the outputs, pieces of the vocabulary, sizes and workspace rules of ls_head_loss_bwd.  A row whose g or e
+ * is not finite makes its row of dh and the head's gradient NaN.  entropy and lse are the forward
+ * call's, for the same scale, h, embed and targets.  workspace: at least
+ * ls_token_logprob_workspace(tokens, hidden, vocab, top, piece) bytes, which serve the forward call with this
+ * top (or 0) and the backward call with this piece.  Every output is deterministic. */
+size_t ls_token_logprob_workspace(int64_t tokens, int32_t hidden, int32_t vocab, int32_t top, int32_t piece);
+int ls_token_logprob_fwd(int64_t tokens, int32_t hidden, int32_t vocab, float scale, const ls_bf16* h,
+                         const ls_bf16* embed, const int32_t* targets, float* logprob, float* entropy, float* lse,
+                         int32_t top, int32_t* top_ids, float* top_logprob, void* workspace, size_t workspace_bytes,
+                         void* stream);
+int ls_token_logprob_bwd(int64_t tokens, int32_t hidden, int32_t vocab, float scale, const ls_bf16* h,
+                         const ls_bf16* embed, const int32_t* targets, const float* entropy, const float* lse,
+                         const float* dlogprob, const float* dentropy, ls_bf16* dh, float* d_embed, int accumulate,
+                         ls_bf16* d_embed_bf16, int32_t piece, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Token embedding rows: x[t] = embed[ids[t]] ([tokens, hidden] bf16; an id
  * outside [0, vocab) gives a NaN row), and its backward, which ADDS dx[t] into
  * d_embed[ids[t]] (fp32; the rows of repeated ids summed in token order, so
@@ -561,7 +598,8 @@ int ls_gemm_tile_override(int32_t bm, int32_t bn);
  * "dWd", "dh2", "dWg/dWu", "rmsnorm bwd", "dO", "dWo", "attention bwd",
  * "dh1", "dWqkv", "packed plan", "packed rope", "packed attention fwd",
  * "packed attention bwd", "packed qk norm rope", "packed qk norm rope bwd", "packed score attention fwd",
- * "packed score attention bwd", "gradient norm", "gradient clip", "head loss logits", "head loss rows", "head loss gather",
+ * "packed score attention bwd", "gradient norm", "gradient clip", "logprob logits", "logprob rows", "logprob top", "logprob gather",
+ * "logprob dz", "logprob dh", "logprob dE", "logprob scatter", "head loss logits", "head loss rows", "head loss gather",
  * "head loss dz", "head loss dh", "head loss dE", "head loss scatter", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
  * "logits", "cross-entropy", "dh head", "dE head", "loss", "embedding bwd",
  * and "adamw" for ls_adamw_step),

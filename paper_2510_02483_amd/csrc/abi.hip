@@ -1638,11 +1638,15 @@ int ls_cross_entropy(int64_t tokens, int32_t seq, int32_t vocab, ls_bf16* logits
 // workspace serves either.
 struct HeadWs {
   int64_t fwd_piece, bwd_piece, ldz;
-  size_t stats, zt, fwd_total;
-  size_t coef, rows, slot, tc, lc, hc, dz, dh, kpart, bwd_total, total;
+  size_t stats, zt, gmax, fwd_total;
+  size_t coef, rows, slot, tc, lc, gc, ec, nc, hc, dz, dh, kpart, bwd_total, total;
   int64_t kpart_floats;
 };
+// What the workspace is for: the head loss, or log probabilities (with gradients of each row, and with top
+// alternatives or without).
+enum HeadKind { HEAD_LOSS, HEAD_LOGPROB, HEAD_LOGPROB_TOP };
 
+static constexpr float kLog2e = 1.4426950408889634f;
 static constexpr int64_t kHeadDzBytes = (int64_t)512 << 20;  // dz of one piece, unless the caller says
 
 static ls::GemmArgs head_logits(int64_t T, int64_t H, int64_t V, int64_t col0, int64_t cols, int epi) {
@@ -1681,7 +1685,7 @@ static ls::GemmArgs head_de(int64_t T, int64_t H, int64_t cols, int64_t ldz, boo
   return a;
 }
 
-static HeadWs head_ws(int64_t T, int64_t H, int64_t V, int64_t piece) {
+static HeadWs head_ws(int64_t T, int64_t H, int64_t V, int64_t piece, HeadKind kind = HEAD_LOSS) {
   HeadWs w;
   // a piece's rows of E are one operand of a product, its dz another
   auto fit = [&](int64_t p) { return std::max<int64_t>(p & ~(int64_t)255, 256); };
@@ -1695,11 +1699,13 @@ static HeadWs head_ws(int64_t T, int64_t H, int64_t V, int64_t piece) {
   int64_t blocks = 0;
   for (int64_t c0 = 0; c0 < V; c0 += w.fwd_piece) {
     const int64_t cols = std::min(w.fwd_piece, V - c0);
-    const ls::GemmPlan p = ls::gemm_plan_free(head_logits(T, H, V, c0, cols, ls::EPI_LSE));
+    const ls::GemmPlan p = ls::gemm_plan_free(head_logits(T, H, V, c0, cols, kind ? ls::EPI_STAT : ls::EPI_LSE));
     blocks += 2 * ((cols + p.bn - 1) / p.bn);
   }
-  w.stats = f.take((size_t)(blocks * T * 8));
+  w.stats = f.take((size_t)(blocks * T * (kind ? 16 : 8)));
   w.zt = f.take((size_t)T * 4);
+  // (whole tiles write their groups of 16 columns past the vocabulary too)
+  w.gmax = f.take(kind == HEAD_LOGPROB_TOP ? (size_t)((V + 255) / 256 * 16 * T * 4) : 0);
   w.fwd_total = f.off;
   Carver b;
   w.coef = b.take(16);
@@ -1707,6 +1713,9 @@ static HeadWs head_ws(int64_t T, int64_t H, int64_t V, int64_t piece) {
   w.slot = b.take((size_t)T * 4);
   w.tc = b.take((size_t)T * 4);
   w.lc = b.take((size_t)T * 4);
+  w.gc = b.take(kind ? (size_t)T * 4 : 0);
+  w.ec = b.take(kind ? (size_t)T * 4 : 0);
+  w.nc = b.take(kind ? (size_t)T * 4 : 0);
   w.hc = b.take((size_t)(T * H * 2));
   w.dz = b.take((size_t)(T * w.ldz * 2));
   w.dh = b.take((size_t)(T * H * 4));
@@ -1769,6 +1778,69 @@ int ls_head_loss_fwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
   return LS_OK;
 }
 
+// The products of the backward pass on the gathered rows, a piece of the vocabulary at a time.  scale2: 0 for the
+// head loss; of log probabilities, what a logit is multiplied with in base 2.
+static int head_products(const HeadWs& w, int64_t T, int64_t H, int64_t V, const bf16_t* embed, float scale2,
+                         bf16_t* dh, float* d_embed, int accumulate, bf16_t* d_embed_bf16, void* workspace,
+                         hipStream_t st) {
+  const bool logprob = scale2 != 0.f;
+  float* coef = at<float>(workspace, w.coef);
+  int* rows = at<int>(workspace, w.rows);
+  bf16_t* hc = at<bf16_t>(workspace, w.hc);
+  bf16_t* dz = at<bf16_t>(workspace, w.dz);
+  float* dh32 = at<float>(workspace, w.dh);
+  float* kpart = at<float>(workspace, w.kpart);
+  for (int64_t c0 = 0; c0 < V; c0 += w.bwd_piece) {
+    const int64_t cols = std::min(w.bwd_piece, V - c0);
+    {
+      ls::GemmArgs a = head_logits(T, H, V, c0, cols, logprob ? ls::EPI_DLP : ls::EPI_DZ);
+      a.A = hc;
+      a.B[0] = embed + c0 * H;
+      a.target = at<int32_t>(workspace, w.tc);
+      a.lse = at<float>(workspace, w.lc);
+      a.rows = rows;
+      a.C = dz;
+      a.ldc = w.ldz;
+      if (logprob) {
+        a.scale2 = scale2;
+        a.dlogp = at<float>(workspace, w.gc);
+        a.dent = at<float>(workspace, w.ec);
+        a.ent = at<float>(workspace, w.nc);
+        a.cmax = coef + 1;
+      }
+      LS_STEP(logprob ? "logprob dz" : "head loss dz", st, ls::gemm(a, st));
+    }
+    if (dh) {
+      ls::GemmArgs a = head_dh(T, H, cols, w.ldz);
+      a.A = dz;
+      a.B[0] = embed + c0 * H;
+      a.rows = rows;
+      a.F[0] = dh32;
+      a.accumulate = c0 > 0;
+      a.kpart = kpart;
+      a.kpart_floats = w.kpart_floats;
+      LS_STEP(logprob ? "logprob dh" : "head loss dh", st, ls::gemm(a, st));
+    }
+    if (d_embed || d_embed_bf16) {
+      ls::GemmArgs a = head_de(T, H, cols, w.ldz, d_embed_bf16 != nullptr);
+      a.A = dz;
+      a.B[0] = hc;
+      a.rows = rows;
+      a.coef = coef;
+      if (d_embed) a.F[0] = d_embed + c0 * H;
+      else a.C = d_embed_bf16 + c0 * H;
+      a.accumulate = accumulate != 0;
+      a.kpart = kpart;
+      a.kpart_floats = w.kpart_floats;
+      LS_STEP(logprob ? "logprob dE" : "head loss dE", st, ls::gemm(a, st));
+    }
+  }
+  if (dh)
+    LS_STEP(logprob ? "logprob scatter" : "head loss scatter", st,
+            ls::head_scatter(T, (int)H, at<int32_t>(workspace, w.slot), coef, dh32, dh, st));
+  return LS_OK;
+}
+
 int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf16* h, const ls_bf16* embed,
                      const int32_t* targets, const float* lse, const float* dloss, ls_bf16* dh, float* d_embed,
                      int accumulate, ls_bf16* d_embed_bf16, int32_t piece, void* workspace, size_t workspace_bytes,
@@ -1792,57 +1864,107 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
   const HeadWs w = head_ws(T, H, V, piece);
   if (workspace_bytes < w.bwd_total) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, w.bwd_total);
   const hipStream_t st = (hipStream_t)stream;
-  float* coef = at<float>(workspace, w.coef);
-  int* rows = at<int>(workspace, w.rows);
-  int32_t* slot = at<int32_t>(workspace, w.slot);
-  int32_t* tc = at<int32_t>(workspace, w.tc);
-  float* lc = at<float>(workspace, w.lc);
-  bf16_t* hc = at<bf16_t>(workspace, w.hc);
-  bf16_t* dz = at<bf16_t>(workspace, w.dz);
-  float* dh32 = at<float>(workspace, w.dh);
-  float* kpart = at<float>(workspace, w.kpart);
   LS_STEP("head loss gather", st,
-          ls::head_gather(T, (int)H, (int)V, targets, dloss, (const bf16_t*)h, lse, slot, rows, coef, hc, tc, lc, st));
-  for (int64_t c0 = 0; c0 < V; c0 += w.bwd_piece) {
-    const int64_t cols = std::min(w.bwd_piece, V - c0);
-    {
-      ls::GemmArgs a = head_logits(T, H, V, c0, cols, ls::EPI_DZ);
-      a.A = hc;
-      a.B[0] = (const bf16_t*)embed + c0 * H;
-      a.target = tc;
-      a.lse = lc;
-      a.rows = rows;
-      a.C = dz;
-      a.ldc = w.ldz;
-      LS_STEP("head loss dz", st, ls::gemm(a, st));
-    }
-    if (dh) {
-      ls::GemmArgs a = head_dh(T, H, cols, w.ldz);
-      a.A = dz;
-      a.B[0] = (const bf16_t*)embed + c0 * H;
-      a.rows = rows;
-      a.F[0] = dh32;
-      a.accumulate = c0 > 0;
-      a.kpart = kpart;
-      a.kpart_floats = w.kpart_floats;
-      LS_STEP("head loss dh", st, ls::gemm(a, st));
-    }
-    if (d_embed || d_embed_bf16) {
-      ls::GemmArgs a = head_de(T, H, cols, w.ldz, d_embed_bf16 != nullptr);
-      a.A = dz;
-      a.B[0] = hc;
-      a.rows = rows;
-      a.coef = coef;
-      if (d_embed) a.F[0] = d_embed + c0 * H;
-      else a.C = (bf16_t*)d_embed_bf16 + c0 * H;
-      a.accumulate = accumulate != 0;
-      a.kpart = kpart;
-      a.kpart_floats = w.kpart_floats;
-      LS_STEP("head loss dE", st, ls::gemm(a, st));
-    }
-  }
-  if (dh) LS_STEP("head loss scatter", st, ls::head_scatter(T, (int)H, slot, coef, dh32, (bf16_t*)dh, st));
+          ls::head_gather(T, (int)H, (int)V, targets, dloss, (const bf16_t*)h, lse, at<int32_t>(workspace, w.slot),
+                          at<int>(workspace, w.rows), at<float>(workspace, w.coef), at<bf16_t>(workspace, w.hc),
+                          at<int32_t>(workspace, w.tc), at<float>(workspace, w.lc), st));
+  return head_products(w, T, H, V, (const bf16_t*)embed, 0.f, (bf16_t*)dh, d_embed, accumulate, (bf16_t*)d_embed_bf16,
+                       workspace, st);
+}
+
+// ---- log probabilities of given tokens ------------------------------------------------------
+
+static int check_logprob(int64_t tokens, int32_t hidden, int32_t vocab, int32_t piece, float scale, int32_t top) {
+  if (int e = check_head(tokens, hidden, vocab, piece)) return e;
+  if (!(scale > 0.0f) || !(scale <= 3.4e38f)) return fail(LS_ERR_SHAPE, "scale must be positive and finite");
+  if (top < 0) return fail(LS_ERR_SHAPE, "top must be >= 0");
+  if (top > ls::LOGPROB_TOP) return fail(LS_ERR_UNSUPPORTED, "top (%d) exceeds %d", top, ls::LOGPROB_TOP);
   return LS_OK;
+}
+static HeadKind logprob_kind(int32_t top) { return top > 0 ? HEAD_LOGPROB_TOP : HEAD_LOGPROB; }
+
+size_t ls_token_logprob_workspace(int64_t tokens, int32_t hidden, int32_t vocab, int32_t top, int32_t piece) {
+  return check_logprob(tokens, hidden, vocab, piece, 1.0f, top) ? 0 : head_ws(tokens, hidden, vocab, piece, logprob_kind(top)).total;
+}
+
+int ls_token_logprob_fwd(int64_t tokens, int32_t hidden, int32_t vocab, float scale, const ls_bf16* h,
+                         const ls_bf16* embed, const int32_t* targets, float* logprob, float* entropy, float* lse,
+                         int32_t top, int32_t* top_ids, float* top_logprob, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  if (int e = check_logprob(tokens, hidden, vocab, 0, scale, top)) return e;
+  const int64_t T = tokens, H = hidden, V = vocab;
+  const Range in[] = {{h, (size_t)(T * H * 2), "h"}, {embed, (size_t)(V * H * 2), "embed"}, {targets, (size_t)T * 4, "targets"}};
+  const Range out[] = {{logprob, (size_t)T * 4, "logprob"},
+                       {entropy, (size_t)T * 4, "entropy"},
+                       {lse, (size_t)T * 4, "lse"},
+                       {workspace, workspace_bytes, "workspace"},
+                       {top_ids, (size_t)T * top * 4, "top_ids"},
+                       {top_logprob, (size_t)T * top * 4, "top_logprob"}};
+  if (int e = check_ranges(in, 3, out, top > 0 ? 6 : 4)) return e;
+  const HeadWs w = head_ws(T, H, V, 0, logprob_kind(top));
+  if (workspace_bytes < w.fwd_total) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, w.fwd_total);
+  const hipStream_t st = (hipStream_t)stream;
+  float* stats = at<float>(workspace, w.stats);
+  float* zt = at<float>(workspace, w.zt);
+  float* gmax = top > 0 ? at<float>(workspace, w.gmax) : nullptr;
+  int64_t blocks = 0;
+  for (int64_t c0 = 0; c0 < V; c0 += w.fwd_piece) {
+    const int64_t cols = std::min(w.fwd_piece, V - c0);
+    ls::GemmArgs a = head_logits(T, H, V, c0, cols, ls::EPI_STAT);
+    a.A = (const bf16_t*)h;
+    a.B[0] = (const bf16_t*)embed + c0 * H;
+    a.target = targets;
+    a.stats = stats + blocks * T * 4;
+    a.zt = zt;
+    a.gmax = gmax;
+    a.scale2 = scale * kLog2e;
+    ls::GemmPlan used;
+    LS_STEP("logprob logits", st, ls::gemm(a, st, &used));
+    blocks += 2 * ((cols + used.bn - 1) / used.bn);
+  }
+  LS_STEP("logprob rows", st,
+          ls::logprob_rows(T, (int)V, blocks, scale, stats, zt, targets, logprob, entropy, lse, st));
+  if (top > 0)
+    LS_STEP("logprob top", st,
+            ls::logprob_top(T, (int)H, (int)V, top, scale, (const bf16_t*)h, (const bf16_t*)embed, gmax, lse, top_ids,
+                            top_logprob, st));
+  return LS_OK;
+}
+
+int ls_token_logprob_bwd(int64_t tokens, int32_t hidden, int32_t vocab, float scale, const ls_bf16* h,
+                         const ls_bf16* embed, const int32_t* targets, const float* entropy, const float* lse,
+                         const float* dlogprob, const float* dentropy, ls_bf16* dh, float* d_embed, int accumulate,
+                         ls_bf16* d_embed_bf16, int32_t piece, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int e = check_logprob(tokens, hidden, vocab, piece, scale, 0)) return e;
+  if (!dlogprob && !dentropy) return fail(LS_ERR_NULL, "dlogprob and dentropy are both NULL");
+  if (!dh && !d_embed && !d_embed_bf16) return fail(LS_ERR_NULL, "dh, d_embed and d_embed_bf16 are all NULL");
+  if (d_embed && d_embed_bf16) return fail(LS_ERR_UNSUPPORTED, "d_embed and d_embed_bf16 are both given");
+  if (d_embed_bf16 && accumulate) return fail(LS_ERR_UNSUPPORTED, "d_embed_bf16 is overwritten, never added to");
+  const int64_t T = tokens, H = hidden, V = vocab;
+  Range in[7] = {{h, (size_t)(T * H * 2), "h"},
+                 {embed, (size_t)(V * H * 2), "embed"},
+                 {targets, (size_t)T * 4, "targets"},
+                 {entropy, (size_t)T * 4, "entropy"},
+                 {lse, (size_t)T * 4, "lse"}};
+  size_t nin = 5, nout = 1;
+  if (dlogprob) in[nin++] = {dlogprob, (size_t)T * 4, "dlogprob"};
+  if (dentropy) in[nin++] = {dentropy, (size_t)T * 4, "dentropy"};
+  Range out[4] = {{workspace, workspace_bytes, "workspace"}};
+  if (dh) out[nout++] = {dh, (size_t)(T * H * 2), "dh"};
+  if (d_embed) out[nout++] = {d_embed, (size_t)(V * H * 4), "d_embed"};
+  if (d_embed_bf16) out[nout++] = {d_embed_bf16, (size_t)(V * H * 2), "d_embed_bf16"};
+  if (int e = check_ranges(in, nin, out, nout)) return e;
+  const HeadWs w = head_ws(T, H, V, piece, HEAD_LOGPROB);
+  if (workspace_bytes < w.bwd_total) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, w.bwd_total);
+  const hipStream_t st = (hipStream_t)stream;
+  const ls::LogprobGrads x{dlogprob, dentropy, entropy, at<float>(workspace, w.gc), at<float>(workspace, w.ec),
+                           at<float>(workspace, w.nc), scale};
+  LS_STEP("logprob gather", st,
+          ls::logprob_gather(T, (int)H, (int)V, targets, x, (const bf16_t*)h, lse, at<int32_t>(workspace, w.slot),
+                             at<int>(workspace, w.rows), at<float>(workspace, w.coef), at<bf16_t>(workspace, w.hc),
+                             at<int32_t>(workspace, w.tc), at<float>(workspace, w.lc), st));
+  return head_products(w, T, H, V, (const bf16_t*)embed, scale * kLog2e, (bf16_t*)dh, d_embed, accumulate,
+                       (bf16_t*)d_embed_bf16, workspace, st);
 }
 
 int ls_embed_fwd(int64_t tokens, int32_t hidden, int32_t vocab, const int32_t* ids, const ls_bf16* embed, ls_bf16* x,

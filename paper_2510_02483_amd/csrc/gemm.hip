@@ -326,7 +326,8 @@ hipError_t gemm(const GemmArgs& args, hipStream_t s, GemmPlan* used) {
     a.fill = (int)std::min<int64_t>(wgs, t == TILE_128 ? 2 * compute_units() : compute_units());
   }
   if (p.ks > 1 && t == TILE_256 && !f32_out(epi)) a.epi = EPI_PART;
-  hipError_t e = epi >= EPI_LSE ? gemm_head(a, t, s)
+  hipError_t e = epi >= EPI_STAT  ? gemm_logprob(a, t, s)
+                 : epi >= EPI_LSE ? gemm_head(a, t, s)
                  : a.a_kcontig ? (a.b_kcontig ? gemm_nt(a, t, s) : gemm_nn(a, t, s)) : gemm_tn(a, t, s);
   a.epi = epi;
   if (e != hipSuccess || (p.ks == 1 && a.fill == 0)) return e;

@@ -423,6 +423,79 @@ LS_DEV void lse_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw,
   else lse_rows<TM, TN, false>(p, acc, mw, nw, block, lr, lh);
 }
 
+// EPI_STAT: per row and wave the maximum m of scale z in base 2 (a wave's columns as in
+// EPI_LSE), the sum of 2^(z - m) and that of (z - m) 2^(z - m), from which come the
+// log-sum-exp and the entropy; the row's target logit (unscaled); and with gmax the largest
+// unscaled logit of every 16 columns, from which the largest of a row are found.  A lane's
+// eight values of either group of a 32-column block are reduced first, then both groups
+// across the halves of the wave with one lane swap, so that the groups cost nothing that
+// the row's maximum does not need anyway but their store, 4 bytes for 16 logits.
+// (z - m) of a logit of -inf counts as -1000, as 2^-inf times it would be NaN.
+template <int TM, int TN, bool EDGE>
+LS_DEV void stat_rows(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw, int nw, int block, int lr, int lh) {
+  int t[TM];  // target as a column of the wave's
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = mw + 32 * i + lr;
+    t[i] = m < p.M ? p.target[m] : -1;
+    t[i] = t[i] < 0 ? -1 : t[i] - p.col0 - nw;
+  }
+  const int cols = p.N - nw - 4 * lh;  // EDGE: the lane's columns 32j + 8q + e below this count
+  const float k = p.scale2;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = mw + 32 * i + lr;
+    auto z = [&](int j, int r) {
+      return EDGE && 32 * j + 8 * (r >> 2) + (r & 3) >= cols ? -INFINITY : acc[i][j][r];
+    };
+    float g[TN];  // of columns 32j + 16lh .. + 15
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      float a = -INFINITY, b = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        a = fmaxf(a, z(j, r));
+        b = fmaxf(b, z(j, 8 + r));
+      }
+      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+      g[j] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    }
+    if (p.gmax && m < p.M) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) p.gmax[(int64_t)((p.col0 + nw) / 16 + 2 * j + lh) * p.M + m] = g[j];
+    }
+    float mx = g[0];
+#pragma unroll
+    for (int j = 1; j < TN; ++j) mx = fmaxf(mx, g[j]);
+    mx = halves_max(mx);
+    const float m2 = mx * k, ref = mx == -INFINITY ? 0.f : m2;
+    float s[2] = {0.f, 0.f}, u[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float d = fmaf(z(j, r), k, -ref), e = __builtin_amdgcn_exp2f(d);
+        s[r & 1] += e;
+        u[r & 1] = fmaf(e, fmaxf(d, -1000.0f), u[r & 1]);
+      }
+    const float sum = halves_sum(s[0] + s[1]), dot = halves_sum(u[0] + u[1]);
+    if (lh == 0 && m < p.M) *(f32x4*)(p.stats + 4 * ((int64_t)block * p.M + m)) = f32x4{m2, sum, dot, 0.f};
+    if (__builtin_amdgcn_ballot_w64(t[i] >= 0 && t[i] < 32 * TN)) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * j + 8 * (r >> 2) + 4 * lh + (r & 3) == t[i]) p.zt[m] = acc[i][j][r];
+    }
+    __builtin_amdgcn_sched_barrier(0);  // one row block's values in vector registers at a time
+  }
+}
+template <int TM, int TN>
+LS_DEV void stat_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw, int nw, int block, int lr, int lh) {
+  if (nw + 32 * TN > p.N) stat_rows<TM, TN, true>(p, acc, mw, nw, block, lr, lh);
+  else stat_rows<TM, TN, false>(p, acc, mw, nw, block, lr, lh);
+}
+
 // EPI_DZ: what a row's logits become: softmax(z) - onehot, NaN in a row whose
 // target is out of range.  One rounding, to bf16, as the operand of the
 // gradients' products; the loss's factor comes after them, in fp32: with it, the
@@ -444,7 +517,42 @@ struct DzRow {
   // logit z of the product's column n
   LS_DEV float operator()(float z, int n) const { return p(z) - (n == t ? 1.f : 0.f); }
   LS_DEV float p(float z) const { return __builtin_amdgcn_exp2f(fmaf(z, EPI_LOG2E, -l2)); }
+  LS_DEV float target(float z) const { return p(z) - 1.f; }
 };
+
+// EPI_DLP: the gradient, for the scaled logits z, of g logprob + e entropy over the
+// common factor c (the largest |g| and |e| of all rows, so that the target's entry of
+// rows with the same g is exactly 1 less p, as above):
+//   dz = (g / c) (onehot - p) - (e / c) p (ln p + H).
+// With x = log2 p this is p (b x + a), a = -(g + e H) / c and b = -(e / c) ln 2; NaN in a
+// row whose target is out of range, or whose g or e is not finite.
+struct DlpRow {
+  float l2, k, a, b, g;
+  int t;
+  LS_DEV DlpRow() {}
+  LS_DEV DlpRow(const GemmArgs& p, int M, int m) {
+    const bool in = m < M;
+    k = p.scale2;
+    t = in ? p.target[m] : 0;
+    const float c = p.cmax[0], gm = in ? p.dlogp[m] : 0.f, em = in ? p.dent[m] : 0.f;
+    const bool ok = t >= 0 && t < p.vocab && fabsf(gm) < INFINITY && fabsf(em) < INFINITY;
+    l2 = in ? (ok ? p.lse[m] * EPI_LOG2E : NAN) : 0.f;
+    g = c > 0.f ? gm / c : 0.f;
+    const float e = c > 0.f ? em / c : 0.f;
+    a = in ? -fmaf(e, p.ent[m], g) : 0.f;
+    b = -e * 0.6931471805599453f;
+    t -= p.col0;
+  }
+  LS_DEV float operator()(float z, int n) const { return n == t ? target(z) : p(z); }
+  LS_DEV float p(float z) const {
+    const float x = fmaf(z, k, -l2);
+    return __builtin_amdgcn_exp2f(x) * fmaf(fmaxf(x, -1000.0f), b, a);  // (an x of -inf: 0, not NaN)
+  }
+  LS_DEV float target(float z) const { return p(z) + g; }
+};
+constexpr bool is_dz(int epi) { return epi == EPI_DZ || epi == EPI_DLP; }
+template <int EPI>
+using DzOf = std::conditional_t<EPI == EPI_DLP, DlpRow, DzRow>;
 
 // Epilogue of a 128-column tile (all but the fp32 weight gradients): 8 columns
 // per lane and step, straight from the registers.  c0, c1: tile-local first
@@ -476,8 +584,8 @@ LS_DEV void small_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int M
         }
       } else if constexpr (EPI == EPI_ROPE || EPI == EPI_ROPE64) {
         if (na < p.N) store_rope8<EPI == EPI_ROPE ? 128 : 64>(p, m, na, a, b);
-      } else if constexpr (EPI == EPI_DZ) {
-        const DzRow row(p, M, m);
+      } else if constexpr (is_dz(EPI)) {
+        const DzOf<EPI> row(p, M, m);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {  // columns past N, up to the next multiple of 8, become 0
           a[e] = na + e < p.N ? row(a[e], na + e) : 0.f;
@@ -557,7 +665,7 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
   // the head loss's products count only the rows that have a target, as many as
   // the device says (a split product with k-strided operands and a bf16 result
   // is one of them too)
-  constexpr bool DEV_M = EPI == EPI_DZ || EPI == EPI_DH;
+  constexpr bool DEV_M = is_dz(EPI) || EPI == EPI_DH;
   constexpr bool DEV_K = EPI == EPI_DE || EPI == EPI_DE16 || (EPI == EPI_PART && !AK);
   constexpr uint32_t A_BYTES = AK ? (BM / 8) * KC_PITCH : BM * KT * 2;
   constexpr uint32_t B_BYTES = BKC ? (BN / 8) * KC_PITCH : BN * KT * 2;
@@ -851,6 +959,10 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
     lse_epilogue<TM, TN>(p, acc, m0 + wm * WM, n0 + wn * WN, 2 * tn + wn, lr, lh);
     return;
   }
+  if constexpr (EPI == EPI_STAT) {
+    stat_epilogue<TM, TN>(p, acc, m0 + wm * WM, n0 + wn * WN, 2 * tn + wn, lr, lh);
+    return;
+  }
   if constexpr (SMALL && !F32OUT) {
     small_epilogue<EPI, TM, TN>(p, acc, M, m0 + wm * WM, n0, bcol(0), bcol(1), slice, ks, lr, lh);
     return;
@@ -901,7 +1013,7 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
     }
   };
 
-  if constexpr ((SMALL && !F32OUT) || EPI == EPI_PART || EPI == EPI_LSE) {
+  if constexpr ((SMALL && !F32OUT) || EPI == EPI_PART || EPI == EPI_LSE || EPI == EPI_STAT) {
   } else if constexpr (F32OUT) {
     // fp32 weight gradients straight from the registers: a lane's 4 columns are
     // 16 contiguous bytes (read-modify-write with accumulate).  Slices 1.. of a
@@ -1092,13 +1204,13 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
       }
     }
   } else {
-    // EPI_BF16, EPI_DZ, EPI_DE16, EPI_ROPE, EPI_ROPE64
+    // EPI_BF16, EPI_DZ, EPI_DLP, EPI_DE16, EPI_ROPE, EPI_ROPE64
     float coef = 1.f;
     if constexpr (EPI == EPI_DE16) coef = p.coef[0];
-    DzRow dzr[TM];
-    if constexpr (EPI == EPI_DZ) {
+    DzOf<EPI> dzr[TM];
+    if constexpr (is_dz(EPI)) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) dzr[i] = DzRow(p, M, mw + 32 * i + lr);
+      for (int i = 0; i < TM; ++i) dzr[i] = DzOf<EPI>(p, M, mw + 32 * i + lr);
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -1155,7 +1267,7 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
-            if constexpr (EPI == EPI_DZ) {
+            if constexpr (is_dz(EPI)) {
 #pragma unroll
               for (int e = 0; e < 4; ++e) v[e] = dzr[i].p(v[e]);
             }
@@ -1165,7 +1277,7 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
             }
             put4(32 * i + lr, 32 * j + 8 * q + 4 * lh, v);
           }
-        if constexpr (EPI == EPI_DZ) {
+        if constexpr (is_dz(EPI)) {
           // the few targets among these columns, over their staged probabilities; then
           // zeros in the columns from N to the next multiple of 8
           const int c = dzr[i].t - nw;
@@ -1175,7 +1287,7 @@ __global__ __launch_bounds__(NW * 64, 1) void gemm_kernel(GemmArgs p) {
 #pragma unroll
               for (int r = 0; r < 16; ++r)
                 if (32 * j + 8 * (r >> 2) + 4 * lh + (r & 3) == c)
-                  stg[sb(32 * i + lr, c)] = (bf16_t)f2bf(dzr[i].p(acc[i][j][r]) - 1.f);
+                  stg[sb(32 * i + lr, c)] = (bf16_t)f2bf(dzr[i].target(acc[i][j][r]));
           }
           for (int z = p.N - nw; z >= 0 && z < WN && (z & 7); ++z)
             if (lh == 0) stg[sb(32 * i + lr, z)] = 0;

@@ -17,6 +17,8 @@
 // block forward, a copy of h and of dh backward.
 #include <math.h>
 
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -143,6 +145,8 @@ __global__ __launch_bounds__(HL_THREADS) void head_mean_kernel(int64_t T, int V,
 // them by itself (4 bytes a row, from the L2), so that one launch does it all; the
 // last one sees every row and leaves the number and the factor.
 // Bound by HBM bandwidth: h is read once and written once.
+// LOGPROB: the rows' gradients and entropies go along, and the factor is the largest of the gradients.
+template <bool LOGPROB>
 __global__ __launch_bounds__(HL_GATHER) void head_gather_kernel(int64_t T, int H, int V, int64_t per,
                                                                 const int32_t* __restrict__ targets,
                                                                 const float* __restrict__ dloss,
@@ -150,16 +154,27 @@ __global__ __launch_bounds__(HL_GATHER) void head_gather_kernel(int64_t T, int H
                                                                 const float* __restrict__ lse,
                                                                 int32_t* __restrict__ slot, int* __restrict__ rows,
                                                                 float* __restrict__ coef, bf16_t* __restrict__ hc,
-                                                                int32_t* __restrict__ tc, float* __restrict__ lc) {
+                                                                int32_t* __restrict__ tc, float* __restrict__ lc,
+                                                                LogprobGrads x) {
   constexpr int WAVES = HL_GATHER / 64;
   __shared__ int part[2][WAVES], place[HL_GATHER];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t r0 = (int64_t)blockIdx.x * per, r1 = r0 + per < T ? r0 + per : T;
   int before = 0, valid = 0;
+  float most = 0.f;  // (of the last workgroup's rows, all of them)
+  auto larger = [&](int64_t t, int g) {
+    if constexpr (LOGPROB) {
+      if (blockIdx.x + 1 < gridDim.x || !has_target(g, V)) return;
+      const float a = x.g ? fabsf(x.g[t]) : 0.f, b = x.e ? fabsf(x.e[t]) : 0.f;
+      if (a < INFINITY) most = fmaxf(most, a);
+      if (b < INFINITY) most = fmaxf(most, b);
+    }
+  };
   for (int64_t t = tid; t < r0; t += HL_GATHER) {
     const int g = targets[t];
     before += g != -1;
     valid += has_target(g, V);
+    larger(t, g);
   }
   auto sum = [&](int v, int* p) {
 #pragma unroll
@@ -176,6 +191,7 @@ __global__ __launch_bounds__(HL_GATHER) void head_gather_kernel(int64_t T, int H
     const int64_t t = c0 + tid;
     const int g = t < r1 ? targets[t] : -1;
     valid += has_target(g, V);
+    if (t < r1) larger(t, g);
     const unsigned long long in = __ballot(g != -1);
     if (lane == 0) part[1][wave] = __popcll(in);
     __syncthreads();
@@ -191,6 +207,11 @@ __global__ __launch_bounds__(HL_GATHER) void head_gather_kernel(int64_t T, int H
       if (g != -1) {
         tc[at] = g;
         lc[at] = lse[t];
+        if constexpr (LOGPROB) {
+          x.gc[at] = x.g ? x.g[t] : 0.f;
+          x.ec[at] = x.e ? x.e[t] : 0.f;
+          x.nc[at] = x.ent[t];
+        }
       }
     }
     __syncthreads();
@@ -205,6 +226,18 @@ __global__ __launch_bounds__(HL_GATHER) void head_gather_kernel(int64_t T, int H
     __syncthreads();
   }
   if (blockIdx.x + 1 < gridDim.x) return;
+  if constexpr (LOGPROB) {
+    __shared__ float big[WAVES];
+    most = wave_max(most);
+    if (lane == 0) big[wave] = most;
+    __syncthreads();
+    if (tid > 0) return;
+    for (int w = 0; w < WAVES; ++w) most = fmaxf(most, big[w]);
+    rows[0] = before;
+    coef[0] = most * x.scale;
+    coef[1] = most;
+    return;
+  }
   valid = sum(valid, part[0]);
   if (tid == 0) {
     rows[0] = before;
@@ -247,14 +280,24 @@ hipError_t head_rows(int64_t T, int V, int64_t blocks, const float* stats, const
   return hipGetLastError();
 }
 
+// a row per wave, or as many as leave 512 workgroups
+static int64_t gather_rows(int64_t T) { return std::max<int64_t>((T + 511) / 512, HL_GATHER / 64); }
+
 hipError_t head_gather(int64_t T, int H, int V, const int32_t* targets, const float* dloss, const bf16_t* h,
                        const float* lse, int32_t* slot, int* rows, float* coef, bf16_t* hc, int32_t* tc, float* lc,
                        hipStream_t s) {
-  // a row per wave, or as many as leave 512 workgroups
-  int64_t per = (T + 511) / 512;
-  if (per < HL_GATHER / 64) per = HL_GATHER / 64;
-  hipLaunchKernelGGL(head_gather_kernel, dim3((unsigned)((T + per - 1) / per)), dim3(HL_GATHER), 0, s, T, H, V, per,
-                     targets, dloss, h, lse, slot, rows, coef, hc, tc, lc);
+  const int64_t per = gather_rows(T);
+  hipLaunchKernelGGL((head_gather_kernel<false>), dim3((unsigned)((T + per - 1) / per)), dim3(HL_GATHER), 0, s, T, H, V,
+                     per, targets, dloss, h, lse, slot, rows, coef, hc, tc, lc, LogprobGrads{});
+  return hipGetLastError();
+}
+
+hipError_t logprob_gather(int64_t T, int H, int V, const int32_t* targets, const LogprobGrads& x, const bf16_t* h,
+                          const float* lse, int32_t* slot, int* rows, float* coef, bf16_t* hc, int32_t* tc, float* lc,
+                          hipStream_t s) {
+  const int64_t per = gather_rows(T);
+  hipLaunchKernelGGL((head_gather_kernel<true>), dim3((unsigned)((T + per - 1) / per)), dim3(HL_GATHER), 0, s, T, H, V,
+                     per, targets, (const float*)nullptr, h, lse, slot, rows, coef, hc, tc, lc, x);
   return hipGetLastError();
 }
 

@@ -31,6 +31,8 @@ enum Epilogue {
   EPI_DH = 9,       // F (fp32) (+)= acc
   EPI_DE = 10,      // F (fp32) (+)= coef acc
   EPI_DE16 = 11,    // C (bf16) = coef acc
+  EPI_STAT = 12,    // acc are logits: as EPI_LSE with what the entropy needs, and the largest of every 16 columns
+  EPI_DLP = 13,     // C (bf16) = gradient of log probability and entropy for the scaled logits, over a common factor
 };
 
 struct GemmArgs {
@@ -60,7 +62,9 @@ struct GemmArgs {
   // EPI_LSE and EPI_DZ: columns are entries col0 .. col0 + N - 1 of a vocabulary, row m has target[m] (-1: none)
   int col0 = 0, vocab = 0;
   const int32_t* target = nullptr;
-  float* stats = nullptr;       // EPI_LSE: [column block][M] (max, sum of exp(z - max)); two blocks per tile column
+  // EPI_LSE: [column block][M] (max, sum of exp(z - max)); two blocks per tile column.  EPI_STAT: [column block][M]
+  // (m = max of the scaled logits in base 2, sum of 2^(z - m), sum of (z - m) 2^(z - m), 0)
+  float* stats = nullptr;
   float* zt = nullptr;          // EPI_LSE: [M], the logit of a row's target where this product has it
   const float* lse = nullptr;   // EPI_DZ: [M]
   const float* coef = nullptr;  // EPI_DE, EPI_DE16: one factor of the results (on the device)
@@ -75,6 +79,14 @@ struct GemmArgs {
   int ksplit = 1;   // slices of K (set by gemm())
   int fill = 0;     // EPI_DH: workgroups that its slices may fill when the rows are few (set by gemm())
   int group_m = 8;  // tile rows per group of the launch order (set by the launch)
+  // EPI_STAT and EPI_DLP: what a logit is multiplied with, times log2(e)
+  float scale2 = 0.f;
+  float* gmax = nullptr;  // EPI_STAT: null, or [columns of the vocabulary / 16][M], the largest logit of each 16
+  // EPI_DLP: the rows' gradients of log probability and entropy, the entropy [M], and the common factor (one)
+  const float* dlogp = nullptr;
+  const float* dent = nullptr;
+  const float* ent = nullptr;
+  const float* cmax = nullptr;
 };
 
 // The workgroup tile and the slices of K of a launch.
@@ -101,6 +113,7 @@ hipError_t gemm_nt(const GemmArgs& a, GemmTile t, hipStream_t s);
 hipError_t gemm_nn(const GemmArgs& a, GemmTile t, hipStream_t s);
 hipError_t gemm_tn(const GemmArgs& a, GemmTile t, hipStream_t s);
 hipError_t gemm_head(const GemmArgs& a, GemmTile t, hipStream_t s);  // the instances that only the head loss uses
+hipError_t gemm_logprob(const GemmArgs& a, GemmTile t, hipStream_t s);  // EPI_STAT, EPI_DLP
 // Force the tile shape of later gemm launches (bm, bn in {256, 192}; 0, 0 =
 // automatic).  Variants that only exist as 256 x 256 ignore it.  -1 on bad sizes.
 int gemm_tile_override(int bm, int bn);
@@ -208,9 +221,30 @@ hipError_t head_rows(int64_t T, int V, int64_t blocks, const float* stats, const
 hipError_t head_gather(int64_t T, int H, int V, const int32_t* targets, const float* dloss, const bf16_t* h,
                        const float* lse, int32_t* slot, int* rows, float* coef, bf16_t* hc, int32_t* tc, float* lc,
                        hipStream_t s);
+// The same with the rows' gradients of log probability and entropy (null: 0) and the entropy, gathered to gc, ec and
+// nc; coef[0] = scale c, coef[1] = c, the largest finite |g| or |e| of a row with a target in [0, V).
+struct LogprobGrads {
+  const float *g, *e, *ent;
+  float *gc, *ec, *nc;
+  float scale;
+};
+hipError_t logprob_gather(int64_t T, int H, int V, const int32_t* targets, const LogprobGrads& x, const bf16_t* h,
+                          const float* lse, int32_t* slot, int* rows, float* coef, bf16_t* hc, int32_t* tc, float* lc,
+                          hipStream_t s);
 // dh[t] = coef dhc[slot[t]] rounded to bf16, 0 for a row without a target.
 hipError_t head_scatter(int64_t T, int H, const int32_t* slot, const float* coef, const float* dhc, bf16_t* dh,
                         hipStream_t s);
+
+// ---- log probabilities of given tokens -------------------------------------------------
+// Per row from EPI_STAT's statistics: lse of the scaled logits; logprob and entropy (both 0 without a target, NaN for
+// one outside [-1, V)).
+hipError_t logprob_rows(int64_t T, int V, int64_t blocks, float scale, const float* stats, const float* zt,
+                        const int32_t* targets, float* logprob, float* entropy, float* lse, hipStream_t s);
+// The `top` (1 .. 64) largest logits of every row, ties to the lower column, from the largest of every 16 columns
+// (gmax [ceil(V / 16)][T]): ids (-1 past the vocabulary) and scaled logit - lse.
+constexpr int LOGPROB_TOP = 64;
+hipError_t logprob_top(int64_t T, int H, int V, int top, float scale, const bf16_t* h, const bf16_t* embed,
+                       const float* gmax, const float* lse, int32_t* ids, float* logprob, hipStream_t s);
 
 // ---- gradients of many tensors ------------------------------------------------------
 constexpr int GN_TENSORS = 96;  // tensors that one launch takes

@@ -131,6 +131,13 @@ _PROTOS = {
                                         ctypes.c_size_t, _P]),
     "ls_head_loss_bwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P, _P, _P, _P,
                                         ctypes.c_int, _P, ctypes.c_int32, _P, ctypes.c_size_t, _P]),
+    "ls_token_logprob_workspace": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                                     ctypes.c_int32]),
+    "ls_token_logprob_fwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, _P, _P, _P, _P,
+                                            _P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_size_t, _P]),
+    "ls_token_logprob_bwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, _P, _P, _P, _P,
+                                            _P, _P, _P, _P, _P, ctypes.c_int, _P, ctypes.c_int32, _P, ctypes.c_size_t,
+                                            _P]),
     "ls_embed_fwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P]),
     "ls_embed_bwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P]),
     "ls_adamw_workspace": (ctypes.c_size_t, []),
@@ -492,6 +499,46 @@ def ls_head_loss_bwd(h, embed, targets, lse, dloss, dh, d_embed, accumulate, wor
     _check(lib().ls_head_loss_bwd(T, H, embed.shape[0], _p(h), _p(embed), _p(targets), _p(lse), _p(dloss), _p(dh),
                                   None if low else _p(d_embed), int(accumulate), _p(d_embed) if low else None,
                                   int(piece), _p(workspace), _bytes(workspace), _stream(stream)), "ls_head_loss_bwd")
+
+
+def ls_token_logprob_workspace(tokens: int, hidden: int, vocab: int, top: int = 0, piece: int = 0) -> int:
+    return lib().ls_token_logprob_workspace(int(tokens), int(hidden), int(vocab), int(top), int(piece))
+
+
+def ls_token_logprob_fwd(h, embed, targets, logprob, entropy, lse, workspace, scale=1.0, top_ids=None,
+                         top_logprob=None, stream=None):
+    """top_ids (int32) and top_logprob (fp32), [tokens, top] both, or None both: no alternatives."""
+    T, H = h.shape
+    if (top_ids is None) != (top_logprob is None):
+        raise ValueError("top_ids and top_logprob go together")
+    top = 0 if top_ids is None else top_ids.numel() // max(T, 1)
+    _need(("h", h, _BF16, T * H), ("embed", embed, _BF16, embed.shape[0] * H), ("targets", targets, torch.int32, T),
+          ("logprob", logprob, _F32, T), ("entropy", entropy, _F32, T), ("lse", lse, _F32, T),
+          ("top_ids", top_ids, torch.int32, T * top), ("top_logprob", top_logprob, _F32, T * top),
+          ("workspace", workspace, None, None))
+    if top_ids is not None and (top == 0 or top_logprob.numel() != T * top):
+        raise ValueError("top_ids and top_logprob must both be [tokens, top]")
+    _check(lib().ls_token_logprob_fwd(T, H, embed.shape[0], scale, _p(h), _p(embed), _p(targets), _p(logprob),
+                                      _p(entropy), _p(lse), top, _p(top_ids), _p(top_logprob), _p(workspace),
+                                      _bytes(workspace), _stream(stream)), "ls_token_logprob_fwd")
+
+
+def ls_token_logprob_bwd(h, embed, targets, entropy, lse, dlogprob, dentropy, dh, d_embed, accumulate, workspace,
+                         scale=1.0, piece=0, stream=None):
+    """dlogprob or dentropy (fp32 [tokens]) may be None (0), and so may dh or d_embed; d_embed: fp32, added to with
+    ``accumulate``, or bf16, always overwritten."""
+    T, H = h.shape
+    low = d_embed is not None and d_embed.dtype == torch.bfloat16
+    _need(("h", h, _BF16, T * H), ("embed", embed, _BF16, embed.shape[0] * H), ("targets", targets, torch.int32, T),
+          ("entropy", entropy, _F32, T), ("lse", lse, _F32, T), ("dlogprob", dlogprob, _F32, T),
+          ("dentropy", dentropy, _F32, T), ("dh", dh, _BF16, T * H),
+          ("d_embed", d_embed, _BF16 if low else _F32, embed.shape[0] * H), ("workspace", workspace, None, None))
+    if low and accumulate:
+        raise ValueError("a bf16 d_embed is overwritten, never added to")
+    _check(lib().ls_token_logprob_bwd(T, H, embed.shape[0], scale, _p(h), _p(embed), _p(targets), _p(entropy), _p(lse),
+                                      _p(dlogprob), _p(dentropy), _p(dh), None if low else _p(d_embed), int(accumulate),
+                                      _p(d_embed) if low else None, int(piece), _p(workspace), _bytes(workspace),
+                                      _stream(stream)), "ls_token_logprob_bwd")
 
 
 def ls_embed_fwd(ids, embed, x, stream=None):
