@@ -75,6 +75,11 @@ LS_DEV u32x4 pack_frag(const f32x16& v, int r0) {
                pack_bf2(v[r0 + 6], v[r0 + 7])};
 }
 LS_DEV float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
+// s plus the two bf16 values of a word.
+LS_DEV float add_bf2(uint32_t w, float s) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3f803f80u), s, false);
+}
 
 // What a score is, in the base-2 exponent of the softmax, and which keys a query sees.
 // PlainScore: q.k times a scale, every key up to the query.
@@ -86,7 +91,8 @@ LS_DEV float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 // scale of dq and dk.
 struct PlainScore {
   static constexpr bool ON = false, CAPPED = false;
-  static constexpr int window = 0;  // (unused)
+  static constexpr int window = 0;  // (unused, as c2)
+  static constexpr float c2 = 0.f;
 };
 template <bool CAP>
 struct ModScore {
@@ -365,7 +371,7 @@ LS_DEV void short_fwd(const AttnShape& sh, const SC& sc, const PackedTile& t, in
     }
     if constexpr (SC::CAPPED) sl2 = 1.0f;  // (scores in base 2 already)
     const float m = halves_max(mx) * sl2;
-    float sum = 0.f;
+    float sum = 0.f, sumb = 0.f;  // (ON: also of the probabilities as rounded, as in attn_fwd_kernel)
     f32x16 oacc[D / 32];
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) oacc[i] = f32x16{};
@@ -379,13 +385,17 @@ LS_DEV void short_fwd(const AttnShape& sh, const SC& sc, const PackedTile& t, in
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const u32x4 pf = pack_frag(s[b], 8 * c);
+        if constexpr (SC::ON) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) sumb = add_bf2(pf[w], sumb);
+        }
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) oacc[i] = mfma32(colt_frag<D>(vt + 32 * b * D, 32 * i, c, lane), pf, oacc[i]);
       }
     }
-    const float l = halves_sum(sum);
+    const float l = halves_sum(sum), lb = SC::ON ? halves_sum(sumb) : l;
     if (32 * qb + lr >= t.len) continue;
-    const float inv = 1.0f / l;
+    const float inv = 1.0f / lb;
     const int64_t at_row = (t.start + (int64_t)(32 * qb + lr)) * nq * hd + h * hd;
     bf16_t* orow = o + at_row;
 #pragma unroll
@@ -401,7 +411,7 @@ LS_DEV void short_fwd(const AttnShape& sh, const SC& sc, const PackedTile& t, in
 }
 
 template <int D, bool PACKED, class SC>
-__global__ __launch_bounds__(256, PACKED && D == 64 ? 4 : 2) void attn_fwd_kernel(
+__global__ __launch_bounds__(256, PACKED && D == 64 ? (SC::ON ? 3 : 4) : 2) void attn_fwd_kernel(
     AttnShape sh, PackedView pk, const bf16_t* __restrict__ qkv, bf16_t* __restrict__ o, float* __restrict__ lse,
     float sl2, SC sc) {
   __shared__ __attribute__((aligned(1024))) bf16_t Ks[2][BKV * D];
@@ -462,6 +472,13 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 4 : 2) void attn_fwd_kerne
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
   // (a window may leave a query no key of a tile: its maximum stays finite then)
   float m = SC::ON ? -3.402823466e38f : -INFINITY, l = 0.f;
+  // ON: the sum of the probabilities as rounded for their product with V.  O over it, not over l, has a rounding
+  // in common above and below, and a query whose weight lies on one key gets that key's values: o + rest was 0.0011 of its
+  // norm off over l with scores of a standard deviation of 4.  The log-sum-exp stays that of the unrounded.
+  float lb = 0.f;
+  // Capped: in the tile's registers r = (1 - tanh) / 2 stands for the score, which falls with it: its least value is
+  // the largest score's, a hidden key's is +inf, and one more fma makes it the exponent.
+  constexpr float HIDDEN = SC::CAPPED ? INFINITY : -INFINITY;
 
   // operand reads by per-lane LDS address (K rows, V^T columns); the stage,
   // the array, the 32-key block and the 16-key step add constants
@@ -497,42 +514,49 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 4 : 2) void attn_fwd_kerne
 #pragma unroll
         for (int bb = 0; bb < BKV / 32; ++bb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[bb][r] = sc.less(sc.half(sacc[bb][r]), 0.f);
+          for (int r = 0; r < 16; ++r) sacc[bb][r] = sc.half(sacc[bb][r]);
       }
       if (edge) {
 #pragma unroll
         for (int bb = 0; bb < BKV / 32; ++bb)
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (hidden_key(sc, kv0 + 32 * bb + 8 * (r >> 2) + 4 * lh + (r & 3), qrow)) sacc[bb][r] = -INFINITY;
+            if (hidden_key(sc, kv0 + 32 * bb + 8 * (r >> 2) + 4 * lh + (r & 3), qrow)) sacc[bb][r] = HIDDEN;
       }
-      float mx = -INFINITY;
+      float mx = HIDDEN;
 #pragma unroll
       for (int bb = 0; bb < BKV / 32; ++bb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[bb][r]);
+        for (int r = 0; r < 16; ++r) mx = SC::CAPPED ? fminf(mx, sacc[bb][r]) : fmaxf(mx, sacc[bb][r]);
       // key 0 is visible to every query: finite from the first tile on
-      const float mc = fmaxf(m, SC::CAPPED ? halves_max(mx) : halves_max(mx) * sl2);
+      const float mc = fmaxf(m, SC::CAPPED ? fmaf(halves_max(-mx), 2.0f * sc.c2, sc.c2) : halves_max(mx) * sl2);
       if (__builtin_amdgcn_ballot_w64(mc > m + LAG)) {
         const float alpha = ex2(m - mc);
         m = mc;
         l *= alpha;
+        if constexpr (SC::ON) lb *= alpha;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) oacc[i] *= alpha;
       }
       float ls = 0.f;
+      const float top = sc.c2 - m;
 #pragma unroll
       for (int bb = 0; bb < BKV / 32; ++bb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = ex2(SC::CAPPED ? sacc[bb][r] - m : fmaf(sacc[bb][r], sl2, -m));
+          const float p = ex2(SC::CAPPED ? fmaf(sacc[bb][r], -2.0f * sc.c2, top) : fmaf(sacc[bb][r], sl2, -m));
           sacc[bb][r] = p;
           ls += p;
         }
-      l += halves_sum(ls);
+      if constexpr (SC::ON) l += ls;  // (this lane's keys: the halves are added at the end)
+      else l += halves_sum(ls);
 #pragma unroll
       for (int s = 0; s < BKV / 16; ++s) {
         const u32x4 pf = pack_frag(sacc[s >> 1], 8 * (s & 1));
+        if constexpr (SC::ON) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) lb = add_bf2(pf[w], lb);
+        }
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
           oacc[i] = mfma32(fa.cols(i, v_minus_k + cur * STAGE + s * 16 * D * 2), pf, oacc[i]);
@@ -545,8 +569,12 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 4 : 2) void attn_fwd_kerne
     if (kt + 1 < nkt) step(std::integral_constant<int, 1>{}, kt + 1);
   }
 
+  if constexpr (SC::ON) {
+    l = halves_sum(l);
+    lb = halves_sum(lb);
+  }
   if (qrow < S) {
-    const float inv = 1.0f / l;
+    const float inv = 1.0f / (SC::ON ? lb : l);
     bf16_t* orow = o + (qtile.row0 + qrow) * nq * hd + h * hd;
     if constexpr (SC::ON) store_rest<D>(sc, (qtile.row0 + qrow) * nq * hd + h * hd, oacc, inv, hd, lh);
 #pragma unroll

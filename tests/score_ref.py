@@ -47,7 +47,10 @@ def attention(qkv, lens, first, nq, nkv, d, dout=None, scale=0.0, cap=0.0, windo
             o[a:b, hq] = p @ v
             lse[h, a:b] = (m + np.log(l))[:, 0]
             pv = p @ np.abs(v)
-            err_o = U * (np.abs(o[a:b, hq]) + pv) * 1.01 + slack * pv + n * W * pv
+            # o is sum p' v / sum p' of rounded p' = p (1 + u): off by sum p u (v - o), so by U sum p |v - o| and
+            # U sqrt(sum p (v - o)^2) at most
+            spread = np.sqrt(np.maximum(p @ (v * v) - o[a:b, hq] ** 2, 0.0))
+            err_o = U * (np.abs(o[a:b, hq]) + spread) * 1.01 + 2 * slack * pv + n * W * pv
             tol["o"][a:b, hq] = err_o
             mag = np.where(seen, np.abs(q) @ np.abs(k).T * sc, 0.0).max(1)
             tol["lse"][h, a:b] = 2.0 * d * W * mag + (n + 64) * W + 4 * W * np.abs(lse[h, a:b]) + off

