@@ -1641,6 +1641,7 @@ struct HeadWs {
   size_t stats, zt, gmax, fwd_total;
   size_t coef, rows, slot, tc, lc, gc, ec, nc, hc, dz, dh, kpart, bwd_total, total;
   int64_t kpart_floats;
+  int gmax_groups, gmax_rows;
 };
 // What the workspace is for: the head loss, or log probabilities (with gradients of each row, and with top
 // alternatives or without).
@@ -1704,8 +1705,11 @@ static HeadWs head_ws(int64_t T, int64_t H, int64_t V, int64_t piece, HeadKind k
   }
   w.stats = f.take((size_t)(blocks * T * (kind ? 16 : 8)));
   w.zt = f.take((size_t)T * 4);
-  // (whole tiles write their groups of 16 columns past the vocabulary too)
-  w.gmax = f.take(kind == HEAD_LOGPROB_TOP ? (size_t)((V + 255) / 256 * 16 * T * 4) : 0);
+  // (whole tiles write their groups of 8 columns past the vocabulary too)
+  w.gmax_groups = (int)((V + 255) / 256 * 32);
+  w.gmax_rows = 0;
+  while (w.gmax_rows < 4 && ((int64_t)1 << w.gmax_rows) < T) ++w.gmax_rows;
+  w.gmax = f.take(kind == HEAD_LOGPROB_TOP ? (size_t)ls::gmax_at(w.gmax_groups, w.gmax_rows, T + (1 << w.gmax_rows) - 1, 0) * 4 : 0);
   w.fwd_total = f.off;
   Carver b;
   w.coef = b.take(16);
@@ -1917,17 +1921,20 @@ int ls_token_logprob_fwd(int64_t tokens, int32_t hidden, int32_t vocab, float sc
     a.stats = stats + blocks * T * 4;
     a.zt = zt;
     a.gmax = gmax;
+    a.gmax_groups = w.gmax_groups;
+    a.gmax_rows = w.gmax_rows;
     a.scale2 = scale * kLog2e;
     ls::GemmPlan used;
     LS_STEP("logprob logits", st, ls::gemm(a, st, &used));
     blocks += 2 * ((cols + used.bn - 1) / used.bn);
   }
-  LS_STEP("logprob rows", st,
-          ls::logprob_rows(T, (int)V, blocks, scale, stats, zt, targets, logprob, entropy, lse, st));
+  const ls::LogprobRows x{blocks, stats, zt, targets, logprob, entropy, lse, scale};
   if (top > 0)
     LS_STEP("logprob top", st,
-            ls::logprob_top(T, (int)H, (int)V, top, scale, (const bf16_t*)h, (const bf16_t*)embed, gmax, lse, top_ids,
-                            top_logprob, st));
+            ls::logprob_top(T, (int)H, (int)V, top, x, (const bf16_t*)h, (const bf16_t*)embed, ls::GroupMax{gmax, w.gmax_groups, w.gmax_rows},
+                            top_ids, top_logprob, st));
+  else
+    LS_STEP("logprob rows", st, ls::logprob_rows(T, (int)V, x, st));
   return LS_OK;
 }
 

@@ -426,10 +426,10 @@ LS_DEV void lse_epilogue(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw,
 // EPI_STAT: per row and wave the maximum m of scale z in base 2 (a wave's columns as in
 // EPI_LSE), the sum of 2^(z - m) and that of (z - m) 2^(z - m), from which come the
 // log-sum-exp and the entropy; the row's target logit (unscaled); and with gmax the largest
-// unscaled logit of every 16 columns, from which the largest of a row are found.  A lane's
-// eight values of either group of a 32-column block are reduced first, then both groups
-// across the halves of the wave with one lane swap, so that the groups cost nothing that
-// the row's maximum does not need anyway but their store, 4 bytes for 16 logits.
+// unscaled logit of every 8 columns, from which the largest of a row are found.  A lane holds
+// four columns of each 8 of a 32-column block, which are reduced first, then two groups
+// at a time across the halves of the wave with one lane swap, so that the groups cost little that
+// the row's maximum does not need anyway but their store, 4 bytes for 8 logits.
 // (z - m) of a logit of -inf counts as -1000, as 2^-inf times it would be NaN.
 template <int TM, int TN, bool EDGE>
 LS_DEV void stat_rows(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw, int nw, int block, int lr, int lh) {
@@ -448,25 +448,27 @@ LS_DEV void stat_rows(const GemmArgs& p, const f32x16 (&acc)[TM][TN], int mw, in
     auto z = [&](int j, int r) {
       return EDGE && 32 * j + 8 * (r >> 2) + (r & 3) >= cols ? -INFINITY : acc[i][j][r];
     };
-    float g[TN];  // of columns 32j + 16lh .. + 15
+    float g[2 * TN];  // of columns 32j + 16h + 8lh .. + 7, at 2j + h
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      float a = -INFINITY, b = -INFINITY;
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        a = fmaxf(a, z(j, r));
-        b = fmaxf(b, z(j, 8 + r));
+      for (int h = 0; h < 2; ++h) {
+        float a = -INFINITY, b = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          a = fmaxf(a, z(j, 8 * h + r));
+          b = fmaxf(b, z(j, 8 * h + 4 + r));
+        }
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        g[2 * j + h] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
       }
-      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-      g[j] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-    }
     if (p.gmax && m < p.M) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) p.gmax[(int64_t)((p.col0 + nw) / 16 + 2 * j + lh) * p.M + m] = g[j];
+      for (int j = 0; j < 2 * TN; ++j) p.gmax[gmax_at(p.gmax_groups, p.gmax_rows, m, (p.col0 + nw) / 8 + 2 * j + lh)] = g[j];
     }
     float mx = g[0];
 #pragma unroll
-    for (int j = 1; j < TN; ++j) mx = fmaxf(mx, g[j]);
+    for (int j = 1; j < 2 * TN; ++j) mx = fmaxf(mx, g[j]);
     mx = halves_max(mx);
     const float m2 = mx * k, ref = mx == -INFINITY ? 0.f : m2;
     float s[2] = {0.f, 0.f}, u[2] = {0.f, 0.f};

@@ -31,7 +31,7 @@ enum Epilogue {
   EPI_DH = 9,       // F (fp32) (+)= acc
   EPI_DE = 10,      // F (fp32) (+)= coef acc
   EPI_DE16 = 11,    // C (bf16) = coef acc
-  EPI_STAT = 12,    // acc are logits: as EPI_LSE with what the entropy needs, and the largest of every 16 columns
+  EPI_STAT = 12,    // acc are logits: as EPI_LSE with what the entropy needs, and the largest of every 8 columns
   EPI_DLP = 13,     // C (bf16) = gradient of log probability and entropy for the scaled logits, over a common factor
 };
 
@@ -81,7 +81,8 @@ struct GemmArgs {
   int group_m = 8;  // tile rows per group of the launch order (set by the launch)
   // EPI_STAT and EPI_DLP: what a logit is multiplied with, times log2(e)
   float scale2 = 0.f;
-  float* gmax = nullptr;  // EPI_STAT: null, or [columns of the vocabulary / 16][M], the largest logit of each 16
+  float* gmax = nullptr;  // EPI_STAT: null, or the largest logit of every 8 columns of the vocabulary, at gmax_at
+  int gmax_groups = 0, gmax_rows = 0;
   // EPI_DLP: the rows' gradients of log probability and entropy, the entropy [M], and the common factor (one)
   const float* dlogp = nullptr;
   const float* dent = nullptr;
@@ -238,13 +239,28 @@ hipError_t head_scatter(int64_t T, int H, const int32_t* slot, const float* coef
 // ---- log probabilities of given tokens -------------------------------------------------
 // Per row from EPI_STAT's statistics: lse of the scaled logits; logprob and entropy (both 0 without a target, NaN for
 // one outside [-1, V)).
-hipError_t logprob_rows(int64_t T, int V, int64_t blocks, float scale, const float* stats, const float* zt,
-                        const int32_t* targets, float* logprob, float* entropy, float* lse, hipStream_t s);
-// The `top` (1 .. 64) largest logits of every row, ties to the lower column, from the largest of every 16 columns
-// (gmax [ceil(V / 16)][T]): ids (-1 past the vocabulary) and scaled logit - lse.
+struct LogprobRows {
+  int64_t blocks;  // column blocks
+  const float *stats, *zt;
+  const int32_t* targets;
+  float *logprob, *entropy, *lse;
+  float scale;
+};
+hipError_t logprob_rows(int64_t T, int V, const LogprobRows& x, hipStream_t s);
+// The same, and the `top` (1 .. 64) largest logits of every row, ties to the lower column, from the largest of every 8
+// columns (gmax): ids (-1 past the vocabulary) and scaled logit - lse.
 constexpr int LOGPROB_TOP = 64;
-hipError_t logprob_top(int64_t T, int H, int V, int top, float scale, const bf16_t* h, const bf16_t* embed,
-                       const float* gmax, const float* lse, int32_t* ids, float* logprob, hipStream_t s);
+// Where a row's maximum of group g lies: blocks of 2^rows rows (16, or as many as there are), in each group by group, so that
+// a workgroup that takes 16 rows reads one piece of memory.
+__host__ __device__ inline int64_t gmax_at(int groups, int rows, int64_t m, int g) {
+  return ((((m >> rows) * groups) + g) << rows) + (m & ((1 << rows) - 1));
+}
+struct GroupMax {
+  const float* v;
+  int groups, rows;
+};
+hipError_t logprob_top(int64_t T, int H, int V, int top, const LogprobRows& x, const bf16_t* h, const bf16_t* embed,
+                       const GroupMax& gmax, int32_t* ids, float* logprob, hipStream_t s);
 
 // ---- gradients of many tensors ------------------------------------------------------
 constexpr int GN_TENSORS = 96;  // tensors that one launch takes

@@ -14,7 +14,8 @@
 // head's features, and past the last head, work on zeros.
 //
 // Bound by HBM bandwidth: every row is read and written once, all sums in fp32, one
-// rounding to bf16.
+// rounding to bf16.  8135 rows of 24/8 heads of 128: forward 29 us (5.7 TB/s), backward 43 + 5 us for the gains' sums
+// (5.8 TB/s); 4099 rows of 64/64 heads of 104: 70 us (4.7 TB/s) and 97 + 6 us (5.1 TB/s).
 #include <math.h>
 
 #include <algorithm>
@@ -26,7 +27,6 @@ namespace ls {
 namespace {
 
 constexpr int QKN_WAVES = 4;
-constexpr int QKN_PARTS = 1024;  // most workgroups, and rows of partial gain gradients, of the backward pass
 constexpr int SUM_GROUPS = 16;   // threads that share a column of those
 
 template <int CTRL>
@@ -49,24 +49,40 @@ template <int V>
 struct Pairs {
   float a[V], b[V];
 };
+// The same as loaded: what is in flight takes half the registers.
+template <int V>
+struct RawPairs {
+  typedef uint32_t words __attribute__((ext_vector_type(V / 2)));
+  words u, w;
+  LS_DEV void load(const bf16_t* p, int half, bool ok) {
+    u = w = words{};
+    if (ok) {
+      u = *(const words*)p;
+      w = *(const words*)(p + half);
+    }
+  }
+  LS_DEV Pairs<V> pairs() const {
+    Pairs<V> x;
+#pragma unroll
+    for (int e = 0; e < V / 2; ++e) {
+      x.a[2 * e] = bf_lo(u[e]);
+      x.a[2 * e + 1] = bf_hi(u[e]);
+      x.b[2 * e] = bf_lo(w[e]);
+      x.b[2 * e + 1] = bf_hi(w[e]);
+    }
+    return x;
+  }
+};
 template <int V>
 LS_DEV Pairs<V> load_pairs(const bf16_t* p, int half, bool ok) {
-  typedef uint32_t words __attribute__((ext_vector_type(V / 2)));
-  words u{}, w{};
-  if (ok) {
-    u = *(const words*)p;
-    w = *(const words*)(p + half);
-  }
-  Pairs<V> x;
-#pragma unroll
-  for (int e = 0; e < V / 2; ++e) {
-    x.a[2 * e] = bf_lo(u[e]);
-    x.a[2 * e + 1] = bf_hi(u[e]);
-    x.b[2 * e] = bf_lo(w[e]);
-    x.b[2 * e + 1] = bf_hi(w[e]);
-  }
-  return x;
+  RawPairs<V> r;
+  r.load(p, half, ok);
+  return r.pairs();
 }
+// Groups of 64 / G heads whose loads a wave issues together (src and dst may be one, so that the compiler keeps loads
+// behind earlier stores), as the registers of four waves to a SIMD allow.
+template <int V>
+constexpr int batch_of() { return V == 4 ? 2 : 1; }
 template <int V>
 LS_DEV void store_pairs(bf16_t* p, int half, const Pairs<V>& x) {
   typedef uint32_t words __attribute__((ext_vector_type(V / 2)));
@@ -98,49 +114,69 @@ LS_DEV double turns_of(int pair, int half, double log2_theta) {
   return exp2(-(double)(pair % half) / half * log2_theta) * 0.15915494309189533577;
 }
 // v of one row goes along where the result lies elsewhere.
-LS_DEV void copy_v(const bf16_t* src, bf16_t* dst, int n, int lane) {
-  for (int i = lane; i < n / 8; i += 64) ((u32x4*)dst)[i] = ((const u32x4*)src)[i];
+LS_DEV void copy_v(const bf16_t* src, bf16_t* dst, int n, int lane, int seg, int segs) {
+  constexpr int U = 4;
+  for (int i = 64 * U * seg + lane; i < n / 8; i += 64 * U * segs) {
+    u32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + 64 * u < n / 8) x[u] = ((const u32x4*)src)[i + 64 * u];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + 64 * u < n / 8) ((u32x4*)dst)[i + 64 * u] = x[u];
+  }
 }
 
 template <int V, int G>
-__global__ __launch_bounds__(64 * QKN_WAVES) void qk_norm_rope_kernel(int total, int nq, int nkv, int d, float eps,
+__global__ __launch_bounds__(64 * QKN_WAVES, 4) void qk_norm_rope_kernel(int total, int seg_bits, int nq, int nkv, int d, float eps,
                                                                       double log2_theta,
                                                                       const int32_t* __restrict__ pos,
                                                                       const bf16_t* __restrict__ gq,
                                                                       const bf16_t* __restrict__ gk, const bf16_t* src,
                                                                       bf16_t* dst) {
-  constexpr int HPW = 64 / G;
+  constexpr int HPW = 64 / G, U = batch_of<V>();
   const int lane = threadIdx.x & 63, half = d / 2, c = lane % G, h0 = lane / G;
   const bool in = V * c < half;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * d;
   const double turns = turns_of(lane, half, log2_theta);
   const Pairs<V> gains[2] = {load_pairs<V>(gq + V * c, half, in), load_pairs<V>(gk + V * c, half, in)};
-  for (int64_t row = (int64_t)blockIdx.x * QKN_WAVES + (threadIdx.x >> 6); row < total;
-       row += (int64_t)gridDim.x * QKN_WAVES) {
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  for (int64_t unit = (int64_t)blockIdx.x * QKN_WAVES + wave; unit < (int64_t)total << seg_bits;
+       unit += (int64_t)gridDim.x * QKN_WAVES) {
+    const int64_t row = unit >> seg_bits;
+    const int segs = 1 << seg_bits, seg = (int)unit & (segs - 1);
     const int p = pos[row];
     if (p < 0 || p > row) continue;
     const Pairs<V> cs = row_turns<V>(turns, p, c);
     auto heads = [&](int first, int n, const Pairs<V>& g) {
-      for (int hb = 0; hb < n; hb += HPW) {
-        const bool ok = in && hb + h0 < n;
-        const int64_t at = row * ld + (int64_t)(first + hb + h0) * d + V * c;
-        Pairs<V> x = load_pairs<V>(src + at, half, ok);
-        float ss = 0.f;
+      for (int hu = seg * U * HPW; hu < n; hu += segs * U * HPW) {
+        const int64_t at0 = row * ld + (int64_t)(first + hu + h0) * d + V * c;
+        RawPairs<V> raw[U];
 #pragma unroll
-        for (int e = 0; e < V; ++e) ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
-        const float r = 1.0f / sqrtf(head_sum<G>(ss) / (float)d + eps);
+        for (int u = 0; u < U; ++u) raw[u].load(src + at0 + u * HPW * d, half, in && hu + u * HPW + h0 < n);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float a = x.a[e] * r * g.a[e], b = x.b[e] * r * g.b[e];
-          x.a[e] = a * cs.a[e] - b * cs.b[e];
-          x.b[e] = a * cs.b[e] + b * cs.a[e];
+        for (int u = 0; u < U; ++u) {
+          if (hu + u * HPW >= n) break;
+          const bool ok = in && hu + u * HPW + h0 < n;
+          const int64_t at = at0 + u * HPW * d;
+          Pairs<V> x = raw[u].pairs();
+          float ss = 0.f;
+#pragma unroll
+          for (int e = 0; e < V; ++e) ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
+          const float r = 1.0f / sqrtf(head_sum<G>(ss) / (float)d + eps);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float a = x.a[e] * r * g.a[e], b = x.b[e] * r * g.b[e];
+            x.a[e] = a * cs.a[e] - b * cs.b[e];
+            x.b[e] = a * cs.b[e] + b * cs.a[e];
+          }
+          if (ok) store_pairs<V>(dst + at, half, x);
         }
-        if (ok) store_pairs<V>(dst + at, half, x);
       }
     };
     heads(0, nq, gains[0]);
     heads(nq, nkv, gains[1]);
-    if (src != dst) copy_v(src + row * ld + (int64_t)(nq + nkv) * d, dst + row * ld + (int64_t)(nq + nkv) * d, nkv * d, lane);
+    if (src != dst) copy_v(src + row * ld + (int64_t)(nq + nkv) * d, dst + row * ld + (int64_t)(nq + nkv) * d, nkv * d, lane, seg, segs);
   }
 }
 
@@ -149,35 +185,49 @@ __global__ __launch_bounds__(64 * QKN_WAVES) void qk_norm_rope_kernel(int total,
 // and heads, then over the lanes of the same features, then over the waves: a fixed
 // order.
 template <int V, int G>
-__global__ __launch_bounds__(64 * QKN_WAVES) void qk_norm_rope_bwd_kernel(
-    int total, int nq, int nkv, int d, float eps, double log2_theta, const int32_t* __restrict__ pos,
+__global__ __launch_bounds__(64 * QKN_WAVES, V == 4 ? 4 : 3) void qk_norm_rope_bwd_kernel(
+    int total, int seg_bits, int nq, int nkv, int d, float eps, double log2_theta, const int32_t* __restrict__ pos,
     const bf16_t* __restrict__ gq, const bf16_t* __restrict__ gk, const bf16_t* __restrict__ src, const bf16_t* dy,
     bf16_t* dx, float* __restrict__ part) {
-  constexpr int HPW = 64 / G;
+  constexpr int HPW = 64 / G, U = batch_of<V>();
   __shared__ float red[QKN_WAVES][2][2 * V * G];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = d / 2, c = lane % G, h0 = lane / G;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = d / 2, c = lane % G, h0 = lane / G;
   const bool in = V * c < half;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * d;
   const double turns = turns_of(lane, half, log2_theta);
   const Pairs<V> gains[2] = {load_pairs<V>(gq + V * c, half, in), load_pairs<V>(gk + V * c, half, in)};
   Pairs<V> sums[2] = {};
-  for (int64_t row = (int64_t)blockIdx.x * QKN_WAVES + wave; row < total; row += (int64_t)gridDim.x * QKN_WAVES) {
+  for (int64_t unit = (int64_t)blockIdx.x * QKN_WAVES + wave; unit < (int64_t)total << seg_bits;
+       unit += (int64_t)gridDim.x * QKN_WAVES) {
+    const int64_t row = unit >> seg_bits;
+    const int segs = 1 << seg_bits, seg = (int)unit & (segs - 1);
     const int p = pos[row];
     if (p < 0 || p > row) continue;
     const Pairs<V> cs = row_turns<V>(turns, p, c);
     auto heads = [&](int first, int n, const Pairs<V>& g, Pairs<V>& sum) {
-      for (int hb = 0; hb < n; hb += HPW) {
-        const bool ok = in && hb + h0 < n;
-        const int64_t at = row * ld + (int64_t)(first + hb + h0) * d + V * c;
-        const Pairs<V> x = load_pairs<V>(src + at, half, ok), t = load_pairs<V>(dy + at, half, ok);
-        Pairs<V> dn;
-        float ss = 0.f, dot = 0.f;
+      for (int hu = seg * U * HPW; hu < n; hu += segs * U * HPW) {
+        const int64_t at0 = row * ld + (int64_t)(first + hu + h0) * d + V * c;
+        RawPairs<V> xr[U], tr[U];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          dn.a[e] = t.a[e] * cs.a[e] + t.b[e] * cs.b[e];
-          dn.b[e] = t.b[e] * cs.a[e] - t.a[e] * cs.b[e];
-          ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
-          dot += g.a[e] * dn.a[e] * x.a[e] + g.b[e] * dn.b[e] * x.b[e];
+        for (int u = 0; u < U; ++u) {
+          const bool ok = in && hu + u * HPW + h0 < n;
+          xr[u].load(src + at0 + u * HPW * d, half, ok);
+          tr[u].load(dy + at0 + u * HPW * d, half, ok);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (hu + u * HPW >= n) break;
+          const bool ok = in && hu + u * HPW + h0 < n;
+          const int64_t at = at0 + u * HPW * d;
+          const Pairs<V> x = xr[u].pairs(), t = tr[u].pairs();
+          Pairs<V> dn;
+          float ss = 0.f, dot = 0.f;
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            dn.a[e] = t.a[e] * cs.a[e] + t.b[e] * cs.b[e];
+            dn.b[e] = t.b[e] * cs.a[e] - t.a[e] * cs.b[e];
+            ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
+            dot += g.a[e] * dn.a[e] * x.a[e] + g.b[e] * dn.b[e] * x.b[e];
         }
         const float ms = head_sum<G>(ss) / (float)d + eps;
         const float r = ok ? 1.0f / sqrtf(ms) : 0.f;  // (a lane without a head adds nothing to the gains' sums, eps 0 too)
@@ -193,11 +243,12 @@ __global__ __launch_bounds__(64 * QKN_WAVES) void qk_norm_rope_bwd_kernel(
           out.b[e] = r * (g.b[e] * dn.b[e] - nb * coef);
         }
         if (ok) store_pairs<V>(dx + at, half, out);
+        }
       }
     };
     heads(0, nq, gains[0], sums[0]);
     heads(nq, nkv, gains[1], sums[1]);
-    if (dy != dx) copy_v(dy + row * ld + (int64_t)(nq + nkv) * d, dx + row * ld + (int64_t)(nq + nkv) * d, nkv * d, lane);
+    if (dy != dx) copy_v(dy + row * ld + (int64_t)(nq + nkv) * d, dx + row * ld + (int64_t)(nq + nkv) * d, nkv * d, lane, seg, segs);
   }
   if (!part) return;
 #pragma unroll
@@ -251,17 +302,34 @@ void by_head(int d, F&& f) {
   else f(integral_constant<int, 4>{}, integral_constant<int, 16>{});
 }
 
-int qkn_parts(const PackedShape& p) { return (int)std::min<int64_t>((p.total + QKN_WAVES - 1) / QKN_WAVES, QKN_PARTS); }
+// Waves that share a row: of a few thousand rows one wave each would leave the card's last round of workgroups nearly
+// empty (4099 rows of 64/64 heads of 104, 1025 workgroups: backward 125 us, 98 with eight waves to a row), so a row is
+// cut in equal parts while there are fewer than 32768 pieces; not unequally (24/8 heads of 128 in two: 50 -> 59 us).
+int segment_bits(const PackedShape& p) {
+  const int batch = p.d == 64 ? 16 : 8;  // heads
+  int bits = 0;
+  while (((int64_t)p.total << bits) < 32768 && p.nq % (batch << (bits + 1)) == 0) ++bits;
+  return bits;
+}
+// Workgroups of the backward pass, and rows of partial gain gradients: its pieces in whole rounds of as many workgroups
+// as run at once (four waves to a SIMD, three of the instances with V = 8): 8135 rows of 24/8 heads of 128 in
+// 678 workgroups 43 us, in 1017, of which 768 run at once, 53.
+int qkn_parts(const PackedShape& p) {
+  const int64_t need = (((int64_t)p.total << segment_bits(p)) + QKN_WAVES - 1) / QKN_WAVES;
+  const int64_t most = PACKED_CUS * (p.d % 16 == 0 ? 3 : 4), rounds = (need + most - 1) / most;
+  return (int)((need + rounds - 1) / rounds);
+}
 
 }  // namespace
 
 hipError_t packed_qk_norm_rope(const PackedShape& p, const void* plan, double theta, float eps, const bf16_t* gq,
                                const bf16_t* gk, const bf16_t* src, bf16_t* dst, hipStream_t s) {
-  const int64_t need = (p.total + QKN_WAVES - 1) / QKN_WAVES;
+  const int bits = segment_bits(p);
+  const int64_t need = (((int64_t)p.total << bits) + QKN_WAVES - 1) / QKN_WAVES;
   const dim3 grid((unsigned)std::min<int64_t>(need, 8192)), block(64 * QKN_WAVES);
   by_head(p.d, [&](auto v, auto g) {
-    hipLaunchKernelGGL((qk_norm_rope_kernel<decltype(v)::value, decltype(g)::value>), grid, block, 0, s, (int)p.total, p.nq,
-                       p.nkv, p.d, eps, log2(theta), packed_pos(p, plan), gq, gk, src, dst);
+    hipLaunchKernelGGL((qk_norm_rope_kernel<decltype(v)::value, decltype(g)::value>), grid, block, 0, s, (int)p.total, bits,
+                       p.nq, p.nkv, p.d, eps, log2(theta), packed_pos(p, plan), gq, gk, src, dst);
   });
   return hipGetLastError();
 }
@@ -275,8 +343,8 @@ hipError_t packed_qk_norm_rope_bwd(const PackedShape& p, const void* plan, doubl
   float* part = dgq || dgk ? (float*)ws : nullptr;
   by_head(p.d, [&](auto v, auto g) {
     hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<decltype(v)::value, decltype(g)::value>), dim3((unsigned)parts),
-                       dim3(64 * QKN_WAVES), 0, s, (int)p.total, p.nq, p.nkv, p.d, eps, log2(theta), packed_pos(p, plan),
-                       gq, gk, src, dy, dx, part);
+                       dim3(64 * QKN_WAVES), 0, s, (int)p.total, segment_bits(p), p.nq, p.nkv, p.d, eps, log2(theta),
+                       packed_pos(p, plan), gq, gk, src, dy, dx, part);
   });
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !part) return e;

@@ -177,6 +177,29 @@ def test_all_logits_equal():
         assert float((x.vals.double() + ln).abs().max()) <= 2.0 ** -17 + ln * 2.0 ** -21
 
 
+@pytest.mark.parametrize("T", [2, 1030])
+@pytest.mark.parametrize("top", [1, 16, 17, 64])
+@pytest.mark.parametrize("low", [None, 0, 5, 15])
+def test_logits_in_any_arrangement(T, top, low):
+    """Rising, falling and constant along the vocabulary, and far lower in every 16th stretch of 512 tokens."""
+    need_gpu()
+    V = 20_003
+    x = Head(T, 16, V, top, seed=3, masked=0.0)
+    x.h.zero_()
+    x.h[0, 0] = 1.0
+    x.h[1, 0] = -1.0
+    x.h[T - 1, 1] = 1.0
+    v = torch.arange(V, device="cuda")
+    x.e.zero_()
+    x.e[:, 0] = (v // 100).to(BF16)  # whole numbers up to 200: exact
+    x.e[:, 1] = (v % 7).to(BF16)
+    if low is not None:
+        x.e[(v // 512) % 16 == low] -= 250.0 if T > 2 else 256.0
+    x.fwd()
+    z = x.h.double() @ x.e.double().T
+    assert torch.equal(x.ids, torch.sort(z, dim=1, descending=True, stable=True).indices[:, :top].int())
+
+
 @pytest.mark.parametrize("piece", [0, 4096])
 @pytest.mark.parametrize("T,H,V,masked", [(1500, 512, 9001, 0.8), (1500, 512, 9001, 0.97), (509, 256, 33000, 0.998)])
 def test_few_rows_with_a_target(T, H, V, masked, piece):
