@@ -10,7 +10,8 @@
 // on the tensors' sizes only.
 //
 // Bound by HBM bandwidth: the norm reads every gradient once, clipping reads and
-// writes each once.
+// writes each once.  5.3e8 fp32 elements: norm 370 us (5.7 TB/s), clipped into bf16 583 us (5.5 TB/s; from the last tensor
+// on, which the norm read last, no less: the last-level cache keeps little of a stream).
 #include <math.h>
 
 #include <algorithm>
