@@ -442,7 +442,8 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? (SC::ON ? 3 : 4) : 2) void
   const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv), hd = PACKED ? sh.d : D;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * hd;
   const bf16_t* base = qkv + qtile.row0 * ld;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 31, lh = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lh = lane >> 5;
   const int q0 = qtile.qt * BQ;
   const int qrow = q0 + 32 * wave + lr;
   const int wave_qmin = q0 + 32 * wave, wave_qmax = wave_qmin + 31;
@@ -517,6 +518,7 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? (SC::ON ? 3 : 4) : 2) void
           for (int r = 0; r < 16; ++r) sacc[bb][r] = sc.half(sacc[bb][r]);
       }
       if (edge) {
+        asm volatile("");  // keeps the block a branch rather than selects on every tile
 #pragma unroll
         for (int bb = 0; bb < BKV / 32; ++bb)
 #pragma unroll
@@ -1477,21 +1479,28 @@ LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_
   u32x4 ring[RING];
   f32x16 sacc[2], pacc[2];
   u32x4 sf[2][2];
-  // causal mask: element r of key block bb is key kv0 + 4lh + c with
-  // c = 32bb + 8(r/4) + r%4, kept when c <= hi, i.e. key <= qrow.  Keys past the
+  // causal mask, on tiles that have a key which some query of the wave does not see only: element r of key block bb
+  // is key kv0 + 4lh + c with c = 32bb + 8(r/4) + r%4, kept when c <= hi, i.e. key <= qrow.  Keys past the
   // end of the sequence need no mask beyond that: their K and V read as zero.
-  auto soft = [&](auto bb_c, auto r_c, int hi) {
+  auto soft = [&](auto bb_c, auto r_c, int hi, bool edge) {
     constexpr int bb = decltype(bb_c)::value, r = decltype(r_c)::value;
-    constexpr int c = 32 * bb + 8 * (r >> 2) + (r & 3);
     float w;
     float p = prob_slope(sc, sacc[bb][r], sl2, L2, w);
     if constexpr (SC::CAPPED) p *= w;
-    if (c > hi) p = 0.f;
-    if constexpr (SC::ON) {
-      if (c <= hi - sc.window) p = 0.f;
-    }
     pacc[bb][r] = p * (pacc[bb][r] - Dq);
-    if constexpr ((r & 7) == 7) sf[bb][r >> 3] = pack_frag(pacc[bb], r - 7);
+    if constexpr ((r & 7) == 7) {
+      if (edge) {
+        asm volatile("");  // keeps the block a branch rather than selects on every tile
+#pragma unroll
+        for (int u = r - 7; u <= r; ++u) {
+          const int c = 32 * bb + 8 * (u >> 2) + (u & 3);
+          bool hide = c > hi;
+          if constexpr (SC::ON) hide = hide || c <= hi - sc.window;
+          if (hide) pacc[bb][u] = 0.f;
+        }
+      }
+      sf[bb][r >> 3] = pack_frag(pacc[bb], r - 7);
+    }
   };
 
   sync_lds();
@@ -1503,7 +1512,9 @@ LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_
       tl(base, ld, kv0 + BKV, S, kcol, Ks[cur ^ 1], wave);
       tl(base, ld, kv0 + BKV, S, vcol, Vs[cur ^ 1], wave);
     }
-    const int hi = qrow - kv0 - 4 * lh;
+    const int hi = qrow - kv0 - 4 * lh, wave_qmin = q0 + 32 * wave;
+    bool edge = kv0 + BKV - 1 > wave_qmin;
+    if constexpr (SC::ON) edge = edge || kv0 <= wave_qmin + 31 - sc.window;
     static_for<RA>([&](auto j_c) { ring[decltype(j_c)::value] = operand(j_c, cur_c); });
     static_for<NSLOT>([&](auto j_c) {
       constexpr int j = decltype(j_c)::value;
@@ -1516,7 +1527,7 @@ LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_
         if constexpr (bb == 1) {  // softmax of block 0
           constexpr int PER = 16 / PS;
           static_for<PER>([&](auto u) {
-            soft(std::integral_constant<int, 0>{}, std::integral_constant<int, k * PER + decltype(u)::value>{}, hi);
+            soft(std::integral_constant<int, 0>{}, std::integral_constant<int, k * PER + decltype(u)::value>{}, hi, edge);
           });
         }
       } else {
@@ -1525,7 +1536,7 @@ LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_
         if constexpr (bb == 0) {  // softmax of block 1
           constexpr int PER = 16 / PQ;
           static_for<PER>([&](auto u) {
-            soft(std::integral_constant<int, 1>{}, std::integral_constant<int, c * PER + decltype(u)::value>{}, hi);
+            soft(std::integral_constant<int, 1>{}, std::integral_constant<int, c * PER + decltype(u)::value>{}, hi, edge);
           });
         }
       }
