@@ -23,7 +23,7 @@ hipError_t attn_bwd_t(const AttnShape& sh, const bf16_t* qkv, const bf16_t* o, c
   float* Dv = (float*)ws;
   float* lse2 = Dv + T * sh.nq;
   hipLaunchKernelGGL((attn_bwd_pre_kernel<D, false>), dim3((unsigned)((T + 3) / 4)), dim3(256), 0, s, sh, o, dout, lse, Dv,
-                     lse2, (const bf16_t*)nullptr);
+                     lse2, (const bf16_t*)nullptr, false, 0.f);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const float scale = 1.0f / sqrtf((float)(sh.d_scale > 0 ? sh.d_scale : D));

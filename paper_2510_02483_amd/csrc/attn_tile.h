@@ -596,7 +596,7 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? (SC::ON ? 3 : 4) : 2) void
 template <int D, bool REST>
 LS_DEV void bwd_pre_row(const AttnShape& sh, const bf16_t* __restrict__ orow, const bf16_t* __restrict__ drow,
                         const float* __restrict__ lse, float* __restrict__ Dv, float* __restrict__ lse2, int64_t t,
-                        const bf16_t* __restrict__ rrow) {
+                        const bf16_t* __restrict__ rrow, bool neg, float less) {
   constexpr int CPH = D / 8;
   const int lane = threadIdx.x & 63, c = lane % CPH;
   for (int h = lane / CPH; h - lane / CPH < sh.nq; h += 64 / CPH) {
@@ -615,26 +615,28 @@ LS_DEV void bwd_pre_row(const AttnShape& sh, const bf16_t* __restrict__ orow, co
     for (int off = CPH / 2; off >= 1; off >>= 1) acc += __shfl_xor(acc, off);
     if (c == 0 && h < sh.nq) {
       const int64_t i = (int64_t)h * sh.seq + t;
-      Dv[i] = acc;
-      lse2[i] = lse[i] * LOG2E;
+      Dv[i] = neg ? -acc : acc;
+      lse2[i] = lse[i] * LOG2E - less;
     }
   }
 }
 
 // D[b,h,s] = <dO, O> over the head's d columns (fp32), and the log-sum-exp in
 // base 2 (lse * log2(e)), the form the backward kernels subtract.
-// REST: O is o and the rest that its rounding left.
+// REST: O is o and the rest that its rounding left.  neg: -D, what dP starts from where scores are modified; less: c2 of a
+// cap, which every exponent less the log-sum-exp holds.
 template <int D, bool PACKED, bool REST = false>
 __global__ __launch_bounds__(256) void attn_bwd_pre_kernel(AttnShape sh, const bf16_t* __restrict__ o,
                                                            const bf16_t* __restrict__ dout,
                                                            const float* __restrict__ lse, float* __restrict__ Dv,
-                                                           float* __restrict__ lse2, const bf16_t* __restrict__ rest) {
+                                                           float* __restrict__ lse2, const bf16_t* __restrict__ rest,
+                                                           bool neg, float less) {
   constexpr int CPH = D / 8;  // 16-byte chunks per head
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)(PACKED ? packed_wg() : (int)blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (t >= (int64_t)sh.batch * sh.seq) return;
   if constexpr (PACKED) {
-    bwd_pre_row<D, REST>(sh, o + t * sh.nq * sh.d, dout + t * sh.nq * sh.d, lse, Dv, lse2, t, rest + t * sh.nq * sh.d);
+    bwd_pre_row<D, REST>(sh, o + t * sh.nq * sh.d, dout + t * sh.nq * sh.d, lse, Dv, lse2, t, rest + t * sh.nq * sh.d, neg, less);
     return;
   }
   const int b = (int)(t / sh.seq), s = (int)(t % sh.seq);
@@ -731,14 +733,14 @@ LS_DEV void store_sums(float* row, const f32x16 (&dk)[D / 32], const f32x16 (&dv
     }
 }
 
-// The probability of a raw score, exp2 of the base-2 score less the log-sum-exp L, and
+// The probability of a raw score, exp2 of the base-2 score less the log-sum-exp L (capped: c2 - 2 c2 r - (L + c2)), and
 // (capped) w = r (1 - r), a quarter of the cap's slope.
 template <class SC>
 LS_DEV float prob_slope(const SC& sc, float s, float sl2, float L, float& w) {
   if constexpr (SC::CAPPED) {
     const float r = sc.half(s);
     w = fmaf(-r, r, r);
-    return ex2(sc.less(r, L));
+    return ex2(fmaf(r, -2.0f * sc.c2, -L));
   } else {
     return ex2(fmaf(s, sl2, -L));
   }
@@ -1115,16 +1117,23 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
     }
   }
   const TileLoader<D, BWD_BQ> tlq(ld, wave, lane, hd), tlo(ldo, wave, lane, hd);
-  auto issue = [&](int t, int st) {
-    const int h = kvh * G + hs * Gs + t / nqt, q0 = q_begin + (t % nqt) * BWD_BQ;
+  // the head and the query tile of the next tile to load, and of the current one (counted, as divisions by nqt cost a tenth of
+  // the loop's scalar instructions)
+  int next_h = kvh * G + hs * Gs + tbegin / nqt, next_q = tbegin % nqt, tile_q = next_q;
+  auto issue = [&](int st) {
+    const int h = next_h, q0 = q_begin + next_q * BWD_BQ;
+    if (++next_q == nqt) {
+      next_q = 0;
+      ++next_h;
+    }
     tlq(base, ld, q0, S, h * hd, stg[st].q, wave);
     tlo(dbase, ldo, q0, S, h * hd, stg[st].o, wave);
     const int64_t v0 = vec0 + (int64_t)h * sh.seq;
     if (wave == 0) load_vec64(rsrc(lse2 + v0, (uint32_t)S * 4), q0, S, stg[st].l, lane);
     if (wave == 1) load_vec64(rsrc(Dv + v0, (uint32_t)S * 4), q0, S, stg[st].d, lane);
   };
-  if (!SC::ON || tbegin < ntiles) issue(tbegin, 0);
-  if (tbegin + 1 < ntiles) issue(tbegin + 1, 1);
+  if (!SC::ON || tbegin < ntiles) issue(0);
+  if (tbegin + 1 < ntiles) issue(1);
 
   u32x4 kf[NSD], vf[NSD];
 #pragma unroll
@@ -1164,7 +1173,8 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
   // One tile in stage st; st1 and st2 are the stages of the next two tiles
   // (the three rotate from tile to tile).
   auto tile = [&](int t, int st, int st1, int st2) {
-    const int q0 = q_begin + (t % nqt) * BWD_BQ;
+    const int q0 = q_begin + tile_q * BWD_BQ;
+    if (++tile_q == nqt) tile_q = 0;
     // causal mask, on the tiles at the diagonal only (some query of the tile
     // precedes some key of the wave): element r of block qb is query
     // q0 + 4lh + c with c = 32qb + 8(r/4) + r%4, kept when c >= lo, i.e.
@@ -1183,15 +1193,21 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (t + 2 < ntiles) issue(t + 2, st2);
+        if (t + 2 < ntiles) issue(st2);
       }
       const u32x4 a = ring[j % RING];
       if constexpr (k < P1) {  // S = Q K^T; read the block's log-sum-exp
         sacc = mfma32(a, kf[k], k == 0 ? f32x16{} : sacc);
+        // (modified scores: -D of the block's queries, from which dP's sums start)
+        if constexpr (SC::ON && k < 4) {
+          const f32x4 d = *(const f32x4*)&stg[st].d[32 * qb + 8 * k + 4 * lh];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pacc[4 * k + e] = d[e];
+        }
         if constexpr (k == P1 - 1) Lq[0] = *(const f32x4*)&stg[st].l[32 * qb + 4 * lh];
       } else if constexpr (k < P1 + P2) {  // dP = dO V^T, meanwhile P = exp2(S sl2 - LSE2)
         constexpr int c = k - P1, PER = 16 / P2;
-        pacc = mfma32(a, vf[c], c == 0 ? f32x16{} : pacc);
+        pacc = mfma32(a, vf[c], c == 0 && !SC::ON ? f32x16{} : pacc);
         if constexpr (c == 0 && !SC::CAPPED) {
           if (diag) {
             asm volatile("");  // keeps the block a branch rather than selects on every tile
@@ -1208,7 +1224,7 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
           constexpr int r = c * PER + decltype(u_c)::value, rq = r >> 2, e = r & 3;
           // the next group's log-sum-exp, one group ahead
           if constexpr (e == 0 && rq < 3) Lq[(rq + 1) & 1] = *(const f32x4*)&stg[st].l[32 * qb + 8 * (rq + 1) + 4 * lh];
-          if constexpr (r == 12) Dq[0] = *(const f32x4*)&stg[st].d[32 * qb + 4 * lh];
+          if constexpr (!SC::ON && r == 12) Dq[0] = *(const f32x4*)&stg[st].d[32 * qb + 4 * lh];
           if constexpr (SC::CAPPED) {
             float w;
             sacc[r] = prob_slope(sc, sacc[r], sl2, Lq[rq & 1][e], w);
@@ -1233,8 +1249,10 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
         dv[c % NI] = mfma32(a, pf[c / NI], dv[c % NI]);
         static_for<PER>([&](auto u_c) {
           constexpr int r = c * PER + decltype(u_c)::value, rq = r >> 2, e = r & 3;
-          if constexpr (e == 0 && rq < 3) Dq[(rq + 1) & 1] = *(const f32x4*)&stg[st].d[32 * qb + 8 * (rq + 1) + 4 * lh];
-          pacc[r] = (SC::CAPPED ? wacc[r] : sacc[r]) * (pacc[r] - Dq[rq & 1][e]);
+          if constexpr (!SC::ON && e == 0 && rq < 3)
+            Dq[(rq + 1) & 1] = *(const f32x4*)&stg[st].d[32 * qb + 8 * (rq + 1) + 4 * lh];
+          if constexpr (SC::ON) pacc[r] *= SC::CAPPED ? wacc[r] : sacc[r];
+          else pacc[r] = sacc[r] * (pacc[r] - Dq[rq & 1][e]);
           if constexpr ((r & 7) == 7) sf[r >> 3] = pack_frag(pacc, r - 7);
         });
       } else {  // dK^T += Q^T dS
@@ -1450,7 +1468,7 @@ LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_
     df[s] = ok ? load16(dout + (qtile.row0 + qrow) * ldo + h * hd + 16 * s + 8 * lh) : u32x4{0u, 0u, 0u, 0u};
   }
   const float L2 = qok ? lse2[qtile.vec0 + qrow] : 0.f;
-  const float Dq = qok ? Dv[qtile.vec0 + qrow] : 0.f;
+  const float Dq = qok ? Dv[qtile.vec0 + qrow] : 0.f;  // (modified scores: -D)
 
   f32x16 dq[NI];
 #pragma unroll
@@ -1487,7 +1505,7 @@ LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_
     float w;
     float p = prob_slope(sc, sacc[bb][r], sl2, L2, w);
     if constexpr (SC::CAPPED) p *= w;
-    pacc[bb][r] = p * (pacc[bb][r] - Dq);
+    pacc[bb][r] = SC::ON ? p * (pacc[bb][r] + Dq) : p * (pacc[bb][r] - Dq);
     if constexpr ((r & 7) == 7) {
       if (edge) {
         asm volatile("");  // keeps the block a branch rather than selects on every tile
@@ -1655,10 +1673,10 @@ hipError_t packed_attn_bwd_t(const AttnShape& sh, const PackedView& pk, const bf
   if constexpr (SC::ON) rest = sc.rest;
   if (SC::ON && rest)
     hipLaunchKernelGGL((attn_bwd_pre_kernel<D, true, SC::ON>), packed_grid((T + 3) / 4), dim3(256), 0, s, sh, o, dout, lse,
-                       Dv, lse2, rest);
+                       Dv, lse2, rest, SC::ON, sc.c2);
   else
     hipLaunchKernelGGL((attn_bwd_pre_kernel<D, true>), packed_grid((T + 3) / 4), dim3(256), 0, s, sh, o, dout, lse, Dv,
-                       lse2, rest);
+                       lse2, rest, SC::ON, sc.c2);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const float qk = SC::ON ? own_scale : 1.0f / sqrtf((float)sh.d), sl2 = qk * LOG2E;
