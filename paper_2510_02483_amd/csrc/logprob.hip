@@ -383,7 +383,10 @@ hipError_t logprob_rows(int64_t T, int V, const LogprobRows& x, hipStream_t s) {
 
 hipError_t logprob_top(int64_t T, int H, int V, int top, const LogprobRows& x, const bf16_t* h, const bf16_t* embed,
                        const GroupMax& gmax, int32_t* ids, float* logprob, hipStream_t s) {
-  if (T <= 1024) {
+  // us for all rows, one to a workgroup / one to a wave (hidden 2048): vocabulary 32000, five alternatives, 512 rows 41 / 72,
+  // 1024 rows 77 / 73; vocabulary 128256 96 / 109 and 186 / 120; 64 alternatives, 1024 rows 386 / 573 and 501 / 868,
+  // 2048 rows 720 / 764 and 963 / 941
+  if (T <= (top > 16 ? 1024 : 512)) {
     hipLaunchKernelGGL(logprob_top_one_kernel, dim3((unsigned)T), dim3(LP_THREADS), 0, s, T, H, V, top, x, h, embed, gmax,
                        ids, logprob);
     return hipGetLastError();
