@@ -442,7 +442,7 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? (SC::ON ? 3 : 4) : 2) void
   const int S = qtile.S, h = qtile.h, kvh = h / (nq / nkv), hd = PACKED ? sh.d : D;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * hd;
   const bf16_t* base = qkv + qtile.row0 * ld;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, wave = SC::ON ? __builtin_amdgcn_readfirstlane(tid >> 6) : tid >> 6;
   const int lr = lane & 31, lh = lane >> 5;
   const int q0 = qtile.qt * BQ;
   const int qrow = q0 + 32 * wave + lr;
@@ -518,7 +518,7 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? (SC::ON ? 3 : 4) : 2) void
           for (int r = 0; r < 16; ++r) sacc[bb][r] = sc.half(sacc[bb][r]);
       }
       if (edge) {
-        asm volatile("");  // keeps the block a branch rather than selects on every tile
+        if constexpr (SC::ON) asm volatile("");  // keeps the block a branch rather than selects on every tile
 #pragma unroll
         for (int bb = 0; bb < BKV / 32; ++bb)
 #pragma unroll
@@ -1117,14 +1117,21 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
     }
   }
   const TileLoader<D, BWD_BQ> tlq(ld, wave, lane, hd), tlo(ldo, wave, lane, hd);
-  // the head and the query tile of the next tile to load, and of the current one (counted, as divisions by nqt cost a tenth of
-  // the loop's scalar instructions)
-  int next_h = kvh * G + hs * Gs + tbegin / nqt, next_q = tbegin % nqt, tile_q = next_q;
-  auto issue = [&](int st) {
-    const int h = next_h, q0 = q_begin + next_q * BWD_BQ;
-    if (++next_q == nqt) {
-      next_q = 0;
-      ++next_h;
+  // modified scores: the head and the query tile of the next tile to load, and of the current one, are counted, as divisions
+  // by nqt cost a tenth of the loop's scalar instructions (6007 rows of 12/4 heads of 64 through a window of 300, training
+  // pass 86.5 -> 84.2 us; plain scores, whose loop hides them, 450 -> 461 with both changes of this kind)
+  int next_h = 0, next_q = 0, tile_q = 0;
+  if constexpr (SC::ON) {
+    next_h = kvh * G + hs * Gs + tbegin / nqt;
+    next_q = tile_q = tbegin % nqt;
+  }
+  auto issue = [&](int t, int st) {
+    const int h = SC::ON ? next_h : kvh * G + hs * Gs + t / nqt, q0 = q_begin + (SC::ON ? next_q : t % nqt) * BWD_BQ;
+    if constexpr (SC::ON) {
+      if (++next_q == nqt) {
+        next_q = 0;
+        ++next_h;
+      }
     }
     tlq(base, ld, q0, S, h * hd, stg[st].q, wave);
     tlo(dbase, ldo, q0, S, h * hd, stg[st].o, wave);
@@ -1132,8 +1139,8 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
     if (wave == 0) load_vec64(rsrc(lse2 + v0, (uint32_t)S * 4), q0, S, stg[st].l, lane);
     if (wave == 1) load_vec64(rsrc(Dv + v0, (uint32_t)S * 4), q0, S, stg[st].d, lane);
   };
-  if (!SC::ON || tbegin < ntiles) issue(0);
-  if (tbegin + 1 < ntiles) issue(1);
+  if (!SC::ON || tbegin < ntiles) issue(tbegin, 0);
+  if (tbegin + 1 < ntiles) issue(tbegin + 1, 1);
 
   u32x4 kf[NSD], vf[NSD];
 #pragma unroll
@@ -1173,8 +1180,10 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
   // One tile in stage st; st1 and st2 are the stages of the next two tiles
   // (the three rotate from tile to tile).
   auto tile = [&](int t, int st, int st1, int st2) {
-    const int q0 = q_begin + tile_q * BWD_BQ;
-    if (++tile_q == nqt) tile_q = 0;
+    const int q0 = q_begin + (SC::ON ? tile_q : t % nqt) * BWD_BQ;
+    if constexpr (SC::ON) {
+      if (++tile_q == nqt) tile_q = 0;
+    }
     // causal mask, on the tiles at the diagonal only (some query of the tile
     // precedes some key of the wave): element r of block qb is query
     // q0 + 4lh + c with c = 32qb + 8(r/4) + r%4, kept when c >= lo, i.e.
@@ -1193,7 +1202,7 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (t + 2 < ntiles) issue(st2);
+        if (t + 2 < ntiles) issue(t + 2, st2);
       }
       const u32x4 a = ring[j % RING];
       if constexpr (k < P1) {  // S = Q K^T; read the block's log-sum-exp
@@ -1497,24 +1506,31 @@ LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_
   u32x4 ring[RING];
   f32x16 sacc[2], pacc[2];
   u32x4 sf[2][2];
-  // causal mask, on tiles that have a key which some query of the wave does not see only: element r of key block bb
-  // is key kv0 + 4lh + c with c = 32bb + 8(r/4) + r%4, kept when c <= hi, i.e. key <= qrow.  Keys past the
+  // causal mask: element r of key block bb is key kv0 + 4lh + c with
+  // c = 32bb + 8(r/4) + r%4, kept when c <= hi, i.e. key <= qrow.  Keys past the
   // end of the sequence need no mask beyond that: their K and V read as zero.
+  // Modified scores, with a window's two borders, are masked on the tiles only that have a key which
+  // some query of the wave does not see (`edge`): 8135 rows of 24/8 heads of 128, cap 30, dQ 264 -> 251 us; plain ones, one
+  // comparison and select each, are no faster so.
   auto soft = [&](auto bb_c, auto r_c, int hi, bool edge) {
     constexpr int bb = decltype(bb_c)::value, r = decltype(r_c)::value;
+    constexpr int c0 = 32 * bb + 8 * (r >> 2) + (r & 3);
     float w;
     float p = prob_slope(sc, sacc[bb][r], sl2, L2, w);
     if constexpr (SC::CAPPED) p *= w;
+    if constexpr (!SC::ON) {
+      if (c0 > hi) p = 0.f;
+    }
     pacc[bb][r] = SC::ON ? p * (pacc[bb][r] + Dq) : p * (pacc[bb][r] - Dq);
     if constexpr ((r & 7) == 7) {
-      if (edge) {
-        asm volatile("");  // keeps the block a branch rather than selects on every tile
+      if constexpr (SC::ON) {
+        if (edge) {
+          asm volatile("");  // keeps the block a branch rather than selects on every tile
 #pragma unroll
-        for (int u = r - 7; u <= r; ++u) {
-          const int c = 32 * bb + 8 * (u >> 2) + (u & 3);
-          bool hide = c > hi;
-          if constexpr (SC::ON) hide = hide || c <= hi - sc.window;
-          if (hide) pacc[bb][u] = 0.f;
+          for (int u = r - 7; u <= r; ++u) {
+            const int c = 32 * bb + 8 * (u >> 2) + (u & 3);
+            if (c > hi || c <= hi - sc.window) pacc[bb][u] = 0.f;
+          }
         }
       }
       sf[bb][r >> 3] = pack_frag(pacc[bb], r - 7);
