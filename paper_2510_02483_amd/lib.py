@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 
 import torch
 
@@ -576,15 +577,19 @@ def _tensors(name, ts):
     if not ts:
         raise ValueError(f"{name} must hold a tensor at least")
     here = torch.cuda.current_device() if torch.cuda.is_available() else -2
-    words = []  # of LsTensor: address, elements, type
-    for t in ts:
-        dtype = t.dtype
-        if (dtype is not _F32 and dtype is not _BF16) or not t.is_contiguous() or t.get_device() != here:
-            i = next(k for k, u in enumerate(ts) if u is t)
-            raise ValueError(f"{name}[{i}] must be float32 or bfloat16, contiguous and on the current GPU, not "
-                             f"{dtype}, strides {t.stride()}, {t.device}")
-        words += (t.data_ptr(), t.numel(), dtype is _BF16)
-    return (LsTensor * len(ts)).from_buffer((ctypes.c_uint64 * len(words))(*words))
+    of = torch.Tensor
+    dtypes = [t.dtype for t in ts]
+    if not {_F32, _BF16}.issuperset(dtypes) or set(map(of.get_device, ts)) != {here} or not all(map(of.is_contiguous, ts)):
+        for i, t in enumerate(ts):
+            if t.dtype not in (_F32, _BF16) or t.get_device() != here or not t.is_contiguous():
+                raise ValueError(f"{name}[{i}] must be float32 or bfloat16, contiguous and on the current GPU, not "
+                                 f"{t.dtype}, strides {t.stride()}, {t.device}")
+    # LsTensor's words: address, elements, type (0.25 us a tensor; an entry at a time 0.9)
+    words = array("Q", bytes(24 * len(ts)))
+    words[0::3] = array("Q", map(of.data_ptr, ts))
+    words[1::3] = array("Q", map(of.numel, ts))
+    words[2::3] = array("Q", [d is _BF16 for d in dtypes])
+    return (LsTensor * len(ts)).from_buffer(words)
 
 
 def ls_grad_norm_workspace() -> int:
