@@ -73,6 +73,29 @@ def test_against_the_reference(lens, nq, nkv, d):
     Norm(Batch(nq=nq, nkv=nkv, d=d, seed=11, **LENGTHS[lens])).fwd().bwd().check()
 
 
+@pytest.mark.parametrize("nq,nkv,d", [(16, 2, 128), (32, 8, 64), (64, 64, 104), (48, 3, 72), (32, 1, 88), (128, 4, 64)])
+@pytest.mark.parametrize("lens", ["one_row", "empty_ones", "mixed"])
+def test_rows_that_several_waves_share(lens, nq, nkv, d):
+    """Heads that are cut evenly, with key heads that are not, in place too."""
+    need_gpu()
+    n = Norm(Batch(nq=nq, nkv=nkv, d=d, seed=13, **LENGTHS[lens])).fwd().bwd()
+    n.check()
+    inside = ~n.b.outside
+    work = n.b.qkv.clone()
+    n.fwd(work, work)
+    assert torch.equal(work[inside], n.y[inside]) and torch.isnan(work[~inside]).all()
+    work, gains = n.dy.clone(), (n.dgq.clone(), n.dgk.clone())
+    n.bwd(work, work)
+    assert torch.equal(work[inside], n.dx[inside]) and torch.isnan(work[~inside]).all()
+    assert torch.equal(gains[0], n.dgq) and torch.equal(gains[1], n.dgk)
+
+
+@pytest.mark.parametrize("total", [16383, 32767, 32768])
+def test_rows_around_the_number_that_is_cut(total):
+    need_gpu()
+    Norm(Batch([total - 5, 1, 4], 16, 1, 64 + 8, seed=14)).fwd().bwd().check()
+
+
 @pytest.mark.parametrize("nq,nkv,d", [(4, 2, 64), (2, 1, 104)])
 def test_many_rows(nq, nkv, d):
     """More rows than the backward pass has waves."""
