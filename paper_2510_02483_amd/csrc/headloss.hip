@@ -164,12 +164,15 @@ __global__ __launch_bounds__(HL_GATHER) void head_gather_kernel(int64_t T, int H
   float most = 0.f;  // (of the last workgroup's rows, all of them)
   auto larger = [&](int64_t t, int g) {
     if constexpr (LOGPROB) {
-      if (blockIdx.x + 1 < gridDim.x || !has_target(g, V)) return;
+      if (blockIdx.x + 1 < gridDim.x) return;
+      // (loaded with a target or without, so that the loads of several rows are in flight)
       const float a = x.g ? fabsf(x.g[t]) : 0.f, b = x.e ? fabsf(x.e[t]) : 0.f;
-      if (a < INFINITY) most = fmaxf(most, a);
-      if (b < INFINITY) most = fmaxf(most, b);
+      const bool has = has_target(g, V);
+      if (has && a < INFINITY) most = fmaxf(most, a);
+      if (has && b < INFINITY) most = fmaxf(most, b);
     }
   };
+#pragma unroll 4
   for (int64_t t = tid; t < r0; t += HL_GATHER) {
     const int g = targets[t];
     before += g != -1;
@@ -221,7 +224,15 @@ __global__ __launch_bounds__(HL_GATHER) void head_gather_kernel(int64_t T, int H
       if (to < 0) continue;
       const u32x4* src = (const u32x4*)(h + (c0 + k) * H);
       u32x4* dst = (u32x4*)(hc + (int64_t)to * H);
-      for (int c = lane; c < H / 8; c += 64) dst[c] = src[c];
+      for (int c = lane; c < H / 8; c += 256) {  // four loads in flight
+        u32x4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (c + 64 * u < H / 8) v[u] = src[c + 64 * u];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (c + 64 * u < H / 8) dst[c + 64 * u] = v[u];
+      }
     }
     __syncthreads();
   }
