@@ -16,6 +16,8 @@
 // (groups of 16, 131 MB and 1.3 GB: 288 us with the maxima by group, rows next to each other).
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -313,16 +315,17 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_top_one_kernel(int64_t T, 
   logprob[row * top + tid] = i == INT32_MAX ? -INFINITY : sh.ov[tid] * x.scale - sh.lse;
 }
 
-// A wave to a row, for many rows; the workgroup reads 1024 groups of its 16 rows at a time through LDS, the next
+// A wave to a row, for many rows; the workgroup reads 1024 groups of its 16 (or 4) rows at a time through LDS, the next
 // 1024 in flight meanwhile (with 256, which are 16 KB to a compute unit, memory's latency bounds it: 224 us at the size above).  Bound by reading the chosen groups' head weights again.
-__global__ __launch_bounds__(LP_THREADS) void logprob_top_kernel(int64_t T, int H, int V, int top, float scale,
+template <int ROWS>
+__global__ __launch_bounds__(64 * ROWS) void logprob_top_kernel(int64_t T, int H, int V, int top, float scale,
                                                                  const bf16_t* __restrict__ h,
                                                                  const bf16_t* __restrict__ embed,
                                                                  GroupMax gmax,
                                                                  const float* __restrict__ lse,
                                                                  int32_t* __restrict__ ids,
                                                                  float* __restrict__ logprob) {
-  constexpr int ROWS = LP_WAVES, CHUNKS = 16;
+  constexpr int CHUNKS = 16;
   __shared__ float tile[2][ROWS][64 * CHUNKS + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int groups = (V + GROUP - 1) / GROUP;
@@ -383,9 +386,9 @@ hipError_t logprob_rows(int64_t T, int V, const LogprobRows& x, hipStream_t s) {
 
 hipError_t logprob_top(int64_t T, int H, int V, int top, const LogprobRows& x, const bf16_t* h, const bf16_t* embed,
                        const GroupMax& gmax, int32_t* ids, float* logprob, hipStream_t s) {
-  // us for all rows, one to a workgroup / one to a wave (hidden 2048): vocabulary 32000, five alternatives, 512 rows 41 / 72,
-  // 1024 rows 77 / 73; vocabulary 128256 96 / 109 and 186 / 120; 64 alternatives, 1024 rows 386 / 573 and 501 / 868,
-  // 2048 rows 720 / 764 and 963 / 941
+  // us for all rows, one to a workgroup / 4 / 16 (hidden 2048): vocabulary 32000, five alternatives, 512 rows 41 / 52 / 72,
+  // 1024 rows 77 / 55 / 73, 4096 rows 279 / 153 / 145; vocabulary 128256 96 / 83 / 108, 187 / 87 / 118 and 734 / 268 / 192;
+  // 64 alternatives, 1024 rows 382 / 393 / 570 and 504 / 490 / 875, 2048 rows 722 / 783 / 764 and 968 / 855 / 944
   if (T <= (top > 16 ? 1024 : 512)) {
     hipLaunchKernelGGL(logprob_top_one_kernel, dim3((unsigned)T), dim3(LP_THREADS), 0, s, T, H, V, top, x, h, embed, gmax,
                        ids, logprob);
@@ -393,8 +396,13 @@ hipError_t logprob_top(int64_t T, int H, int V, int top, const LogprobRows& x, c
   }
   const hipError_t e = logprob_rows(T, V, x, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(logprob_top_kernel, dim3((unsigned)((T + LP_WAVES - 1) / LP_WAVES)), dim3(LP_THREADS), 0, s, T, H, V,
-                     top, x.scale, h, embed, gmax, (const float*)x.lse, ids, logprob);
+  auto launch = [&](auto rows) {
+    constexpr int ROWS = decltype(rows)::value;
+    hipLaunchKernelGGL((logprob_top_kernel<ROWS>), dim3((unsigned)((T + ROWS - 1) / ROWS)), dim3(64 * ROWS), 0, s, T, H, V,
+                       top, x.scale, h, embed, gmax, (const float*)x.lse, ids, logprob);
+  };
+  if (T <= 1024) launch(std::integral_constant<int, 4>{});
+  else launch(std::integral_constant<int, 16>{});
   return hipGetLastError();
 }
 

@@ -129,7 +129,7 @@ def check_bwd(x, r, low=False):
 # than one tile of every kind; more rows than one workgroup each serves
 SHAPES = [(1, 64, 100, 8), (1, 2048, 3001, 64), (3, 8, 50, 1), (33, 24, 7, 9), (5, 16, 1, 2), (17, 40, 65, 64), (7, 72, 1003, 17),
           (64, 128, 129, 3), (65, 128, 16, 4), (130, 256, 512, 5), (257, 128, 2049, 64), (300, 320, 5000, 2),
-          (512, 64, 1500, 16), (513, 64, 1500, 16), (1024, 72, 900, 17), (1025, 64, 20003, 6), (1040, 128, 33, 33)]
+          (512, 64, 1500, 16), (513, 64, 1500, 16), (1022, 64, 9000, 8), (1024, 72, 900, 17), (1025, 64, 20003, 6), (1040, 128, 33, 33)]
 
 
 @pytest.mark.parametrize("T,H,V,top", SHAPES)
@@ -177,7 +177,7 @@ def test_all_logits_equal():
         assert float((x.vals.double() + ln).abs().max()) <= 2.0 ** -17 + ln * 2.0 ** -21
 
 
-@pytest.mark.parametrize("T", [2, 1030])
+@pytest.mark.parametrize("T", [2, 601, 1030])
 @pytest.mark.parametrize("top", [1, 16, 17, 64])
 @pytest.mark.parametrize("low", [None, 0, 5, 15])
 def test_logits_in_any_arrangement(T, top, low):
