@@ -382,7 +382,8 @@ int ls_packed_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes
  *
  *   r = (mean x^2 + eps)^-1/2,  y = R_p (x r g),
  *
- * R_p the rotation of ls_packed_rope.  eps >= 0.  dst == src works in place and leaves v
+ * R_p the rotation of ls_packed_rope.  x may be of any finite size, each head of its
+ * own.  eps >= 0 (0: a head of zeros becomes NaN).  dst == src works in place and leaves v
  * alone; otherwise the buffers must not overlap and v is copied.  Rows of no
  * sequence are left as they were.
  *
@@ -392,7 +393,7 @@ int ls_packed_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes
  *
  * ([head_dim] fp32, NULL: not wanted; both NULL: the workspace is not used).
  * src is the forward call's (so the forward pass of a training step works out of place), r is
- * formed again from it.  dx == dy works in place; otherwise v's part is copied.
+ * formed again from it.  Sums over a head are of fp32: g dy of up to 2^115.  dx == dy works in place; otherwise v's part is copied.
  * Rows of no sequence add nothing to the gains' gradients, whatever they hold.
  * Every output is deterministic.  workspace: at least
  * ls_packed_qk_norm_rope_bwd_workspace(cfg) bytes. */

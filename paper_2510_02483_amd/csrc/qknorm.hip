@@ -44,6 +44,15 @@ LS_DEV float head_sum(float v) {
   return v;
 }
 
+template <int G>
+LS_DEV float head_max(float v) {  // (of values from 0 on)
+  v = fmaxf(v, dpp<0xB1>(v));
+  v = fmaxf(v, dpp<0x4E>(v));
+  if constexpr (G >= 8) v = fmaxf(v, dpp<0x141>(v));
+  if constexpr (G >= 16) v = fmaxf(v, dpp<0x140>(v));
+  return v;
+}
+
 // V features of either half of a head, and the cos and sin of their angles.
 template <int V>
 struct Pairs {
@@ -94,6 +103,39 @@ LS_DEV void store_pairs(bf16_t* p, int half, const Pairs<V>& x) {
   }
   *(words*)p = u;
   *(words*)(p + half) = w;
+}
+// A head's sum of squares.
+template <int V, int G>
+LS_DEV float squares(const Pairs<V>& x) {
+  float ss = 0.f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
+  return head_sum<G>(ss);
+}
+// r = (mean x^2 + eps)^-1/2 of a head.  bf16 reaches as far as fp32: squares of values beyond 2^64 leave it, and those
+// below 2^-63 lose bits, which counts where mean and eps are small.  Where a head of the wave is so (`ok`: the lane has one),
+// its x is divided by 2^k, the size of the larger of max |x| and sqrt(eps), r is that of the divided head, and `far` is set; a
+// head that is not has k = 0, so that nothing changes for it.  (r x is the same; what r multiplies otherwise is to be
+// divided by 2^k.)
+template <int V, int G>
+LS_DEV float inverse_size(Pairs<V>& x, int d, float eps, bool ok, bool& far, int& k) {
+  float ms = squares<V, G>(x) / (float)d + eps;
+  far = __ballot(ok && !(ms >= 0x1p-96f && ms < INFINITY));
+  k = 0;
+  if (far) {
+    float big = 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) big = fmaxf(big, fmaxf(fabsf(x.a[e]), fabsf(x.b[e])));
+    big = fmaxf(head_max<G>(big), sqrtf(eps));
+    if (!(ms >= 0x1p-96f && ms < INFINITY) && big > 0.f && big < INFINITY) k = ilogbf(big);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      x.a[e] = ldexpf(x.a[e], -k);
+      x.b[e] = ldexpf(x.b[e], -k);
+    }
+    ms = squares<V, G>(x) / (float)d + ldexpf(eps, -2 * k);
+  }
+  return 1.0f / sqrtf(ms);
 }
 // The row's angles, one per lane in fp64 as turns without their whole part (in fp32 the
 // fraction of a far position's angle would be lost), then handed to the lanes of the pairs.
@@ -160,10 +202,9 @@ __global__ __launch_bounds__(64 * QKN_WAVES, 4) void qk_norm_rope_kernel(int tot
           const bool ok = in && hu + u * HPW + h0 < n;
           const int64_t at = at0 + u * HPW * d;
           Pairs<V> x = raw[u].pairs();
-          float ss = 0.f;
-#pragma unroll
-          for (int e = 0; e < V; ++e) ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
-          const float r = 1.0f / sqrtf(head_sum<G>(ss) / (float)d + eps);
+          bool far;
+          int k;
+          const float r = inverse_size<V, G>(x, d, eps, ok, far, k);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             const float a = x.a[e] * r * g.a[e], b = x.b[e] * r * g.b[e];
@@ -219,30 +260,39 @@ __global__ __launch_bounds__(64 * QKN_WAVES, V == 4 ? 4 : 3) void qk_norm_rope_b
           if (hu + u * HPW >= n) break;
           const bool ok = in && hu + u * HPW + h0 < n;
           const int64_t at = at0 + u * HPW * d;
-          const Pairs<V> x = xr[u].pairs(), t = tr[u].pairs();
+          Pairs<V> x = xr[u].pairs();
+          const Pairs<V> t = tr[u].pairs();
+          bool far;
+          int k;
+          const float size = inverse_size<V, G>(x, d, eps, ok, far, k);
+          const float r = ok ? size : 0.f;  // (a lane without a head adds nothing to the gains' sums, eps 0 too)
           Pairs<V> dn;
-          float ss = 0.f, dot = 0.f;
+          float dot = 0.f;
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             dn.a[e] = t.a[e] * cs.a[e] + t.b[e] * cs.b[e];
             dn.b[e] = t.b[e] * cs.a[e] - t.a[e] * cs.b[e];
-            ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
             dot += g.a[e] * dn.a[e] * x.a[e] + g.b[e] * dn.b[e] * x.b[e];
-        }
-        const float ms = head_sum<G>(ss) / (float)d + eps;
-        const float r = ok ? 1.0f / sqrtf(ms) : 0.f;  // (a lane without a head adds nothing to the gains' sums, eps 0 too)
-        // <a, x r> / d: with r inside, no power of it can leave the range
-        const float coef = r * head_sum<G>(dot) / (float)d;
-        Pairs<V> out;
+          }
+          // <a, x r> / d: with r inside, no power of it can leave the range
+          const float coef = r * head_sum<G>(dot) / (float)d;
+          Pairs<V> out;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float na = x.a[e] * r, nb = x.b[e] * r;
-          sum.a[e] += dn.a[e] * na;
-          sum.b[e] += dn.b[e] * nb;
-          out.a[e] = r * (g.a[e] * dn.a[e] - na * coef);
-          out.b[e] = r * (g.b[e] * dn.b[e] - nb * coef);
-        }
-        if (ok) store_pairs<V>(dx + at, half, out);
+          for (int e = 0; e < V; ++e) {
+            const float na = x.a[e] * r, nb = x.b[e] * r;
+            sum.a[e] += dn.a[e] * na;
+            sum.b[e] += dn.b[e] * nb;
+            out.a[e] = r * (g.a[e] * dn.a[e] - na * coef);
+            out.b[e] = r * (g.b[e] * dn.b[e] - nb * coef);
+          }
+          if (far) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              out.a[e] = ldexpf(out.a[e], -k);
+              out.b[e] = ldexpf(out.b[e], -k);
+            }
+          }
+          if (ok) store_pairs<V>(dx + at, half, out);
         }
       }
     };
