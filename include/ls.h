@@ -559,8 +559,9 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
  * is not finite makes its row of dh and the head's gradient NaN.  entropy and lse are the forward
  * call's, for the same scale, h, embed and targets.  workspace: at least
  * ls_token_logprob_workspace(tokens, hidden, vocab, top, piece) bytes, which serve the forward call with this
- * top (or 0) and the backward call with this piece.  With a top it holds 4 bytes for every 8 logits (the largest of
- * each 8 entries); tokens may be split over calls.  Every output is deterministic. */
+ * top (or 0) and the backward call with this piece: the larger of the two.  Without a backward call, piece 1
+ * leaves little but the forward call's share.  With a top that holds 4 bytes for every 8 logits (the largest of
+ * each 8 entries) and is not taken by pieces; tokens may be split over calls.  Every output is deterministic. */
 size_t ls_token_logprob_workspace(int64_t tokens, int32_t hidden, int32_t vocab, int32_t top, int32_t piece);
 int ls_token_logprob_fwd(int64_t tokens, int32_t hidden, int32_t vocab, float scale, const ls_bf16* h,
                          const ls_bf16* embed, const int32_t* targets, float* logprob, float* entropy, float* lse,
