@@ -1182,13 +1182,14 @@ int ls_packed_qk_norm_rope_bwd(const ls_packed_cfg* cfg, const void* plan, size_
                       {k_gain, gain, "k_gain"},
                       {src, bytes, "src"},
                       {dy, bytes, "dy"}};
-  Range out[4] = {{dx, bytes, "dx"}, {workspace, workspace_bytes, "workspace"}};
-  size_t nout = 2;
+  Range out[4] = {{dx, bytes, "dx"}};
+  size_t nout = 1;
+  if (dq_gain || dk_gain) out[nout++] = {workspace, workspace_bytes, "workspace"};
   if (dq_gain) out[nout++] = {dq_gain, 2 * gain, "dq_gain"};
   if (dk_gain) out[nout++] = {dk_gain, 2 * gain, "dk_gain"};
   if (int e = check_ranges(in, dy == dx ? 4 : 5, out, nout)) return e;
   if (int e = check_plan_bytes(p, plan_bytes)) return e;
-  const size_t need = ls::packed_qk_norm_rope_bwd_workspace(p);
+  const size_t need = dq_gain || dk_gain ? ls::packed_qk_norm_rope_bwd_workspace(p) : 0;
   if (workspace_bytes < need) return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, need);
   const hipStream_t st = (hipStream_t)stream;
   LS_STEP("packed qk norm rope bwd", st,

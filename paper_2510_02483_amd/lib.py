@@ -365,7 +365,8 @@ def ls_packed_qk_norm_rope_bwd_workspace(c) -> int:
 
 def ls_packed_qk_norm_rope_bwd(c, plan, theta, eps, q_gain, k_gain, src, dy, dx, dq_gain, dk_gain, accumulate,
                                workspace, stream=None):
-    """src: the forward call's, before the norm; dx may be dy; either gain's gradient (head_dim fp32) may be None."""
+    """src: the forward call's, before the norm; dx may be dy; either gain's gradient (head_dim fp32) may be None, and
+    with both of them the workspace."""
     n, _ = _packed_sizes(c)
     _need(("plan", plan, None, None), ("q_gain", q_gain, _BF16, c.head_dim), ("k_gain", k_gain, _BF16, c.head_dim),
           ("src", src, _BF16, n), ("dy", dy, _BF16, n), ("dx", dx, _BF16, n), ("dq_gain", dq_gain, _F32, c.head_dim),
