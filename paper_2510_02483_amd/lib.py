@@ -517,12 +517,14 @@ def ls_token_logprob_fwd(h, embed, targets, logprob, entropy, lse, workspace, sc
     if (top_ids is None) != (top_logprob is None):
         raise ValueError("top_ids and top_logprob go together")
     top = 0 if top_ids is None else top_ids.numel() // max(T, 1)
+    # (buffers of another number of tokens would be filled with rows of another length)
+    if top_ids is not None and (top == 0 or top_logprob.numel() != T * top or
+                                any(t.dim() > 1 and t.shape[-1] != top for t in (top_ids, top_logprob))):
+        raise ValueError("top_ids and top_logprob must both be [tokens, top]")
     _need(("h", h, _BF16, T * H), ("embed", embed, _BF16, embed.shape[0] * H), ("targets", targets, torch.int32, T),
           ("logprob", logprob, _F32, T), ("entropy", entropy, _F32, T), ("lse", lse, _F32, T),
           ("top_ids", top_ids, torch.int32, T * top), ("top_logprob", top_logprob, _F32, T * top),
           ("workspace", workspace, None, None))
-    if top_ids is not None and (top == 0 or top_logprob.numel() != T * top):
-        raise ValueError("top_ids and top_logprob must both be [tokens, top]")
     _check(lib().ls_token_logprob_fwd(T, H, embed.shape[0], scale, _p(h), _p(embed), _p(targets), _p(logprob),
                                       _p(entropy), _p(lse), top, _p(top_ids), _p(top_logprob), _p(workspace),
                                       _bytes(workspace), _stream(stream)), "ls_token_logprob_fwd")
