@@ -438,7 +438,7 @@ int ls_packed_attn_bwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_b
  * every score's gradient of a row holds, then carries 2^-17 of its terms and not 2^-8
  * (scores of a standard deviation of 4: dqkv 0.0024 of its norm off instead of 0.0032). */
 typedef struct {
-  float scale;    /* 0: 1/sqrt(head_dim); positive */
+  float scale;    /* 0: 1/sqrt(head_dim); positive, at most 2^127 */
   float cap;      /* 0: none; 0.01 .. 1000, scale / cap at most 1e30 */
   int32_t window; /* positions that a query sees, itself included; 0: all before it */
 } ls_score_cfg;
@@ -536,7 +536,7 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
 /* ---- log probabilities of given tokens, entropies and top alternatives ---------------
  *
  * For hidden states h [tokens, hidden], head weights embed [vocab, hidden] and the scaled
- * logits z = scale h embed^T (scale > 0: one over a temperature), formed tile by tile and
+ * logits z = scale h embed^T (0 < scale <= 2^127: one over a temperature), formed tile by tile and
  * not stored:
  *
  *   lse[t] = ln sum_v exp z[t,v];  logprob[t] = z[t, targets[t]] - lse[t];

@@ -1239,9 +1239,11 @@ int ls_packed_attn_bwd(const ls_packed_cfg* cfg, const void* plan, size_t plan_b
   return LS_OK;
 }
 
+static constexpr float kMaxScale = 0x1p127f;  // (its product with log2(e) is finite)
+
 static int check_score_cfg(const ls_score_cfg* c, const ls::PackedShape& p, ls::ScoreShape& out, bool& plain) {
   if (!c) return fail(LS_ERR_NULL, "score is NULL");
-  if (!(c->scale >= 0.0f) || !(c->scale <= 3.4e38f)) return fail(LS_ERR_SHAPE, "scale must be positive and finite, or 0");
+  if (!(c->scale >= 0.0f) || !(c->scale <= kMaxScale)) return fail(LS_ERR_SHAPE, "scale must be positive and at most 2^127, or 0");
   if (!(c->cap >= 0.0f)) return fail(LS_ERR_SHAPE, "cap must be positive, or 0");
   if (c->cap > 0.0f && (c->cap < 0.01f || c->cap > 1000.0f))
     return fail(LS_ERR_UNSUPPORTED, "cap (%g) outside 0.01 .. 1000", (double)c->cap);
@@ -1881,7 +1883,7 @@ int ls_head_loss_bwd(int64_t tokens, int32_t hidden, int32_t vocab, const ls_bf1
 
 static int check_logprob(int64_t tokens, int32_t hidden, int32_t vocab, int32_t piece, float scale, int32_t top) {
   if (int e = check_head(tokens, hidden, vocab, piece)) return e;
-  if (!(scale > 0.0f) || !(scale <= 3.4e38f)) return fail(LS_ERR_SHAPE, "scale must be positive and finite");
+  if (!(scale > 0.0f) || !(scale <= kMaxScale)) return fail(LS_ERR_SHAPE, "scale must be positive and at most 2^127");
   if (top < 0) return fail(LS_ERR_SHAPE, "top must be >= 0");
   if (top > ls::LOGPROB_TOP) return fail(LS_ERR_UNSUPPORTED, "top (%d) exceeds %d", top, ls::LOGPROB_TOP);
   return LS_OK;
