@@ -379,7 +379,8 @@ def ls_packed_qk_norm_rope_bwd(c, plan, theta, eps, q_gain, k_gain, src, dy, dx,
 
 
 def make_score_cfg(s: ScoreConfig) -> LsScoreCfg:
-    return LsScoreCfg(s.scale, s.cap, s.window)
+    most = 2 ** 31 - 1  # more rows than a call takes
+    return LsScoreCfg(s.scale, s.cap, max(-most, min(s.window, most)))
 
 
 def ls_packed_score_attn_fwd(c, score, plan, qkv, o, lse, o_rest=None, stream=None):
