@@ -176,10 +176,13 @@ def _p(t):  # (the prototypes make a pointer of it)
 
 def _stream(stream=None):
     """The handle of `stream`, or of the current device's current stream (2.8 us through torch.cuda.current_stream(), which
-    makes an object of it; 0.4 us so)."""
+    makes an object of it; 0.4 us so, by a name that PyTorch does not promise to keep)."""
     if stream is not None:
         return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    try:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    except AttributeError:
+        return torch.cuda.current_stream().cuda_stream
 
 
 def make_cfg(c: BlockConfig) -> LsBlockCfg:
