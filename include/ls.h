@@ -393,7 +393,8 @@ int ls_packed_rope(const ls_packed_cfg* cfg, const void* plan, size_t plan_bytes
  *
  * ([head_dim] fp32, NULL: not wanted; both NULL: the workspace is not used).
  * src is the forward call's (so the forward pass of a training step works out of place), r is
- * formed again from it.  Sums over a head are of fp32: g dy of up to 2^115.  dx == dy works in place; otherwise v's part is copied.
+ * formed again from it.  Sums over a head are of fp32: g dy of up to 2^115.
+ * dx == dy works in place; otherwise v's part is copied.
  * Rows of no sequence add nothing to the gains' gradients, whatever they hold.
  * Every output is deterministic.  workspace: at least
  * ls_packed_qk_norm_rope_bwd_workspace(cfg) bytes. */
@@ -602,8 +603,8 @@ int ls_gemm_tile_override(int32_t bm, int32_t bn);
  * "dWd", "dh2", "dWg/dWu", "rmsnorm bwd", "dO", "dWo", "attention bwd",
  * "dh1", "dWqkv", "packed plan", "packed rope", "packed attention fwd",
  * "packed attention bwd", "packed qk norm rope", "packed qk norm rope bwd", "packed score attention fwd",
- * "packed score attention bwd", "gradient norm", "gradient clip", "logprob logits", "logprob rows", "logprob top", "logprob gather",
- * "logprob dz", "logprob dh", "logprob dE", "logprob scatter", "head loss logits", "head loss rows", "head loss gather",
+ * "packed score attention bwd", "gradient norm", "gradient clip", "logprob logits", "logprob rows",
+ * "logprob top", "logprob gather", "logprob dz", "logprob dh", "logprob dE", "logprob scatter", "head loss logits", "head loss rows", "head loss gather",
  * "head loss dz", "head loss dh", "head loss dE", "head loss scatter", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
  * "logits", "cross-entropy", "dh head", "dE head", "loss", "embedding bwd",
  * and "adamw" for ls_adamw_step),

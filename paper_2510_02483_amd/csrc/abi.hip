@@ -1243,7 +1243,8 @@ static constexpr float kMaxScale = 0x1p127f;  // (its product with log2(e) is fi
 
 static int check_score_cfg(const ls_score_cfg* c, const ls::PackedShape& p, ls::ScoreShape& out, bool& plain) {
   if (!c) return fail(LS_ERR_NULL, "score is NULL");
-  if (!(c->scale >= 0.0f) || !(c->scale <= kMaxScale)) return fail(LS_ERR_SHAPE, "scale must be positive and at most 2^127, or 0");
+  if (!(c->scale >= 0.0f) || !(c->scale <= kMaxScale))
+    return fail(LS_ERR_SHAPE, "scale must be positive and at most 2^127, or 0");
   if (!(c->cap >= 0.0f)) return fail(LS_ERR_SHAPE, "cap must be positive, or 0");
   if (c->cap > 0.0f && (c->cap < 0.01f || c->cap > 1000.0f))
     return fail(LS_ERR_UNSUPPORTED, "cap (%g) outside 0.01 .. 1000", (double)c->cap);
@@ -1712,7 +1713,8 @@ static HeadWs head_ws(int64_t T, int64_t H, int64_t V, int64_t piece, HeadKind k
   w.gmax_groups = (int)((V + 255) / 256 * 32);
   w.gmax_rows = 0;
   while (w.gmax_rows < 4 && ((int64_t)1 << w.gmax_rows) < T) ++w.gmax_rows;
-  w.gmax = f.take(kind == HEAD_LOGPROB_TOP ? (size_t)ls::gmax_at(w.gmax_groups, w.gmax_rows, T + (1 << w.gmax_rows) - 1, 0) * 4 : 0);
+  const int64_t room = ls::gmax_at(w.gmax_groups, w.gmax_rows, T + (1 << w.gmax_rows) - 1, 0);
+  w.gmax = f.take(kind == HEAD_LOGPROB_TOP ? (size_t)room * 4 : 0);
   w.fwd_total = f.off;
   Carver b;
   w.coef = b.take(16);
@@ -1891,7 +1893,8 @@ static int check_logprob(int64_t tokens, int32_t hidden, int32_t vocab, int32_t 
 static HeadKind logprob_kind(int32_t top) { return top > 0 ? HEAD_LOGPROB_TOP : HEAD_LOGPROB; }
 
 size_t ls_token_logprob_workspace(int64_t tokens, int32_t hidden, int32_t vocab, int32_t top, int32_t piece) {
-  return check_logprob(tokens, hidden, vocab, piece, 1.0f, top) ? 0 : head_ws(tokens, hidden, vocab, piece, logprob_kind(top)).total;
+  if (check_logprob(tokens, hidden, vocab, piece, 1.0f, top)) return 0;
+  return head_ws(tokens, hidden, vocab, piece, logprob_kind(top)).total;
 }
 
 int ls_token_logprob_fwd(int64_t tokens, int32_t hidden, int32_t vocab, float scale, const ls_bf16* h,
@@ -1934,8 +1937,8 @@ int ls_token_logprob_fwd(int64_t tokens, int32_t hidden, int32_t vocab, float sc
   const ls::LogprobRows x{blocks, stats, zt, targets, logprob, entropy, lse, scale};
   if (top > 0)
     LS_STEP("logprob top", st,
-            ls::logprob_top(T, (int)H, (int)V, top, x, (const bf16_t*)h, (const bf16_t*)embed, ls::GroupMax{gmax, w.gmax_groups, w.gmax_rows},
-                            top_ids, top_logprob, st));
+            ls::logprob_top(T, (int)H, (int)V, top, x, (const bf16_t*)h, (const bf16_t*)embed,
+                            ls::GroupMax{gmax, w.gmax_groups, w.gmax_rows}, top_ids, top_logprob, st));
   else
     LS_STEP("logprob rows", st, ls::logprob_rows(T, (int)V, x, st));
   return LS_OK;
@@ -2067,7 +2070,8 @@ int ls_grad_norm(int32_t n, const ls_tensor* grads, float* norm, void* workspace
   if (int e = check_ranges(nullptr, 0, out, 2)) return e;
   for (const ls::GradTensor& t : g)
     for (const Range& r : out)
-      if (overlaps(r, Range{t.p, (size_t)t.n * (t.bf16 ? 2 : 4), ""})) return fail(LS_ERR_ALIAS, "%s overlaps a gradient", r.name);
+      if (overlaps(r, Range{t.p, (size_t)t.n * (t.bf16 ? 2 : 4), ""}))
+        return fail(LS_ERR_ALIAS, "%s overlaps a gradient", r.name);
   if (workspace_bytes < ls::grad_norm_workspace())
     return fail(LS_ERR_WORKSPACE, "workspace %zu < %zu bytes", workspace_bytes, ls::grad_norm_workspace());
   const hipStream_t st = (hipStream_t)stream;

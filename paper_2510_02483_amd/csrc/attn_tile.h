@@ -89,6 +89,9 @@ LS_DEV float add_bf2(uint32_t w, float s) {
 // at its ends).  r carries 1.9 x 2^-23 from the instructions (exp2 and reciprocal good to
 // 2^-23, the sum to 2^-24), the score 2 cap times that; the factor 4 of the slope goes into the
 // scale of dq and dk.
+// P, and in the backward pass dS, go into their products as bf16, which the matrix cores multiply sixteen times as fast as
+// fp32: one rounding of each entry, while scores, softmax and sums are of 32 bits.  Of dqkv's norm 0.0024 are off in all
+// (scores of a standard deviation of 4; 0.0017 is the rounding of dqkv itself).
 struct PlainScore {
   static constexpr bool ON = false, CAPPED = false;
   static constexpr int window = 0;  // (unused, as c2)
@@ -624,7 +627,8 @@ LS_DEV void bwd_pre_row(const AttnShape& sh, const bf16_t* __restrict__ orow, co
 // D[b,h,s] = <dO, O> over the head's d columns (fp32), and the log-sum-exp in
 // base 2 (lse * log2(e)), the form the backward kernels subtract.
 // REST: O is o and the rest that its rounding left.  neg: -D, what dP starts from where scores are modified; less: c2 of a
-// cap, which every exponent less the log-sum-exp holds.
+// cap, which every exponent less the log-sum-exp holds (the difference, at most 2 c2, is rounded once: 2^-24 of it, below
+// the 2^-21 cap that a capped score carries).
 template <int D, bool PACKED, bool REST = false>
 __global__ __launch_bounds__(256) void attn_bwd_pre_kernel(AttnShape sh, const bf16_t* __restrict__ o,
                                                            const bf16_t* __restrict__ dout,
@@ -636,7 +640,8 @@ __global__ __launch_bounds__(256) void attn_bwd_pre_kernel(AttnShape sh, const b
   const int64_t t = (int64_t)(PACKED ? packed_wg() : (int)blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (t >= (int64_t)sh.batch * sh.seq) return;
   if constexpr (PACKED) {
-    bwd_pre_row<D, REST>(sh, o + t * sh.nq * sh.d, dout + t * sh.nq * sh.d, lse, Dv, lse2, t, rest + t * sh.nq * sh.d, neg, less);
+    const int64_t at = t * sh.nq * sh.d;
+    bwd_pre_row<D, REST>(sh, o + at, dout + at, lse, Dv, lse2, t, rest + at, neg, less);
     return;
   }
   const int b = (int)(t / sh.seq), s = (int)(t % sh.seq);
@@ -1060,13 +1065,15 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
     const PackedKind kind = packed_piece(pk, kvt, sh.seq, t, part_no);
     if (kind == PACKED_IS_MID) {
       const int pair = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 7);
-      mid_bwd<D>(sh, sc, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + pair * mid_lds_bytes<D>(), 0, G, nullptr);
+      mid_bwd<D>(sh, sc, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + pair * mid_lds_bytes<D>(), 0, G,
+                 nullptr);
       return;
     }
     if (t.len == 0) return;
     if (kind == PACKED_IS_SHORT) {
       const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-      short_bwd<D>(sh, sc, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + w * short_lds_bytes<D>(), 0, G, nullptr);
+      short_bwd<D>(sh, sc, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + w * short_lds_bytes<D>(), 0, G,
+                   nullptr);
       return;
     }
     parts = __builtin_amdgcn_readfirstlane((int)t.parts);
@@ -1079,7 +1086,8 @@ LS_DEV void dkdv_tile(const AttnShape& sh, const SC& sc, const PackedView& pk, c
         if (w == 0) short_bwd<D>(sh, sc, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0], g0, g1, sums);
       } else {
         if (w >= 2) t.len = 0;  // (the first pair's)
-        mid_bwd<D>(sh, sc, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + (w >> 1) * mid_lds_bytes<D>(), g0, g1, sums);
+        mid_bwd<D>(sh, sc, t, kvh, qkv, dout, lse2, dqkv, scale, sl2, (char*)&stg[0] + (w >> 1) * mid_lds_bytes<D>(), g0,
+                   g1, sums);
       }
       return;
     }
@@ -1311,8 +1319,8 @@ __global__ __launch_bounds__(256, PACKED && D == 64 ? 2 : 1) void attn_bwd_dkdv_
                                                                 const float* __restrict__ rope_cs, float scale,
                                                                 float sl2, int hsplit, float* __restrict__ part, SC sc) {
   __shared__ __attribute__((aligned(1024))) DkdvStage<D> stg[DKDV_STAGES];
-  dkdv_tile<D, SPLIT, PACKED>(sh, sc, pk, PACKED ? packed_wg() : (int)blockIdx.x, stg, qkv, dout, lse2, Dv, dqkv, rope_cs, scale, sl2,
-                              hsplit, part);
+  dkdv_tile<D, SPLIT, PACKED>(sh, sc, pk, PACKED ? packed_wg() : (int)blockIdx.x, stg, qkv, dout, lse2, Dv, dqkv,
+                              rope_cs, scale, sl2, hsplit, part);
 }
 
 // dK and dV of 32 rows of a packed key tile, if its work was cut into parts, and one kv
@@ -1440,8 +1448,8 @@ __global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, int hs
 // of registers within the tile; two workgroups per compute unit keep the
 // matrix cores busy across tile boundaries and while one wave waits.
 template <int D, bool PACKED, class SC>
-LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_t (&Ks)[2][BKV * D], bf16_t (&Vs)[2][BKV * D],
-                    const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
+LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_t (&Ks)[2][BKV * D],
+                    bf16_t (&Vs)[2][BKV * D], const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
                     const float* __restrict__ Dv, bf16_t* __restrict__ dqkv, const float* __restrict__ rope_cs,
                     float scale, float sl2) {
   constexpr int NSD = D / 16, NI = D / 32;

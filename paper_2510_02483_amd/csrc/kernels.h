@@ -250,8 +250,8 @@ hipError_t logprob_rows(int64_t T, int V, const LogprobRows& x, hipStream_t s);
 // The same, and the `top` (1 .. 64) largest logits of every row, ties to the lower column, from the largest of every 8
 // columns (gmax): ids (-1 past the vocabulary) and scaled logit - lse.
 constexpr int LOGPROB_TOP = 64;
-// Where a row's maximum of group g lies: blocks of 2^rows rows (16, or as many as there are), in each group by group, so that
-// a workgroup that takes 16 rows reads one piece of memory.
+// Where a row's maximum of group g lies: blocks of 2^rows rows (16, or as many as there are), in each group by group,
+// so that a workgroup that takes 16 rows reads one piece of memory.
 __host__ __device__ inline int64_t gmax_at(int groups, int rows, int64_t m, int g) {
   return ((((m >> rows) * groups) + g) << rows) + (m & ((1 << rows) - 1));
 }

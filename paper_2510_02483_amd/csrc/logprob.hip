@@ -229,7 +229,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_top_one_kernel(int64_t T, 
     const unsigned long long in = __ballot(i != INT32_MAX && v == wv);
     // (lanes hold groups in no order: of equal ones the lowest)
     int wi = INT32_MAX;
-    for (unsigned long long left = in; left; left &= left - 1) wi = min(wi, __builtin_amdgcn_readlane(i, __builtin_ctzll(left)));
+    for (unsigned long long left = in; left; left &= left - 1)
+      wi = min(wi, __builtin_amdgcn_readlane(i, __builtin_ctzll(left)));
     if (lane == 0) {
       sh.bv[wave] = wi == INT32_MAX ? -INFINITY : wv;
       sh.bi[wave] = wi;
@@ -316,7 +317,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_top_one_kernel(int64_t T, 
 }
 
 // A wave to a row, for many rows; the workgroup reads 1024 groups of its 16 (or 4) rows at a time through LDS, the next
-// 1024 in flight meanwhile (with 256, which are 16 KB to a compute unit, memory's latency bounds it: 224 us at the size above).  Bound by reading the chosen groups' head weights again.
+// 1024 in flight meanwhile (with 256, which are 16 KB to a compute unit, memory's latency bounds it: 224 us at the size
+// above).  Bound by reading the chosen groups' head weights again.
 template <int ROWS>
 __global__ __launch_bounds__(64 * ROWS) void logprob_top_kernel(int64_t T, int H, int V, int top, float scale,
                                                                  const bf16_t* __restrict__ h,

@@ -112,11 +112,12 @@ LS_DEV float squares(const Pairs<V>& x) {
   for (int e = 0; e < V; ++e) ss += x.a[e] * x.a[e] + x.b[e] * x.b[e];
   return head_sum<G>(ss);
 }
-// r = (mean x^2 + eps)^-1/2 of a head.  bf16 reaches as far as fp32: squares of values beyond 2^64 leave it, and those
-// below 2^-63 lose bits, which counts where mean and eps are small.  Where a head of the wave is so (`ok`: the lane has one),
-// its x is divided by 2^k, the size of the larger of max |x| and sqrt(eps), r is that of the divided head, and `far` is set; a
-// head that is not has k = 0, so that nothing changes for it.  (r x is the same; what r multiplies otherwise is to be
-// divided by 2^k.)
+// r = (mean x^2 + eps)^-1/2 of a head.  bf16 reaches as far as fp32: squares of values beyond 2^64 leave its
+// range, and those below 2^-63 lose bits, which counts where mean and eps are small.  Where a head of the wave is so
+// (`ok`: the lane has one), its x is divided by 2^k, the size of the larger of max |x| and sqrt(eps), r is that of
+// the divided head, and `far` is set; any other head has k = 0, so that nothing changes for it.  (r x is the same;
+// what else r multiplies is to be divided by 2^k.)  Ordinary data pays a comparison and a ballot: 8135 rows of
+// 24/8 heads of 128, both passes, 77.6 -> 77.9 us.
 template <int V, int G>
 LS_DEV float inverse_size(Pairs<V>& x, int d, float eps, bool ok, bool& far, int& k) {
   float ms = squares<V, G>(x) / (float)d + eps;
@@ -170,12 +171,9 @@ LS_DEV void copy_v(const bf16_t* src, bf16_t* dst, int n, int lane, int seg, int
 }
 
 template <int V, int G>
-__global__ __launch_bounds__(64 * QKN_WAVES, 4) void qk_norm_rope_kernel(int total, int seg_bits, int nq, int nkv, int d, float eps,
-                                                                      double log2_theta,
-                                                                      const int32_t* __restrict__ pos,
-                                                                      const bf16_t* __restrict__ gq,
-                                                                      const bf16_t* __restrict__ gk, const bf16_t* src,
-                                                                      bf16_t* dst) {
+__global__ __launch_bounds__(64 * QKN_WAVES, 4) void qk_norm_rope_kernel(
+    int total, int seg_bits, int nq, int nkv, int d, float eps, double log2_theta, const int32_t* __restrict__ pos,
+    const bf16_t* __restrict__ gq, const bf16_t* __restrict__ gk, const bf16_t* src, bf16_t* dst) {
   constexpr int HPW = 64 / G, U = batch_of<V>();
   const int lane = threadIdx.x & 63, half = d / 2, c = lane % G, h0 = lane / G;
   const bool in = V * c < half;
@@ -217,7 +215,8 @@ __global__ __launch_bounds__(64 * QKN_WAVES, 4) void qk_norm_rope_kernel(int tot
     };
     heads(0, nq, gains[0]);
     heads(nq, nkv, gains[1]);
-    if (src != dst) copy_v(src + row * ld + (int64_t)(nq + nkv) * d, dst + row * ld + (int64_t)(nq + nkv) * d, nkv * d, lane, seg, segs);
+    const int64_t v = row * ld + (int64_t)(nq + nkv) * d;
+    if (src != dst) copy_v(src + v, dst + v, nkv * d, lane, seg, segs);
   }
 }
 
@@ -232,7 +231,8 @@ __global__ __launch_bounds__(64 * QKN_WAVES, V == 4 ? 4 : 3) void qk_norm_rope_b
     bf16_t* dx, float* __restrict__ part) {
   constexpr int HPW = 64 / G, U = batch_of<V>();
   __shared__ float red[QKN_WAVES][2][2 * V * G];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = d / 2, c = lane % G, h0 = lane / G;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int half = d / 2, c = lane % G, h0 = lane / G;
   const bool in = V * c < half;
   const int64_t ld = (int64_t)(nq + 2 * nkv) * d;
   const double turns = turns_of(lane, half, log2_theta);
@@ -298,7 +298,8 @@ __global__ __launch_bounds__(64 * QKN_WAVES, V == 4 ? 4 : 3) void qk_norm_rope_b
     };
     heads(0, nq, gains[0], sums[0]);
     heads(nq, nkv, gains[1], sums[1]);
-    if (dy != dx) copy_v(dy + row * ld + (int64_t)(nq + nkv) * d, dx + row * ld + (int64_t)(nq + nkv) * d, nkv * d, lane, seg, segs);
+    const int64_t v = row * ld + (int64_t)(nq + nkv) * d;
+    if (dy != dx) copy_v(dy + v, dx + v, nkv * d, lane, seg, segs);
   }
   if (!part) return;
 #pragma unroll
