@@ -604,8 +604,9 @@ int ls_gemm_tile_override(int32_t bm, int32_t bn);
  * "dh1", "dWqkv", "packed plan", "packed rope", "packed attention fwd",
  * "packed attention bwd", "packed qk norm rope", "packed qk norm rope bwd", "packed score attention fwd",
  * "packed score attention bwd", "gradient norm", "gradient clip", "logprob logits", "logprob rows",
- * "logprob top", "logprob gather", "logprob dz", "logprob dh", "logprob dE", "logprob scatter", "head loss logits", "head loss rows", "head loss gather",
- * "head loss dz", "head loss dh", "head loss dE", "head loss scatter", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
+ * "logprob top", "logprob gather", "logprob dz", "logprob dh", "logprob dE", "logprob scatter",
+ * "head loss logits", "head loss rows", "head loss gather", "head loss dz", "head loss dh", "head loss dE",
+ * "head loss scatter", and in ls_stack_fwd_bwd also "embedding fwd", "targets",
  * "logits", "cross-entropy", "dh head", "dE head", "loss", "embedding bwd",
  * and "adamw" for ls_adamw_step),
  * creating up to max_launches event pairs up front;

@@ -1449,9 +1449,9 @@ __global__ __launch_bounds__(256) void attn_bwd_dkdv_reduce(AttnShape sh, int hs
 // matrix cores busy across tile boundaries and while one wave waits.
 template <int D, bool PACKED, class SC>
 LS_DEV void dq_tile(const AttnShape& sh, const SC& sc, const QTile& qtile, bf16_t (&Ks)[2][BKV * D],
-                    bf16_t (&Vs)[2][BKV * D], const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout, const float* __restrict__ lse2,
-                    const float* __restrict__ Dv, bf16_t* __restrict__ dqkv, const float* __restrict__ rope_cs,
-                    float scale, float sl2) {
+                    bf16_t (&Vs)[2][BKV * D], const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ dout,
+                    const float* __restrict__ lse2, const float* __restrict__ Dv, bf16_t* __restrict__ dqkv,
+                    const float* __restrict__ rope_cs, float scale, float sl2) {
   constexpr int NSD = D / 16, NI = D / 32;
   constexpr int PS = 2 * NSD;                // slots of one block's S^T and dP^T (interleaved)
   constexpr int PQ = 2 * NI;                 // slots of one block's dQ^T
